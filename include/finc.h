@@ -513,6 +513,190 @@ int finc_conv1x1_forward(const float *x, float *y, const float *Wm, double *logd
 int finc_conv1x1_inverse(const float *y, float *x, const float *Wm, int B, int C, int H, int W,
                          void *workspace, hipStream_t stream);
 
+/* ---- Sequence operators: a model that reads a raster position by position ---
+ * A prior over the flow's latents (or the pixels) in raster order: residual
+ * rows through norm, projection, short causal convolution, selective scan and
+ * projection, trained on whole rasters and sampled one position at a time.
+ *
+ * Conventions beside the ones at the top:
+ *  - Activations have a type (FINC_F32, FINC_BF16, FINC_F16), one per call
+ *    where nothing else is said; parameters, scan states, statistics and the
+ *    parameters' gradients are fp32.  Sums are fp32 and results are rounded
+ *    once, to nearest even.
+ *  - Inner tensors are (B, D, L) with the L positions of a row contiguous (an
+ *    image's H*W), given with their steps: a finc_raster, so that a
+ *    projection's halves need no copy.  Inputs may repeat rows (steps of 0);
+ *    an output's elements must lie at different addresses.  Any alignment of
+ *    the element's size.  L < 2^30, B*D < 2^31; offsets are 64-bit.
+ *  - lengths: device ints, B, or NULL (all L); clamped to [0, L].  Positions at
+ *    or past a row's length are padding: whatever they hold (NaN included) takes
+ *    part in nothing, and outputs and gradients there are written as 0.
+ *  - slots (single-token calls): device ints, B, or NULL (row b's state is entry
+ *    b); row b's state is entry slots[b] of S.  A slot outside [0, S) marks an
+ *    idle row: its output is 0 and no state changes.  Slots of one call must
+ *    differ from each other.
+ *  - Outputs overlapping inputs, the workspace or each other: FINC_EINVAL,
+ *    except where a call names an alias it takes.
+ *  - Deterministic: fixed summation orders, no atomics. */
+enum { FINC_F32 = 0, FINC_BF16 = 1, FINC_F16 = 2 };
+
+#define FINC_MAX_TAPS 8
+#define FINC_MAX_STATE 64
+#define FINC_MAX_ROW 16384
+
+/* Element (b, d, t) at p + b*sb + d*sd + t (elements; p NULL: absent). */
+typedef struct {
+    void *p;
+    long long sb, sd;
+} finc_raster;
+
+/* Short causal convolution along every channel's raster, 1 <= K <= 8 taps:
+ *   p[b,d,t] = bias[d] + sum_j w[d,j] e[b,d,t+j],  y = p, or p sigmoid(p),
+ * e the K-1 inputs before the raster (state, or zeros) followed by x.
+ *   x, y: (B, D, L); w: (D, K); bias: D or NULL; state: (B, D, K-1) of x's type,
+ *   contiguous, or NULL; state_out: the same, written with the last K-1 of e up
+ *   to each row's length (of state where the row is shorter), or NULL. */
+typedef struct {
+    int type, B, D, L, K, silu;
+    finc_raster x, y;
+    const float *w, *bias;
+    const void *state;
+    void *state_out;
+    const int *lengths;
+} finc_conv_args;
+int finc_causal_conv_forward(const finc_conv_args *a, hipStream_t stream);
+
+/* Its gradients (a->y and a->state_out are not used).  dy (B, D, L); dx (B, D,
+ * L); dw (D, K); dbias (D) or NULL; dstate_out: the gradient of state_out,
+ * (B, D, K-1) of the type, or NULL for 0; dstate: (B, D, K-1), or NULL.
+ * workspace: device, >= finc_causal_conv_workspace_bytes(B, D, L, K) bytes,
+ * 256-byte aligned, overwritten. */
+typedef struct {
+    finc_raster dy, dx;
+    float *dw, *dbias;
+    const void *dstate_out;
+    void *dstate;
+    void *workspace;
+} finc_conv_grads;
+size_t finc_causal_conv_workspace_bytes(int B, int D, int L, int K);
+int finc_causal_conv_backward(const finc_conv_args *a, const finc_conv_grads *g,
+                              hipStream_t stream);
+
+/* One position: x, y (B, D) with rows sx, sy elements apart; state (S, D, K-1)
+ * of the type, contiguous, shifted by one input in place. */
+int finc_causal_conv_step(int type, const void *x, long long sx, void *y, long long sy,
+                          const float *w, const float *bias, void *state, const int *slots,
+                          int B, int S, int D, int K, int silu, hipStream_t stream);
+
+/* Selective state space scan, 1 <= N <= 64 states a channel, G groups of
+ * channels that share B and C (G divides D):
+ *   delta = softplus(dt + dt_bias) (softplus 0: dt + dt_bias itself),
+ *   h_t = exp(delta A) h_{t-1} + delta B_t x_t,
+ *   y_t = (C_t . h_t + Dskip x_t) * silu(z_t).
+ *   x, dt, z, y: (B, D, L), z absent for no gate; Bm, Cm: (B, G N, L) rasters
+ *   (state n of group g is row g N + n); A: (D, N), Dskip, dt_bias: D, each of
+ *   the two or NULL; state: h before the raster, (B, D, N) fp32, or NULL for 0;
+ *   state_out: h after each row's length, or NULL; may be state itself.
+ *   states: NULL, or for the gradients finc_selective_scan_states_bytes(B, D,
+ *   L, N) bytes, 256-byte aligned: h at the starts of the parts that the
+ *   backward recomputes, in a private layout. */
+typedef struct {
+    int type, B, D, L, N, G, softplus;
+    finc_raster x, dt, z, Bm, Cm, y;
+    const float *A, *Dskip, *dt_bias, *state;
+    float *state_out;
+    float *states;
+    const int *lengths;
+} finc_scan_args;
+size_t finc_selective_scan_states_bytes(int B, int D, int L, int N);
+int finc_selective_scan_forward(const finc_scan_args *a, hipStream_t stream);
+
+/* Its gradients, from the states that a forward of the same arguments wrote
+ * (a->state, a->state_out and a->y are not used).  dy, dx, ddt (and dz, with z):
+ * (B, D, L); dBm, dCm: (B, G N, L) rasters; dA (D, N); dDskip, ddt_bias: D or
+ * NULL; dstate_out: the gradient of state_out, (B, D, N), or NULL for 0; dstate:
+ * the gradient of state, or NULL.  workspace: device, >=
+ * finc_selective_scan_workspace_bytes(B, D, L, N, G) bytes, 256-byte aligned,
+ * overwritten. */
+typedef struct {
+    finc_raster dy, dx, ddt, dz, dBm, dCm;
+    float *dA, *dDskip, *ddt_bias;
+    const float *dstate_out;
+    float *dstate;
+    void *workspace;
+} finc_scan_grads;
+size_t finc_selective_scan_workspace_bytes(int B, int D, int L, int N, int G);
+int finc_selective_scan_backward(const finc_scan_args *a, const finc_scan_grads *g,
+                                 hipStream_t stream);
+
+/* One position: x, dt, z, y (B, D) and Bm, Cm (B, G N) with rows s* elements
+ * apart; state (S, D, N) fp32, contiguous, updated in place. */
+typedef struct {
+    int type, B, S, D, N, G, softplus;
+    const void *x, *dt, *z, *Bm, *Cm;
+    long long sx, sdt, sz, sB, sC, sy;
+    void *y;
+    const float *A, *Dskip, *dt_bias;
+    float *state;
+    const int *slots;
+} finc_scan_step_args;
+int finc_selective_scan_step(const finc_scan_step_args *a, hipStream_t stream);
+
+/* Dropout without a stored mask: sixteen bits u of every element (row, col) come
+ * from Philox4x32-10 (Salmon, Moraes, Dror and Shaw 2011) at counter offset +
+ * row ceil(D / 8) + col / 8 with key seed (64 bits each): word (col % 8) / 2,
+ * low half first.  An element is dropped where u < cut = rint(65536 p), the
+ * others are multiplied by 65536 / (65536 - cut), so that the mean is kept
+ * exactly; 0 <= p < 1, cut <= 65535.  The same call on dy is the gradient.  A
+ * call uses finc_dropout_counters(M, D) counters from offset on.
+ *   y = dropout(x), or residual + dropout(x): (M, D) with rows s* elements apart;
+ *   y may be x or residual itself, with its rows' step. */
+unsigned long long finc_dropout_counters(int M, int D);
+int finc_dropout(int type, const void *x, long long sx, const void *residual, long long sr,
+                 void *y, long long sy, int M, int D, double p, unsigned long long seed,
+                 unsigned long long offset, hipStream_t stream);
+
+/* Root-mean-square norm of rows with the residual's addition, D <= FINC_MAX_ROW:
+ *   r = residual + dropout(x) (p 0: residual + x),
+ *   y = r (mean_d r^2 + eps)^(-1/2) w,
+ * from r in fp32.  x, y: type; residual, r: rtype (type itself or FINC_F32),
+ * residual NULL for 0, r NULL where it is not wanted; w: D.  With scale (M
+ * floats) y is instead 8 bits wide, OCP e4m3: scale[m] = max(max_d |y| / 448,
+ * 2^-126), and y / scale rounded to nearest even.  A NaN in a row makes its
+ * outputs and its scale NaN.  r may be residual itself and y may be x itself,
+ * with their rows' steps. */
+typedef struct {
+    int type, rtype, M, D;
+    const void *x, *residual;
+    void *y, *r;
+    long long sx, sres, sy, sr;
+    const float *w;
+    float *scale;
+    double eps, p;
+    unsigned long long seed, offset;
+} finc_norm_args;
+int finc_add_norm_forward(const finc_norm_args *a, hipStream_t stream);
+
+/* Its gradients.  dy: type; r (as the forward wrote it), dr (the gradient that
+ * reaches r from elsewhere, or NULL for 0) and dresidual: rtype; dx: type, or
+ * NULL; dresidual, or NULL (dx and dresidual hold the same values where p is 0
+ * and the types agree); dw: D floats.  dx may be dy itself, dresidual dr
+ * itself, with their rows' steps.  workspace: device, >=
+ * finc_add_norm_workspace_bytes(M, D) bytes, 256-byte aligned, overwritten. */
+typedef struct {
+    int type, rtype, M, D;
+    const void *dy, *r, *dr;
+    void *dx, *dresidual;
+    long long sdy, sr, sdr, sdx, sdres;
+    const float *w;
+    float *dw;
+    double eps, p;
+    unsigned long long seed, offset;
+    void *workspace;
+} finc_norm_grad_args;
+size_t finc_add_norm_workspace_bytes(int M, int D);
+int finc_add_norm_backward(const finc_norm_grad_args *a, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

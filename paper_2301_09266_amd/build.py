@@ -1,8 +1,9 @@
 """Build the HIP library in-tree for gfx950: paper_2301_09266_amd/csrc/libfinc.so.
 
 finc.hip compiles as several translation units in parallel (FINC_PART: one
-per group of inverse kernel instances, and one with everything else), flow.hip
-as one more; all are linked into the one shared library.
+per group of inverse kernel instances, and one with everything else), flow.hip,
+backward.hip and the sequence operators' sources as one more each; all are linked
+into the one shared library.
 """
 from __future__ import annotations
 
@@ -17,6 +18,8 @@ ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "finc.hip")
 FLOW_SRC = os.path.join(PKG, "csrc", "flow.hip")
 BACKWARD_SRC = os.path.join(PKG, "csrc", "backward.hip")
+SEQ_SRCS = [os.path.join(PKG, "csrc", f)
+            for f in ("selective_scan.hip", "causal_conv.hip", "add_norm.hip")]
 LIB = os.path.join(PKG, "csrc", "libfinc.so")
 CALIB_SRC = os.path.join(PKG, "csrc", "calib.hip")
 CALIB_LIB = os.path.join(PKG, "csrc", "libfinc_calib.so")
@@ -43,8 +46,8 @@ def build(out: str = LIB, extra: list[str] | None = None) -> str:
     """Compile every part of finc.hip and link them into `out`."""
     tmpdir = tempfile.mkdtemp(prefix="finc_build_")
     try:
-        # finc.hip in parts (FINC_PART), then flow.hip and backward.hip
-        parts = [-2] + list(range(INVERSE_GROUPS)) + [FLOW_SRC, BACKWARD_SRC]
+        # finc.hip in parts (FINC_PART), then the other sources
+        parts = [-2] + list(range(INVERSE_GROUPS)) + [FLOW_SRC, BACKWARD_SRC, *SEQ_SRCS]
         objs = [os.path.join(tmpdir, f"part{i}.o") for i in range(len(parts))]
 
         def compile_part(i: int) -> None:
