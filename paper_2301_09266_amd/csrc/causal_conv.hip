@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kThreads) void conv_forward_kernel(ConvArgs a) {
 #pragma unroll
         for (int j = 0; j < K; ++j)
             p = __builtin_fmaf(w[j], v[H - (K - 1) + i + j], p);
-        y[i] = t0 + i < n ? (SILU ? silu(p) : p) : 0.0f;
+        y[i] = keep_if(t0 + i < n, SILU ? silu(p) : p);
     }
     store_upto<E, V>((E *)a.y + (b * a.yb + d * a.yd) + t0, a.L - t0, y);
     if (t0 == 0 && a.state_out) {
@@ -132,12 +132,10 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
         // padding may hold anything, also to the left of a tile that lies in it
 #pragma unroll
         for (int i = 0; i < H + V + H; ++i)
-            if (t0 - H + i >= n)
-                v[i] = 0.0f;
+            v[i] = keep_if(t0 - H + i < n, v[i]);
 #pragma unroll
         for (int i = 0; i < V + H; ++i)
-            if (t0 + i >= n)
-                g[i] = 0.0f;
+            g[i] = keep_if(t0 + i < n, g[i]);
         if (SILU) {
 #pragma unroll
             for (int i = 0; i < V + Q; ++i) {
@@ -145,8 +143,7 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
 #pragma unroll
                 for (int j = 0; j < K; ++j)
                     p = __builtin_fmaf(w[j], v[H - Q + i + j], p);
-                const float s = g[i] * silu_grad(p, sigmoid(p));
-                g[i] = t0 + i < n ? s : 0.0f;
+                g[i] = keep_if(t0 + i < n, g[i] * silu_grad(p, sigmoid(p)));
             }
         }
         float dx[V];
@@ -167,8 +164,7 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
             const int t = t0 + i;
             if (dso && t < n && t + Q >= n)
                 dx[i] += (float)dso[t + Q - n];
-            if (t >= n)
-                dx[i] = 0.0f;
+            dx[i] = keep_if(t < n, dx[i]);
         }
         store_upto<E, V>((E *)a.dx + (b * a.ob + d * a.od) + t0, a.L - t0, dx);
         if (t0 == 0 && a.dstate) {

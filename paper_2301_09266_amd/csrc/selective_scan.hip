@@ -37,7 +37,8 @@ struct ScanArgs {
     float *state_out, *states;
     const int *lengths;
     int B, D, L, N, G, Dg;   // Dg: channels of a group
-    int softplus, parts;     // parts: of 16 T positions, of the whole raster
+    int softplus, parts;     // parts: that states are kept for, of the whole raster
+    int every;               // a forward's lanes between two of them
     int blocks;              // of channels, in a group
 };
 
@@ -95,77 +96,127 @@ __device__ inline int tile_at(int n, int j4, int lane) {
     return ((n * (T / 4) + j4) * 16 + lane) * 4;
 }
 
-template <int S>
-struct Out {
-    float h[S];
-};
-
-// S states of a row's part: adds C h to y and gives the state at the part's end in
-// the row's last lane; `in` are the states before the part.
+// S states of a row's part: adds C h to y, and gives the states at the start of the
+// lane's run and at the part's end (in the row's last lane); `in` are the states
+// before the part.
 template <int T, int S>
-__device__ inline Out<S> scan_states(const float *tb, const float *tc, const int (&n)[S],
-                                     const float (&A2)[S], const float (&in)[S], int lane,
-                                     const float (&delta)[T], const float (&dx)[T], float sum,
-                                     float (&y)[T], float (&start)[S]) {
-    float a[S][T], h[S], m[S];
+__device__ inline void scan_states(const float *tb, const float *tc, const int (&n)[S],
+                                   const float (&A2)[S], const float (&in)[S], int lane,
+                                   const float (&delta)[T], const float (&dx)[T], float sum,
+                                   float (&y)[T], float (&start)[S], float (&end)[S]) {
+    float a[S][T], b[S][T], m[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        h[s] = 0.0f;
+        end[s] = 0.0f;
 #pragma unroll
         for (int j4 = 0; j4 < T / 4; ++j4) {
-            const float4 b = *(const float4 *)(tb + tile_at<T>(n[s], j4, lane));
-            const float bv[4] = {b.x, b.y, b.z, b.w};
+            const float4 v = *(const float4 *)(tb + tile_at<T>(n[s], j4, lane));
+            const float bv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int j = 4 * j4 + i;
                 a[s][j] = __builtin_amdgcn_exp2f(A2[s] * delta[j]);
-                h[s] = __builtin_fmaf(a[s][j], h[s], dx[j] * bv[i]);
+                b[s][j] = dx[j] * bv[i];
+                end[s] = j ? __builtin_fmaf(a[s][j], end[s], b[s][j]) : b[s][j];
             }
         }
         m[s] = __builtin_amdgcn_exp2f(A2[s] * sum);
     }
-    scan_up(m, h);
-    Out<S> end;
+    scan_up(m, end);
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        end.h[s] = __builtin_fmaf(m[s], in[s], h[s]);
-        float g = start[s] = neighbour<kFromLower>(in[s], end.h[s]);
+        end[s] = __builtin_fmaf(m[s], in[s], end[s]);
+        float h = start[s] = neighbour<kFromLower>(in[s], end[s]);
 #pragma unroll
         for (int j4 = 0; j4 < T / 4; ++j4) {
-            const float4 b = *(const float4 *)(tb + tile_at<T>(n[s], j4, lane));
-            const float4 c = *(const float4 *)(tc + tile_at<T>(n[s], j4, lane));
-            const float bv[4] = {b.x, b.y, b.z, b.w}, cv[4] = {c.x, c.y, c.z, c.w};
+            const float4 v = *(const float4 *)(tc + tile_at<T>(n[s], j4, lane));
+            const float cv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int j = 4 * j4 + i;
-                g = __builtin_fmaf(a[s][j], g, dx[j] * bv[i]);
-                y[j] = __builtin_fmaf(cv[i], g, y[j]);
+                h = __builtin_fmaf(a[s][j], h, b[s][j]);
+                y[j] = __builtin_fmaf(cv[i], h, y[j]);
             }
         }
     }
-    return end;
 }
 
-// One block: CB = 16 / W channels of one batch row and group, W waves sharing a
-// channel's states (each N / W of them) where there are few channels.
+// Position t of a part in its channel's or its state's slots (see tile_at).
+template <int T>
+__device__ inline int slot_at(int t) {
+    return ((t % T / 4) * 16 + t / T) * 4 + t % 4;
+}
+
+// Elements as they lie in memory, for loads that are under way while others are used;
+// 0 past `count`.
+template <typename E, int N>
+__device__ inline typename Vec<E, N>::type load_raw(const E *p, int count) {
+    typename Vec<E, N>::type v;
+    if (count >= N)
+        return *(const typename Vec<E, N>::type *)p;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        v[i] = (E)0.0f;
+    if (count > 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = p[min(i, count - 1)];
+#pragma unroll
+        for (int i = 1; i < N; ++i)
+            v[i] = i < count ? v[i] : (E)0.0f;
+    }
+    return v;
+}
+
+constexpr int kUnit = 8;   // elements of B and C that a thread moves at once
+
+// What a thread loads of B and C for one part: unit u of 2 N P / 8.
+template <typename E, int T>
+__device__ inline typename Vec<E, kUnit>::type load_tile(const ScanArgs &a, int b, int grp, int u,
+                                                         int p0, int n_pos) {
+    constexpr int Q = 16 * T / kUnit;
+    const int r = u / Q, q = (u % Q) * kUnit;
+    const E *row = (r >= a.N ? a.Cm : a.Bm)
+                       .row<const E>(b, (long long)grp * a.N + (r >= a.N ? r - a.N : r));
+    return load_raw<E, kUnit>(row + p0 + q, n_pos - p0 - q);
+}
+template <typename E, int T>
+__device__ inline void store_tile(float *tb, int u, typename Vec<E, kUnit>::type v) {
+    constexpr int Q = 16 * T / kUnit;
+    const int r = u / Q, q = (u % Q) * kUnit;   // C's rows follow B's
+#pragma unroll
+    for (int k = 0; k < kUnit; k += 4)
+        *(float4 *)(tb + r * 16 * T + slot_at<T>(q + k)) =
+            make_float4((float)v[k], (float)v[k + 1], (float)v[k + 2], (float)v[k + 3]);
+}
+
+// One block: CB = 16 / W channels of one batch row and group.  W waves share a
+// channel's states (each N / W of them) where there are few channels; then a wave
+// prepares one channel's positions for all of them and sums that channel's outputs.
+// The next part's loads are under way while a part is computed.
 template <typename E, int T, int W>
-__global__ __launch_bounds__(kThreads) void scan_forward_kernel(ScanArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void scan_forward_kernel(ScanArgs a) {
     constexpr int CB = 16 / W, P = 16 * T;   // P: positions of a part
+    constexpr int I = T / W;                 // positions that a thread prepares
+    constexpr int K = 4;                     // units of B and C loaded ahead
     extern __shared__ __attribute__((aligned(16))) float lds[];
     float *tb = lds, *tc = tb + a.N * P;
     float *hs = tc + a.N * P;                // the states between parts, CB x N
     float *As = hs + CB * a.N;               // A log2 e, CB x N
-    float *red = As + CB * a.N;              // W > 1: the waves' sums of y
+    float *pre = As + CB * a.N;              // W > 1: delta, delta x of CB channels
+    float *red = pre + 2 * CB * P;           // W > 1: the waves' sums of y
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 15, rowi = (tid >> 4) & 3;
     int blk = blockIdx.x;
     const int cb = blk % a.blocks;
     blk /= a.blocks;
     const int grp = blk % a.G, b = blk / a.G;
-    const int split = wave % W, cl = (wave / W) * 4 + rowi;   // channel in the block
-    const int dg = cb * CB + cl;
-    const bool live = dg < a.Dg;
-    const int d = grp * a.Dg + (live ? dg : 0);
+    const int split = wave % W;
+    const int cl = W > 1 ? rowi : wave * 4 + rowi;   // the channel whose states it scans
+    const int cp = tid * I / P, pos = tid * I % P;   // the one whose positions it prepares
+    const bool live = cb * CB + cp < a.Dg;
+    const int d = grp * a.Dg + (live ? cb * CB + cp : 0);
     const int n_pos = row_length(a.lengths, b, a.L);
+    const int units = 2 * a.N * (P / kUnit);
     for (int i = tid; i < CB * a.N; i += kThreads) {
         const int c = i / a.N, n = i - c * a.N, dd = cb * CB + c;
         const bool ok = dd < a.Dg;
@@ -175,83 +226,145 @@ __global__ __launch_bounds__(kThreads) void scan_forward_kernel(ScanArgs a) {
     }
     const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
     const float skip = a.Dskip ? a.Dskip[d] : 0.0f;
-    const E *xr = a.x.row<const E>(b, d), *dr = a.dt.row<const E>(b, d);
-    const E *zr = a.z.p ? a.z.row<const E>(b, d) : nullptr;
-    E *yr = a.y.row<E>(b, d);
+    const E *xr = a.x.row<const E>(b, d) + pos, *dr = a.dt.row<const E>(b, d) + pos;
+    const E *zr = a.z.p ? a.z.row<const E>(b, d) + pos : nullptr;
+    E *yr = a.y.row<E>(b, d) + pos;
+    const int own = live ? n_pos - pos : 0;
     const int parts = (n_pos + P - 1) / P;
-    for (int part = 0; part < parts; ++part) {
-        const int p0 = part * P, t0 = p0 + lane * T;
-        // positions past the row's length: delta 0 keeps the state, B and C are 0
-        for (int u = tid; u < 2 * a.N * (P / 4); u += kThreads) {
-            const int which = u >= a.N * (P / 4), v = u - which * a.N * (P / 4);
-            const int n = v / (P / 4), q = v - n * (P / 4);
-            float t[4];
-            load_upto<E, 4>((which ? a.Cm : a.Bm).row<const E>(b, grp * a.N + n) + p0 + 4 * q,
-                            n_pos - p0 - 4 * q, t);
-            *(float4 *)((which ? tc : tb) + tile_at<T>(n, q % (T / 4), q / (T / 4))) =
-                make_float4(t[0], t[1], t[2], t[3]);
-        }
-        float x[T], delta[T], dx[T], y[T];
-        load_upto<E, T>(xr + t0, live ? n_pos - t0 : 0, x);
-        load_upto<E, T>(dr + t0, live ? n_pos - t0 : 0, delta);
-        float sum = 0.0f;
+    typename Vec<E, I>::type nx, nd, nz;
+    typename Vec<E, kUnit>::type nt[K];
+    if (parts > 0) {
+        nx = load_raw<E, I>(xr, own);
+        nd = load_raw<E, I>(dr, own);
 #pragma unroll
-        for (int j = 0; j < T; ++j) {
-            float v = delta[j] + bias;
+        for (int k = 0; k < K; ++k)
+            if (tid + k * kThreads < units)
+                nt[k] = load_tile<E, T>(a, b, grp, tid + k * kThreads, 0, n_pos);
+    }
+    for (int part = 0; part < parts; ++part) {
+        const int p0 = part * P;
+        // positions past the row's length: delta 0 keeps the state, B and C are 0
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (tid + k * kThreads < units)
+                store_tile<E, T>(tb, tid + k * kThreads, nt[k]);
+        for (int u = tid + K * kThreads; u < units; u += kThreads)
+            store_tile<E, T>(tb, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
+        float x[I], delta[T], dx[T], y[T];
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            x[i] = (float)nx[i];
+            float v = (float)nd[i] + bias;
             if (a.softplus)
                 v = softplus(v);
-            delta[j] = live && t0 + j < n_pos ? v : 0.0f;
-            dx[j] = delta[j] * x[j];
-            sum += delta[j];
-            y[j] = 0.0f;
-        }
-        __syncthreads();
-        for (int i = split; i < a.N; i += W) {
-            const int n[1] = {i};
-            const float A2[1] = {As[cl * a.N + i]}, in[1] = {hs[cl * a.N + i]};
-            float start[1];
-            const Out<1> end =
-                scan_states<T, 1>(tb, tc, n, A2, in, lane, delta, dx, sum, y, start);
-            if (a.states && live && lane == 0)
-                a.states[(((long long)b * a.D + d) * a.parts + part) * a.N + i] = in[0];
-            if (lane == 15)
-                hs[cl * a.N + i] = end.h[0];
+            delta[i] = keep_if(i < own - p0, v);
+            dx[i] = delta[i] * x[i];
         }
         if (W > 1) {
-            float4 *r = (float4 *)red;
+            float *q = pre + cp * P + slot_at<T>(pos);
 #pragma unroll
-            for (int j4 = 0; j4 < T / 4; ++j4)
-                r[(wave * (T / 4) + j4) * 64 + (tid & 63)] =
-                    make_float4(y[4 * j4], y[4 * j4 + 1], y[4 * j4 + 2], y[4 * j4 + 3]);
-            __syncthreads();
-            if (split == 0) {
-#pragma unroll
-                for (int w = 1; w < W; ++w)
-#pragma unroll
-                    for (int j4 = 0; j4 < T / 4; ++j4) {
-                        const float4 v = r[((wave + w) * (T / 4) + j4) * 64 + (tid & 63)];
-                        y[4 * j4] += v.x;
-                        y[4 * j4 + 1] += v.y;
-                        y[4 * j4 + 2] += v.z;
-                        y[4 * j4 + 3] += v.w;
-                    }
+            for (int i = 0; i < I; ++i) {
+                q[i] = delta[i];
+                q[CB * P + i] = dx[i];
             }
-        }
-        if (split == 0 && live) {
-            float z[T];
-            if (zr)
-                load_upto<E, T>(zr + t0, n_pos - t0, z);
-#pragma unroll
-            for (int j = 0; j < T; ++j) {
-                y[j] = __builtin_fmaf(skip, x[j], y[j]);
-                if (zr)
-                    y[j] *= silu(z[j]);
-                if (t0 + j >= n_pos)
-                    y[j] = 0.0f;
-            }
-            store_upto<E, T>(yr + t0, a.L - t0, y);
         }
         __syncthreads();
+        // under way until the part is done
+        if (zr)
+            nz = load_raw<E, I>(zr + p0, own - p0);
+        if (part + 1 < parts) {
+            nx = load_raw<E, I>(xr + p0 + P, own - p0 - P);
+            nd = load_raw<E, I>(dr + p0 + P, own - p0 - P);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (tid + k * kThreads < units)
+                    nt[k] = load_tile<E, T>(a, b, grp, tid + k * kThreads, p0 + P, n_pos);
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int j4 = 0; j4 < T / 4; ++j4) {
+            if (W > 1) {
+                const float *q = pre + cl * P + (j4 * 16 + lane) * 4;
+                const float4 u = *(const float4 *)q, v = *(const float4 *)(q + CB * P);
+                delta[4 * j4] = u.x;
+                delta[4 * j4 + 1] = u.y;
+                delta[4 * j4 + 2] = u.z;
+                delta[4 * j4 + 3] = u.w;
+                dx[4 * j4] = v.x;
+                dx[4 * j4 + 1] = v.y;
+                dx[4 * j4 + 2] = v.z;
+                dx[4 * j4 + 3] = v.w;
+            }
+#pragma unroll
+            for (int j = 4 * j4; j < 4 * j4 + 4; ++j) {
+                sum += delta[j];
+                y[j] = 0.0f;
+            }
+        }
+        const int cs = cb * CB + cl;
+        // states are kept every a.every lanes' runs, for the gradients
+        float *kept = a.states && cs < a.Dg && lane % a.every == 0
+                          ? a.states + ((((long long)b * a.D + grp * a.Dg + cs) * a.parts +
+                                         (long long)part * (16 / a.every) + lane / a.every) *
+                                        a.N)
+                          : nullptr;
+        if (kept && p0 + lane * T >= n_pos)
+            kept = nullptr;   // its part is not in the row
+        float *hr = hs + cl * a.N;
+        const float *Ar = As + cl * a.N;
+        int i = split;
+        for (; i + W < a.N; i += 2 * W) {
+            const int n[2] = {i, i + W};
+            const float A2[2] = {Ar[n[0]], Ar[n[1]]}, in[2] = {hr[n[0]], hr[n[1]]};
+            float start[2], end[2];
+            scan_states<T, 2>(tb, tc, n, A2, in, lane, delta, dx, sum, y, start, end);
+            if (kept) {
+                kept[n[0]] = start[0];
+                kept[n[1]] = start[1];
+            }
+            if (lane == 15) {
+                hr[n[0]] = end[0];
+                hr[n[1]] = end[1];
+            }
+        }
+        for (; i < a.N; i += W) {
+            const int n[1] = {i};
+            const float A2[1] = {Ar[i]}, in[1] = {hr[i]};
+            float start[1], end[1];
+            scan_states<T, 1>(tb, tc, n, A2, in, lane, delta, dx, sum, y, start, end);
+            if (kept)
+                kept[i] = start[0];
+            if (lane == 15)
+                hr[i] = end[0];
+        }
+        if (W > 1) {
+            float4 *r = (float4 *)red + (wave * (T / 4)) * 64 + (tid & 63);
+#pragma unroll
+            for (int j4 = 0; j4 < T / 4; ++j4)
+                r[j4 * 64] = make_float4(y[4 * j4], y[4 * j4 + 1], y[4 * j4 + 2], y[4 * j4 + 3]);
+            __syncthreads();
+            const float *q = red + cp * 64 + slot_at<T>(pos) % 64 + slot_at<T>(pos) / 64 * 256;
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                y[i] = q[i];
+#pragma unroll
+                for (int w = 1; w < W; ++w)
+                    y[i] += q[w * (T / 4) * 256 + i];
+            }
+        }
+        if (live) {
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                float v = __builtin_fmaf(skip, x[i], y[i]);
+                if (zr)
+                    v *= silu((float)nz[i]);
+                y[i] = keep_if(i < own - p0, v);
+            }
+            store_upto<E, I>(yr + p0, a.L - p0 - pos, y);
+        }
+        // the next part's tile, and its positions, take the place of this one's
+        if (W == 1)
+            __syncthreads();
     }
     // padding
     for (int c = 0; c < CB; ++c) {
@@ -274,12 +387,14 @@ __global__ __launch_bounds__(kThreads) void scan_forward_kernel(ScanArgs a) {
 // ---- gradients ----------------------------------------------------------------------
 // With G_t = a_t g_t the gradient of the state obeys g_t = C_t dy_t + G_{t+1}: the
 // same scan towards lower positions.  A workgroup owns a set of channels of one batch
-// row and walks the parts from the last to the first; within a part it takes 4 H
-// channels at a time.  W waves share the states of four channels, four states a wave
-// and a channel a row of 16 lanes, so that a wave keeps B, C and their gradients of
-// its four states in registers while the channels pass: dB and dC are sums over the
-// channels, and reach memory once a set.  The states inside a part are recomputed from
-// the one that the forward kept at its start.
+// row and walks the parts from the last to the first.  A wave takes a channel at a
+// time: its four rows of 16 lanes hold a quarter of the states each, S a lane, over
+// the same positions.  So a lane keeps the gradients of B and C of its own states and
+// positions in registers while the wave's channels pass, the sums over the states are
+// sums over the four rows, and the waves meet only where a part ends.  Each row
+// prepares a quarter of the positions and hands them to the others through LDS; the
+// sums come back to the row that prepared them.  The states inside a part are
+// recomputed from the one that the forward kept at its start.
 
 struct GradArgs {
     ScanArgs f;
@@ -291,33 +406,56 @@ struct GradArgs {
     int set, sets;    // channels of a set, sets of a group
 };
 
+constexpr int kGradWaves = 8;
+
+// States a lane whose gradients the waves exchange at once.
 template <int T>
-__device__ inline int slot_at(int t) {
-    return ((t % T / 4) * 16 + t / T) * 4 + t % 4;
+constexpr int kSwap = 32 / T;
+
+inline size_t backward_lds(int N, int T, int set) {
+    return ((size_t)2 * N * 16 * T + kGradWaves * 3 * 16 * T + (size_t)3 * set * N +
+            (size_t)2 * set + (size_t)2 * 32 * 64 * (kGradWaves / 2)) * 4;
 }
 
-// Positions of one channel that a thread prepares and finishes.
-template <int T, int W>
-constexpr int kItems = T / W > 1 ? T / W : 1;
-
-inline size_t backward_lds(int N, int T, int W, int H, int set) {
-    return ((size_t)3 * 4 * H * 16 * T + (size_t)3 * T * 64 * W * H + (size_t)3 * set * N +
-            (size_t)set * W * 2) * 4;
+// The sums over the four rows of T values a lane: row r gets those of positions
+// r T / 4 and on.
+__device__ inline float swap32(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a),
+                                                    __builtin_bit_cast(unsigned, b), false, false);
+    return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+__device__ inline float swap16(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a),
+                                                    __builtin_bit_cast(unsigned, b), false, false);
+    return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+template <int T>
+__device__ inline void sum_rows(const float (&v)[T], float (&out)[T / 4]) {
+    float u[T / 2];
+#pragma unroll
+    for (int j = 0; j < T / 2; ++j)
+        u[j] = swap32(v[j], v[j + T / 2]);
+#pragma unroll
+    for (int j = 0; j < T / 4; ++j)
+        out[j] = swap16(u[j], u[j + T / 4]);
 }
 
-template <typename E, int T, int W, int H>
-__global__ __launch_bounds__(64 * W * H) void scan_backward_kernel(GradArgs ga) {
-    constexpr int P = 16 * T, CB = 4 * H, TH = 64 * W * H, I = kItems<T, W>;
+template <typename E, int T, int S>
+__global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs ga) {
+    constexpr int P = 16 * T, I = T / 4, TH = 64 * kGradWaves, SW = S < kSwap<T> ? S : kSwap<T>;
     const ScanArgs &a = ga.f;
     extern __shared__ __attribute__((aligned(16))) float lds[];
-    float *pre = lds;                              // delta, delta x, dy of CB channels
-    float *sums = pre + 3 * CB * P;                // the waves' sums over their states
-    float *carry = sums + 3 * T * 64 * W * H;      // G at the part's end, set x N
+    float *tb = lds, *tc = tb + a.N * P;
+    float *pre = tc + a.N * P;                     // delta, delta x, dy of a wave's channel
+    float *swp = pre + kGradWaves * 3 * P;         // half the waves' gradients of B and C
+    float *carry = swp + 2 * 32 * 64 * (kGradWaves / 2);   // G at the part's end, set x N
     float *As = carry + ga.set * a.N;              // A log2 e
     float *dAs = As + ga.set * a.N;                // dA
-    float *ps = dAs + ga.set * a.N;                // dDskip, ddt_bias: set x W rows x 2
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 15, rowi = (tid >> 4) & 3;
-    const int w = wave % W, half = wave / W, n0 = 4 * w;
+    float *ps = dAs + ga.set * a.N;                // dDskip, ddt_bias: set x 2
+    const int tid = threadIdx.x, lane = tid & 15, rowi = (tid >> 4) & 3;
+    // uniform: a wave's rows of activations have their addresses in scalar registers
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n0 = rowi * S;
     int blk = blockIdx.x;
     const int set = blk % ga.sets;
     blk /= ga.sets;
@@ -327,235 +465,242 @@ __global__ __launch_bounds__(64 * W * H) void scan_backward_kernel(GradArgs ga) 
     const long long first = (long long)grp * a.Dg + c0;
     const int n_pos = row_length(a.lengths, b, a.L);
     const int parts = (n_pos + P - 1) / P;
+    const int units = 2 * a.N * (P / kUnit);
     for (int i = tid; i < ga.set * a.N; i += TH) {
         const bool ok = i < count * a.N;
         As[i] = ok ? a.A[first * a.N + i] * kLog2e : 0.0f;
         carry[i] = ok && ga.dstate_out ? ga.dstate_out[((long long)b * a.D + first) * a.N + i] : 0.0f;
         dAs[i] = 0.0f;
     }
-    for (int i = tid; i < ga.set * W * 2; i += TH)
+    for (int i = tid; i < count * 2; i += TH)
         ps[i] = 0.0f;
-    __syncthreads();
+    // the positions of a part that this lane prepares, and the wave's place for them
+    const int pos = lane * T + rowi * I;
+    float *mine = pre + wave * 3 * P;
+    typedef typename Vec<E, I>::type Raw;
+    Raw nx, nd, ng, nz;
+    float nin[S];
+    auto fetch = [&](int c, int part) {
+        const int d = (int)first + c, p0 = part * P, left = n_pos - p0 - pos;
+        nx = load_raw<E, I>(a.x.row<const E>(b, d) + p0 + pos, left);
+        nd = load_raw<E, I>(a.dt.row<const E>(b, d) + p0 + pos, left);
+        ng = load_raw<E, I>(ga.dy.row<const E>(b, d) + p0 + pos, left);
+        if (a.z.p)
+            nz = load_raw<E, I>(a.z.row<const E>(b, d) + p0 + pos, left);
+        const float *st = a.states + (((long long)b * a.D + d) * a.parts + part) * a.N;
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+            nin[s] = n0 + s < a.N ? st[n0 + s] : 0.0f;
+    };
+    if (parts > 0 && wave < count)
+        fetch(wave, parts - 1);
     for (int part = parts - 1; part >= 0; --part) {
         const int p0 = part * P;
-        float Bv[4][T], Cv[4][T], dB[4][T], dC[4][T];
+        for (int u = tid; u < units; u += TH)
+            store_tile<E, T>(tb, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
+        __syncthreads();
+        float dB[S][T], dC[S][T];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const bool ok = n0 + s < a.N;
-            const long long r = (long long)grp * a.N + (ok ? n0 + s : 0);
-            const int left = ok ? n_pos - p0 - lane * T : 0;
-            load_upto<E, T>(a.Bm.row<const E>(b, r) + p0 + lane * T, left, Bv[s]);
-            load_upto<E, T>(a.Cm.row<const E>(b, r) + p0 + lane * T, left, Cv[s]);
+        for (int s = 0; s < S; ++s)
 #pragma unroll
             for (int j = 0; j < T; ++j)
                 dB[s][j] = dC[s][j] = 0.0f;
-        }
-        for (int cb = 0; cb < count; cb += CB) {
-            // what a position needs, once a channel: I neighbours a thread
-            const int at = tid * I, cq = at / P, pos = at - cq * P;
-            const bool mine = cq < CB, live = mine && cb + cq < count;
-            const int d = (int)first + (live ? cb + cq : 0);
-            float x[I], delta[I], slope[I], z[I], dout[I], dy[I];
-            const int left = live ? n_pos - p0 - pos : 0;
-            load_upto<E, I>(a.x.row<const E>(b, d) + p0 + pos, left, x);
-            load_upto<E, I>(a.dt.row<const E>(b, d) + p0 + pos, left, delta);
-            load_upto<E, I>(ga.dy.row<const E>(b, d) + p0 + pos, left, dout);
-            if (a.z.p)
-                load_upto<E, I>(a.z.row<const E>(b, d) + p0 + pos, left, z);
+        for (int c = wave; c < count; c += kGradWaves) {
+            const int d = (int)first + c, left = n_pos - p0 - pos;
+            float x[I], delta[I], slope[I], z[I], dout[I], dy[I], in[S];
             const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
+            const float skip = a.Dskip ? a.Dskip[d] : 0.0f;
 #pragma unroll
             for (int i = 0; i < I; ++i) {
-                const float v = delta[i] + bias;
+                const float v = (float)nd[i] + bias;
+                x[i] = (float)nx[i];
+                dout[i] = (float)ng[i];
                 slope[i] = a.softplus ? sigmoid(v) : 1.0f;
-                delta[i] = i < left ? (a.softplus ? softplus(v) : v) : 0.0f;
+                delta[i] = keep_if(i < left, a.softplus ? softplus(v) : v);
+                z[i] = a.z.p ? (float)nz[i] : 0.0f;
                 dy[i] = a.z.p ? dout[i] * silu(z[i]) : dout[i];
+                float *q = mine + slot_at<T>(pos + i);
+                q[0] = delta[i];
+                q[P] = delta[i] * x[i];
+                q[2 * P] = dy[i];
             }
-            if (mine) {
-                float *q = pre + cq * P;
 #pragma unroll
-                for (int i = 0; i < I; ++i) {
-                    q[slot_at<T>(pos + i)] = delta[i];
-                    q[CB * P + slot_at<T>(pos + i)] = delta[i] * x[i];
-                    q[2 * CB * P + slot_at<T>(pos + i)] = dy[i];
+            for (int s = 0; s < S; ++s)
+                in[s] = nin[s];
+            // the next channel's, under way
+            if (c + kGradWaves < count)
+                fetch(c + kGradWaves, part);
+            else if (part > 0)
+                fetch(wave, part - 1);
+            __builtin_amdgcn_wave_barrier();
+            float de[T], dx[T], g[T], gB[T], sA[T], yv[T], sum = 0.0f;
+#pragma unroll
+            for (int j4 = 0; j4 < T / 4; ++j4) {
+                const float *q = mine + (j4 * 16 + lane) * 4;
+                const float4 u = *(const float4 *)q, v = *(const float4 *)(q + P);
+                const float4 e = *(const float4 *)(q + 2 * P);
+                const float uu[4] = {u.x, u.y, u.z, u.w}, vv[4] = {v.x, v.y, v.z, v.w};
+                const float ee[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = 4 * j4 + i;
+                    de[j] = uu[i];
+                    dx[j] = vv[i];
+                    g[j] = ee[i];
+                    sum += uu[i];
+                    gB[j] = sA[j] = yv[j] = 0.0f;
                 }
             }
-            __syncthreads();
-            {
-                const int ch = half * 4 + rowi;                 // of the CB channels
-                const int cs = min(cb + ch, ga.set - 1);        // in the set
-                const bool here = cb + ch < count;
-                const float *q = pre + ch * P + lane * 4;
-                float de[T], dx[T], g[T], gB[T], sA[T], yv[T], sum = 0.0f;
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const bool has = n0 + s < a.N;
+                const int n = has ? n0 + s : 0;
+                const float A2 = has ? As[c * a.N + n] : 0.0f;
+                const float after = has ? carry[c * a.N + n] : 0.0f;
+                float av[T], h[T], Bv[T], Cv[T], m[1], e[1] = {0.0f};
 #pragma unroll
                 for (int j4 = 0; j4 < T / 4; ++j4) {
-                    const float4 u = *(const float4 *)(q + j4 * 64);
-                    const float4 v = *(const float4 *)(q + CB * P + j4 * 64);
-                    const float4 e = *(const float4 *)(q + 2 * CB * P + j4 * 64);
-                    const float uu[4] = {u.x, u.y, u.z, u.w}, vv[4] = {v.x, v.y, v.z, v.w};
-                    const float ee[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int j = 4 * j4 + i;
-                        de[j] = uu[i];
-                        dx[j] = vv[i];
-                        g[j] = ee[i];
-                        sum += uu[i];
-                        gB[j] = sA[j] = yv[j] = 0.0f;
-                    }
+                    const float4 u = *(const float4 *)(tb + tile_at<T>(n, j4, lane));
+                    const float4 v = *(const float4 *)(tc + tile_at<T>(n, j4, lane));
+                    Bv[4 * j4] = u.x;
+                    Bv[4 * j4 + 1] = u.y;
+                    Bv[4 * j4 + 2] = u.z;
+                    Bv[4 * j4 + 3] = u.w;
+                    Cv[4 * j4] = v.x;
+                    Cv[4 * j4 + 1] = v.y;
+                    Cv[4 * j4 + 2] = v.z;
+                    Cv[4 * j4 + 3] = v.w;
                 }
-                const float *st =
-                    a.states + (((long long)b * a.D + first + (here ? cb + ch : 0)) * a.parts +
-                                part) * a.N;
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const int n = n0 + s;
-                    if (n >= a.N)   // the same in the whole wave
-                        break;
-                    const float A2 = As[cs * a.N + n], in = here ? st[n] : 0.0f;
-                    const float after = carry[cs * a.N + n];
-                    float av[T], h[T], m[1], e[1] = {0.0f};
-#pragma unroll
-                    for (int j = 0; j < T; ++j) {
-                        av[j] = __builtin_amdgcn_exp2f(A2 * de[j]);
-                        e[0] = __builtin_fmaf(av[j], e[0], dx[j] * Bv[s][j]);
-                    }
-                    const float run = m[0] = __builtin_amdgcn_exp2f(A2 * sum);
-                    scan_up(m, e);
-                    const float start =
-                        neighbour<kFromLower>(in, __builtin_fmaf(m[0], in, e[0]));
-                    float prev = start;
+                if (!has) {   // a lane without this state adds nothing
 #pragma unroll
                     for (int j = 0; j < T; ++j)
-                        prev = h[j] = __builtin_fmaf(av[j], prev, dx[j] * Bv[s][j]);
-                    // G below the lane's run, from 0 above it, then from the lanes above
-                    e[0] = 0.0f;
-#pragma unroll
-                    for (int j = T - 1; j >= 0; --j)
-                        e[0] = av[j] * __builtin_fmaf(Cv[s][j], g[j], e[0]);
-                    m[0] = run;
-                    scan_down(m, e);
-                    const float low = __builtin_fmaf(m[0], after, e[0]);
-                    float G = neighbour<kFromUpper>(after, low), dA = 0.0f;
-#pragma unroll
-                    for (int j = T - 1; j >= 0; --j) {
-                        const float gt = __builtin_fmaf(Cv[s][j], g[j], G);
-                        G = av[j] * gt;
-                        dC[s][j] = __builtin_fmaf(g[j], h[j], dC[s][j]);
-                        dB[s][j] = __builtin_fmaf(gt, dx[j], dB[s][j]);
-                        gB[j] = __builtin_fmaf(gt, Bv[s][j], gB[j]);
-                        yv[j] = __builtin_fmaf(Cv[s][j], h[j], yv[j]);
-                        const float t = G * (j ? h[j ? j - 1 : 0] : start);
-                        sA[j] = __builtin_fmaf(A2, t, sA[j]);
-                        dA = __builtin_fmaf(de[j], t, dA);
-                    }
-                    dA = row_sum(dA);
-                    if (here) {
-                        if (lane == 15)
-                            dAs[cs * a.N + n] += dA;
-                        if (lane == 0)
-                            carry[cs * a.N + n] = low;
-                    }
+                        Bv[j] = Cv[j] = 0.0f;
                 }
-                float4 *o = (float4 *)sums + (wave * 3 * (T / 4)) * 64 + (tid & 63);
 #pragma unroll
-                for (int j4 = 0; j4 < T / 4; ++j4) {
-                    const int j = 4 * j4;
-                    o[j4 * 64] = make_float4(gB[j], gB[j + 1], gB[j + 2], gB[j + 3]);
-                    o[(T / 4 + j4) * 64] = make_float4(sA[j], sA[j + 1], sA[j + 2], sA[j + 3]);
-                    o[(2 * (T / 4) + j4) * 64] =
-                        make_float4(yv[j], yv[j + 1], yv[j + 2], yv[j + 3]);
+                for (int j = 0; j < T; ++j) {
+                    av[j] = __builtin_amdgcn_exp2f(A2 * de[j]);
+                    e[0] = __builtin_fmaf(av[j], e[0], dx[j] * Bv[j]);
                 }
+                const float run = m[0] = __builtin_amdgcn_exp2f(A2 * sum);
+                scan_up(m, e);
+                const float start =
+                    neighbour<kFromLower>(in[s], __builtin_fmaf(m[0], in[s], e[0]));
+                float prev = start;
+#pragma unroll
+                for (int j = 0; j < T; ++j)
+                    prev = h[j] = __builtin_fmaf(av[j], prev, dx[j] * Bv[j]);
+                // G below the lane's run, from 0 above it, then from the lanes above
+                e[0] = 0.0f;
+#pragma unroll
+                for (int j = T - 1; j >= 0; --j)
+                    e[0] = av[j] * __builtin_fmaf(Cv[j], g[j], e[0]);
+                m[0] = run;
+                scan_down(m, e);
+                const float low = __builtin_fmaf(m[0], after, e[0]);
+                float G = neighbour<kFromUpper>(after, low), dA = 0.0f;
+#pragma unroll
+                for (int j = T - 1; j >= 0; --j) {
+                    const float gt = __builtin_fmaf(Cv[j], g[j], G);
+                    G = av[j] * gt;
+                    dC[s][j] = __builtin_fmaf(g[j], h[j], dC[s][j]);
+                    dB[s][j] = __builtin_fmaf(gt, dx[j], dB[s][j]);
+                    gB[j] = __builtin_fmaf(gt, Bv[j], gB[j]);
+                    yv[j] = __builtin_fmaf(Cv[j], h[j], yv[j]);
+                    const float t = G * (j ? h[j ? j - 1 : 0] : start);
+                    sA[j] = __builtin_fmaf(A2, t, sA[j]);
+                    dA = __builtin_fmaf(de[j], t, dA);
+                }
+                dA = row_sum(dA);
+                if (has) {
+                    if (lane == 15)
+                        dAs[c * a.N + n] += dA;
+                    if (lane == 0)
+                        carry[c * a.N + n] = low;
+                }
+                // one state's values at a time: sums put off to the end would keep every
+                // state's h and g in registers
+#pragma unroll
+                for (int j = 0; j < T; ++j)
+                    asm volatile("" : "+v"(dB[s][j]), "+v"(dC[s][j]), "+v"(gB[j]), "+v"(sA[j]),
+                                 "+v"(yv[j]));
             }
-            __syncthreads();
-            // the gradients of the positions that this thread prepared
-            float sD = 0.0f, sb = 0.0f;
-            if (live) {
-                const float skip = a.Dskip ? a.Dskip[d] : 0.0f;
-                float ox[I], ot[I], oz[I];
+            // the gradients of the positions that this lane prepared
+            float v0[I], v1[I], v2[I], ox[I], ot[I], oz[I], sD = 0.0f, sb = 0.0f;
+            sum_rows<T>(gB, v0);
+            sum_rows<T>(sA, v1);
+            sum_rows<T>(yv, v2);
 #pragma unroll
-                for (int i = 0; i < I; ++i) {
-                    const int t = pos + i, ln = (cq & 3) * 16 + t / T, j = t % T;
-                    const float *s0 = sums + (((cq >> 2) * W * 3 * (T / 4) + j / 4) * 64 + ln) * 4 +
-                                      j % 4;
-                    float v[3] = {0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int k = 0; k < W; ++k)
-#pragma unroll
-                        for (int kind = 0; kind < 3; ++kind)
-                            v[kind] += s0[((k * 3 + kind) * (T / 4)) * 256];
-                    const bool in = i < left;
-                    const float dd = x[i] * v[0] + v[1] * 0.693147180559945309f;
-                    ot[i] = in ? dd * slope[i] : 0.0f;
-                    ox[i] = in ? __builtin_fmaf(delta[i], v[0], skip * dy[i]) : 0.0f;
-                    sb += ot[i];
-                    sD = __builtin_fmaf(dy[i], x[i], sD);
-                    if (a.z.p) {
-                        const float y = __builtin_fmaf(skip, x[i], v[2]);
-                        oz[i] = in ? dout[i] * y * silu_grad(z[i], sigmoid(z[i])) : 0.0f;
-                    }
-                }
-                const int room = a.L - p0 - pos;
-                store_upto<E, I>(ga.dx.row<E>(b, d) + p0 + pos, room, ox);
-                store_upto<E, I>(ga.ddt.row<E>(b, d) + p0 + pos, room, ot);
-                if (a.z.p)
-                    store_upto<E, I>(ga.dz.row<E>(b, d) + p0 + pos, room, oz);
+            for (int i = 0; i < I; ++i) {
+                const bool inside = i < left;
+                const float dd = __builtin_fmaf(x[i], v0[i], v1[i] * 0.693147180559945309f);
+                ot[i] = keep_if(inside, dd * slope[i]);
+                ox[i] = keep_if(inside, __builtin_fmaf(delta[i], v0[i], skip * dy[i]));
+                const float y = __builtin_fmaf(skip, x[i], v2[i]);
+                oz[i] = keep_if(inside, dout[i] * y * silu_grad(z[i], sigmoid(z[i])));
+                sb += ot[i];
+                sD = __builtin_fmaf(dy[i], x[i], sD);
             }
-            sD = row_sum(sD);
-            sb = row_sum(sb);
-            if (live && lane == 15) {
-                // the channel's P / I threads are P / I / 16 rows
-                float *q = ps + ((cb + cq) * W + (pos / I) / 16) * 2;
-                q[0] += sD;
-                q[1] += sb;
+            const int room = a.L - p0 - pos;
+            store_upto<E, I>(ga.dx.row<E>(b, d) + p0 + pos, room, ox);
+            store_upto<E, I>(ga.ddt.row<E>(b, d) + p0 + pos, room, ot);
+            if (a.z.p)
+                store_upto<E, I>(ga.dz.row<E>(b, d) + p0 + pos, room, oz);
+            sD = wave_sum(sD);
+            sb = wave_sum(sb);
+            if ((tid & 63) == 0) {
+                ps[2 * c] += sD;
+                ps[2 * c + 1] += sb;
             }
         }
-        // dB and dC of the part: the rows, then the halves
+        // dB and dC of the part: the upper half of the waves to the lower, by halves
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+        for (int s0 = 0; s0 < S; s0 += SW) {
 #pragma unroll
-            for (int j = 0; j < T; ++j) {
-                dB[s][j] += __shfl_xor(dB[s][j], 16, 64);
-                dB[s][j] += __shfl_xor(dB[s][j], 32, 64);
-                dC[s][j] += __shfl_xor(dC[s][j], 16, 64);
-                dC[s][j] += __shfl_xor(dC[s][j], 32, 64);
-            }
-        // sums is free once every thread has finished its positions
-        __syncthreads();
-        if (H > 1) {
-            if (half > 0 && rowi == 0)
+            for (int half = kGradWaves / 2; half; half >>= 1) {
+                float *q = swp + (wave & (half - 1)) * 2 * SW * T * 64 + (tid & 63) * 4;
+                if (wave >= half && wave < 2 * half)
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    store_vec<float, T>(sums + ((wave * 8 + s) * 16 + lane) * T, dB[s]);
-                    store_vec<float, T>(sums + ((wave * 8 + 4 + s) * 16 + lane) * T, dC[s]);
-                }
-            __syncthreads();
-        }
-        if (half == 0 && rowi == 0) {
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                if (n0 + s >= a.N)
-                    break;
-#pragma unroll
-                for (int k = 1; k < H; ++k) {
-                    float u[T], v[T];
-                    load_vec<float, T>(sums + (((k * W + w) * 8 + s) * 16 + lane) * T, u);
-                    load_vec<float, T>(sums + (((k * W + w) * 8 + 4 + s) * 16 + lane) * T, v);
-#pragma unroll
-                    for (int j = 0; j < T; ++j) {
-                        dB[s][j] += u[j];
-                        dC[s][j] += v[j];
+                    for (int k = 0; k < SW * T / 4; ++k) {
+                        const int s = s0 + 4 * k / T, j = 4 * k % T;
+                        *(float4 *)(q + 2 * k * 256) =
+                            make_float4(dB[s][j], dB[s][j + 1], dB[s][j + 2], dB[s][j + 3]);
+                        *(float4 *)(q + (2 * k + 1) * 256) =
+                            make_float4(dC[s][j], dC[s][j + 1], dC[s][j + 2], dC[s][j + 3]);
                     }
-                }
-                const long long rows = (long long)a.G * a.N;
-                const long long r =
-                    ((long long)set * a.B + b) * rows + (long long)grp * a.N + n0 + s;
-                const int t0 = p0 + lane * T;
-                store_upto<float, T>(ga.shared + r * a.L + t0, a.L - t0, dB[s]);
-                store_upto<float, T>(ga.shared + ((long long)ga.sets * a.B * rows + r) * a.L + t0,
-                                     a.L - t0, dC[s]);
+                __syncthreads();
+                if (wave < half)
+#pragma unroll
+                    for (int k = 0; k < SW * T / 4; ++k) {
+                        const int s = s0 + 4 * k / T, j = 4 * k % T;
+                        const float4 u = *(const float4 *)(q + 2 * k * 256);
+                        const float4 v = *(const float4 *)(q + (2 * k + 1) * 256);
+                        dB[s][j] += u.x;
+                        dB[s][j + 1] += u.y;
+                        dB[s][j + 2] += u.z;
+                        dB[s][j + 3] += u.w;
+                        dC[s][j] += v.x;
+                        dC[s][j + 1] += v.y;
+                        dC[s][j + 2] += v.z;
+                        dC[s][j + 3] += v.w;
+                    }
+                __syncthreads();
             }
         }
-        __syncthreads();
+        if (wave == 0) {
+            const long long rows = (long long)a.G * a.N;
+            const int t0 = p0 + lane * T;
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (n0 + s < a.N) {
+                    const long long r =
+                        ((long long)set * a.B + b) * rows + (long long)grp * a.N + n0 + s;
+                    store_upto<float, T>(ga.shared + r * a.L + t0, a.L - t0, dB[s]);
+                    store_upto<float, T>(ga.shared + ((long long)ga.sets * a.B * rows + r) * a.L +
+                                             t0,
+                                         a.L - t0, dC[s]);
+                }
+        }
     }
     __syncthreads();
     // padding
@@ -573,13 +718,8 @@ __global__ __launch_bounds__(64 * W * H) void scan_backward_kernel(GradArgs ga) 
             ga.dstate[((long long)b * a.D + first) * a.N + i] = carry[i];
     }
     for (int c = tid; c < count; c += TH) {
-        float sD = 0.0f, sb = 0.0f;
-        for (int k = 0; k < W; ++k) {
-            sD += ps[(c * W + k) * 2];
-            sb += ps[(c * W + k) * 2 + 1];
-        }
-        out[(long long)a.D * a.N + first + c] = sD;
-        out[(long long)a.D * (a.N + 1) + first + c] = sb;
+        out[(long long)a.D * a.N + first + c] = ps[2 * c];
+        out[(long long)a.D * (a.N + 1) + first + c] = ps[2 * c + 1];
     }
 }
 
@@ -715,19 +855,20 @@ inline bool scan_shape(int type, int B, int D, int L, int N, int G) {
 }
 
 // Positions a lane: the gradients' parts and the states' layout depend on it.
-// More than 32 states need 16 waves in the gradients, whose registers hold four.
-inline int lane_positions(int L, int N) { return L <= 64 || N > 32 ? 4 : 8; }
+// More than 16 states leave the gradients' registers room for four.
+inline int lane_positions(int L, int N) { return L <= 64 || N > 16 ? 4 : 8; }
 inline long long part_count(int L, int N) {
     return cdivll(L > 0 ? L : 1, 16 * lane_positions(L, N));
 }
 
 inline size_t forward_lds(int N, int T, int W) {
-    return ((size_t)2 * N * 16 * T + 2 * (16 / W) * N + (W > 1 ? 4 * 64 * T : 0)) * 4;
+    return ((size_t)2 * N * 16 * T + 2 * (16 / W) * N + (W > 1 ? (2 * 4 * 16 + 4 * 64) * T : 0)) * 4;
 }
 
 template <typename E, int T, int W>
 int launch_forward(ScanArgs &c, hipStream_t s) {
     c.blocks = (int)cdivll(c.Dg, 16 / W);
+    c.every = lane_positions(c.L, c.N) * 16 / T;
     const long long grid = (long long)c.blocks * c.G * c.B;
     const size_t lds = forward_lds(c.N, T, W);
     if (grid >= (1ll << 31) || lds > (size_t)kLds)
@@ -765,54 +906,47 @@ bool scan_common(const finc_scan_args *a, ScanArgs &c) {
     return true;
 }
 
-// The gradients' waves: W share the states (four each), H fours of channels.
-inline int state_waves(int N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
-inline int channel_fours(int W) { return W >= 8 ? 1 : 8 / W; }
-
 // Channels of a set: a workgroup a compute unit where there are that many channels,
 // and at most 64, which the state in LDS holds.
-inline int set_channels(int B, int D, int N, int G) {
-    const int step = 4 * channel_fours(state_waves(N));
-    long long c = cdivll(cdivll((long long)B * D, 256), step) * step;
-    const long long most = cdivll(D / G, step) * step;
+inline int set_channels(int B, int D, int G) {
+    long long c = cdivll(cdivll((long long)B * D, 256), kGradWaves) * kGradWaves;
+    const long long most = cdivll(D / G, kGradWaves) * kGradWaves;
     c = c < most ? c : most;
-    return (int)(c < step ? step : c > 64 ? 64 : c);
+    return (int)(c > 64 ? 64 : c);
 }
 
-template <typename E, int T, int W, int H>
+template <typename E, int T, int S>
 int launch_backward(GradArgs &c, hipStream_t s) {
     const long long grid = (long long)c.sets * c.f.G * c.f.B;
-    const size_t lds = backward_lds(c.f.N, T, W, H, c.set);
+    const size_t lds = backward_lds(c.f.N, T, c.set);
     if (grid >= (1ll << 31) || lds > (size_t)kLds)
         return FINC_EUNSUPPORTED;
-    if (lds > 64 * 1024)
-        (void)hipFuncSetAttribute((const void *)scan_backward_kernel<E, T, W, H>,
-                                  hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    (void)hipFuncSetAttribute((const void *)scan_backward_kernel<E, T, S>,
+                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     (void)hipGetLastError();   // the launch check decides
-    hipLaunchKernelGGL((scan_backward_kernel<E, T, W, H>), dim3((unsigned)grid),
-                       dim3(64 * W * H), (unsigned)lds, s, c);
+    hipLaunchKernelGGL((scan_backward_kernel<E, T, S>), dim3((unsigned)grid),
+                       dim3(64 * kGradWaves), (unsigned)lds, s, c);
     return launched();
 }
 
+// S states a lane, a quarter of them all.
 template <typename E>
 int dispatch_backward(GradArgs &c, hipStream_t s) {
-    const int W = state_waves(c.f.N);
-    if (W == 16)
-        return launch_backward<E, 4, 16, 1>(c, s);
-    if (lane_positions(c.f.L, c.f.N) == 4)
-        return W == 1   ? launch_backward<E, 4, 1, 8>(c, s)
-               : W == 2 ? launch_backward<E, 4, 2, 4>(c, s)
-               : W == 4 ? launch_backward<E, 4, 4, 2>(c, s)
-                        : launch_backward<E, 4, 8, 1>(c, s);
-    return W == 1   ? launch_backward<E, 8, 1, 8>(c, s)
-           : W == 2 ? launch_backward<E, 8, 2, 4>(c, s)
-           : W == 4 ? launch_backward<E, 8, 4, 2>(c, s)
-                    : launch_backward<E, 8, 8, 1>(c, s);
+    const int N = c.f.N;
+    if (lane_positions(c.f.L, N) == 4)
+        return N <= 4    ? launch_backward<E, 4, 1>(c, s)
+               : N <= 8  ? launch_backward<E, 4, 2>(c, s)
+               : N <= 16 ? launch_backward<E, 4, 4>(c, s)
+               : N <= 32 ? launch_backward<E, 4, 8>(c, s)
+                         : launch_backward<E, 4, 16>(c, s);
+    return N <= 4   ? launch_backward<E, 8, 1>(c, s)
+           : N <= 8 ? launch_backward<E, 8, 2>(c, s)
+                    : launch_backward<E, 8, 4>(c, s);
 }
 
 inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 inline size_t shared_bytes(int B, int D, int L, int N, int G) {
-    return up256((size_t)2 * cdivll(D / G, set_channels(B, D, N, G)) * B * G * N * L * 4);
+    return up256((size_t)2 * cdivll(D / G, set_channels(B, D, G)) * B * G * N * L * 4);
 }
 
 }  // namespace
@@ -860,12 +994,17 @@ int finc_selective_scan_forward(const finc_scan_args *a, hipStream_t stream) {
     int rc = FINC_EINVAL;
     // 2048 waves are two a SIMD
     const bool few = (long long)B * D < 4 * 2048;
+    const int T = L <= 64 ? 4 : L <= 128 || a->N > 32 ? 8 : 16;
     with_type(a->type, [&](auto e) {
         typedef decltype(e) E;
-        if (lane_positions(L, a->N) == 4)
-            rc = few ? launch_forward<E, 4, 4>(c, stream) : launch_forward<E, 4, 1>(c, stream);
+        if (few)
+            rc = T == 4   ? launch_forward<E, 4, 4>(c, stream)
+                 : T == 8 ? launch_forward<E, 8, 4>(c, stream)
+                          : launch_forward<E, 16, 4>(c, stream);
         else
-            rc = few ? launch_forward<E, 8, 4>(c, stream) : launch_forward<E, 8, 1>(c, stream);
+            rc = T == 4   ? launch_forward<E, 4, 1>(c, stream)
+                 : T == 8 ? launch_forward<E, 8, 1>(c, stream)
+                          : launch_forward<E, 16, 1>(c, stream);
     });
     return rc;
 }
@@ -918,7 +1057,7 @@ int finc_selective_scan_backward(const finc_scan_args *a, const finc_scan_grads 
     c.dstate = g->dstate;
     c.shared = (float *)g->workspace;
     c.params = (float *)((char *)g->workspace + shared_bytes(B, D, L, N, G));
-    c.set = set_channels(B, D, N, G);
+    c.set = set_channels(B, D, G);
     c.sets = (int)cdivll(c.f.Dg, c.set);
     int rc = FINC_OK;
     const long long sums = 2ll * B * GN * cdivll(L, 1024);

@@ -48,7 +48,9 @@ __device__ inline void load_vec(const E *p, float *v) {
     }
 }
 
-// The first `count` (any int) of N elements; the others are 0.
+// The first `count` (any int) of N elements; the others are 0.  A part of a vector
+// takes its elements one by one, the last one again in place of those past it: no
+// branch an element.
 template <typename E, int N>
 __device__ inline void load_upto(const E *p, int count, float *v) {
     if (count >= N) {
@@ -57,7 +59,15 @@ __device__ inline void load_upto(const E *p, int count, float *v) {
     }
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        v[i] = i < count ? (float)p[i] : 0.0f;
+        v[i] = 0.0f;
+    if (count > 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = (float)p[min(i, count - 1)];
+#pragma unroll
+        for (int i = 1; i < N; ++i)
+            v[i] = i < count ? v[i] : 0.0f;
+    }
 }
 
 template <typename E, int N>
@@ -95,13 +105,22 @@ __device__ inline float sigmoid(float v) {
     // 1 / (1 + inf) = 0 on the left, 1 / (1 + 0) = 1 on the right
     return __builtin_amdgcn_rcpf(1.0f + exp_fast(-v));
 }
+// v, at most 1e30 from 0 (NaN stays): an infinite v times a sigmoid of 0 has no value.
+__device__ inline float finite(float v) {
+    v = v < -1e30f ? -1e30f : v;
+    return v > 1e30f ? 1e30f : v;
+}
 __device__ inline float silu(float v) {
-    // -inf would give -inf * 0
-    return v == -__builtin_inff() ? 0.0f : v * sigmoid(v);
+    const float sg = sigmoid(v);
+    return (v < -1e30f ? -1e30f : v) * sg;
 }
 // d silu / dv, with sg = sigmoid(v).
 __device__ inline float silu_grad(float v, float sg) {
-    return __builtin_isinf(v) ? sg : sg * (1.0f + v * (1.0f - sg));
+    return sg * __builtin_fmaf(finite(v), 1.0f - sg, 1.0f);
+}
+// v, or 0: a mask of bits, so that what v takes to compute gets no branch.
+__device__ inline float keep_if(bool ok, float v) {
+    return __builtin_bit_cast(float, __builtin_bit_cast(int, v) & -(int)ok);
 }
 // log(1 + e^v) = max(v, 0) + log1p(e^-|v|).  The logarithm is the series of
 // 2 atanh(s), s = e / (2 + e) <= 1/3: nine terms leave s^18 / 19 < 2e-10 of it, and
@@ -118,8 +137,8 @@ __device__ inline float softplus(float v) {
     p = __builtin_fmaf(p, q, 1.0f / 5.0f);
     p = __builtin_fmaf(p, q, 1.0f / 3.0f);
     p = __builtin_fmaf(p, q, 1.0f);
-    // a NaN takes the sum: the maximum alone would drop it
-    return v != v ? v : __builtin_fmaxf(v, 0.0f) + 2.0f * s * p;
+    // NaN comes through e: the maximum alone would drop it
+    return __builtin_fmaf(2.0f * s, p, __builtin_fmaxf(v, 0.0f));
 }
 
 // ---- reductions over lanes -------------------------------------------------------
