@@ -39,6 +39,7 @@ struct ScanArgs {
     int B, D, L, N, G, Dg;   // Dg: channels of a group
     int softplus, parts;     // parts: that states are kept for, of the whole raster
     int every;               // a forward's lanes between two of them
+    int NP;                  // states that are kept: N with those that fill four rows
     int blocks;              // of channels, in a group
 };
 
@@ -68,11 +69,15 @@ __device__ inline void scan_up(float (&a)[2], float (&h)[2]) {
                      "row_shr:4") FINC_STEP2("row_shr:8") "s_nop 1"
                  : "+v"(a[0]), "+v"(h[0]), "+v"(a[1]), "+v"(h[1]));
 }
-// The same towards the row's first lane.
-__device__ inline void scan_down(float (&a)[1], float (&h)[1]) {
-    asm volatile("s_nop 1\n" FINC_STEP1("row_shl:1") FINC_STEP1("row_shl:2") FINC_STEP1(
-                     "row_shl:4") FINC_STEP1("row_shl:8") "s_nop 1"
-                 : "+v"(a[0]), "+v"(h[0]));
+// Both directions at once: (a, h) over the lanes before, (c, g) over the lanes after.
+#define FINC_BOTH(n)                                                                        \
+    "v_fmac_f32_dpp %1, %1, %0 row_shr:" n " row_mask:0xf bank_mask:0xf\n"                 \
+    "v_fmac_f32_dpp %3, %3, %2 row_shl:" n " row_mask:0xf bank_mask:0xf\n"                 \
+    "v_mul_f32_dpp %0, %0, %0 row_shr:" n " row_mask:0xf bank_mask:0xf\n"                  \
+    "v_mul_f32_dpp %2, %2, %2 row_shl:" n " row_mask:0xf bank_mask:0xf\n"
+__device__ inline void scan_both(float &a, float &h, float &c, float &g) {
+    asm volatile("s_nop 1\n" FINC_BOTH("1") FINC_BOTH("2") FINC_BOTH("4") FINC_BOTH("8") "s_nop 1"
+                 : "+v"(a), "+v"(h), "+v"(c), "+v"(g));
 }
 
 // The neighbour's value; `edge` where the row has none.
@@ -147,13 +152,56 @@ __device__ inline int slot_at(int t) {
     return ((t % T / 4) * 16 + t / T) * 4 + t % 4;
 }
 
-// Elements as they lie in memory, for loads that are under way while others are used;
-// 0 past `count`.
+// S floats of LDS, aligned to their size (to 16 bytes above four).
+template <int S>
+__device__ inline void lds_load(const float *p, float *v) {
+    constexpr int C = S < 4 ? S : 4;
+    typedef float Q __attribute__((ext_vector_type(C)));
+#pragma unroll
+    for (int i = 0; i < S; i += C) {
+        const Q q = *(const Q *)(p + i);
+#pragma unroll
+        for (int k = 0; k < C; ++k)
+            v[i + k] = q[k];
+    }
+}
+template <int S>
+__device__ inline void lds_store(float *p, const float *v) {
+    constexpr int C = S < 4 ? S : 4;
+    typedef float Q __attribute__((ext_vector_type(C)));
+#pragma unroll
+    for (int i = 0; i < S; i += C) {
+        Q q;
+#pragma unroll
+        for (int k = 0; k < C; ++k)
+            q[k] = v[i + k];
+        *(Q *)(p + i) = q;
+    }
+}
+
+// Element i of a row whose address the whole wave shares: a scalar base and a 32-bit
+// offset of bytes, which is formed where it is used (the sums of all rows' addresses,
+// kept over a loop, would take the registers).
+template <typename E>
+__device__ inline E *at(E *row, unsigned i) {
+    unsigned o = i * (unsigned)sizeof(E);
+    asm volatile("" : "+v"(o));
+    return (E *)((char *)row + o);
+}
+template <typename E>
+__device__ inline const E *at(const E *row, unsigned i) {
+    return at((E *)row, i);
+}
+
+// Elements as they lie in memory, for loads that are under way while others are used.
 template <typename E, int N>
-__device__ inline typename Vec<E, N>::type load_raw(const E *p, int count) {
+__device__ inline typename Vec<E, N>::type load_whole(const E *p) {
+    return *(const typename Vec<E, N>::type *)p;
+}
+// The same, 0 past `count`.
+template <typename E, int N>
+__device__ inline typename Vec<E, N>::type load_part(const E *p, int count) {
     typename Vec<E, N>::type v;
-    if (count >= N)
-        return *(const typename Vec<E, N>::type *)p;
 #pragma unroll
     for (int i = 0; i < N; ++i)
         v[i] = (E)0.0f;
@@ -167,6 +215,12 @@ __device__ inline typename Vec<E, N>::type load_raw(const E *p, int count) {
     }
     return v;
 }
+// `whole`, that every lane has all of them, is the same in the whole wave: a branch of
+// some lanes would wait for the loads of the others, whose registers it fills.
+template <typename E, int N>
+__device__ inline typename Vec<E, N>::type load_raw(const E *p, int count, bool whole) {
+    return whole ? load_whole<E, N>(p) : load_part<E, N>(p, count);
+}
 
 constexpr int kUnit = 8;   // elements of B and C that a thread moves at once
 
@@ -178,44 +232,51 @@ __device__ inline typename Vec<E, kUnit>::type load_tile(const ScanArgs &a, int 
     const int r = u / Q, q = (u % Q) * kUnit;
     const E *row = (r >= a.N ? a.Cm : a.Bm)
                        .row<const E>(b, (long long)grp * a.N + (r >= a.N ? r - a.N : r));
-    return load_raw<E, kUnit>(row + p0 + q, n_pos - p0 - q);
+    return load_raw<E, kUnit>(row + p0 + q, n_pos - p0 - q, p0 + 16 * T <= n_pos);
 }
 template <typename E, int T>
-__device__ inline void store_tile(float *tb, int u, typename Vec<E, kUnit>::type v) {
+__device__ inline void store_tile(float *tb, float *tc, int N, int u,
+                                  typename Vec<E, kUnit>::type v) {
     constexpr int Q = 16 * T / kUnit;
-    const int r = u / Q, q = (u % Q) * kUnit;   // C's rows follow B's
+    const int r = u / Q, q = (u % Q) * kUnit;
+    float *to = r >= N ? tc + (r - N) * 16 * T : tb + r * 16 * T;
 #pragma unroll
     for (int k = 0; k < kUnit; k += 4)
-        *(float4 *)(tb + r * 16 * T + slot_at<T>(q + k)) =
+        *(float4 *)(to + slot_at<T>(q + k)) =
             make_float4((float)v[k], (float)v[k + 1], (float)v[k + 2], (float)v[k + 3]);
 }
 
-// One block: CB = 16 / W channels of one batch row and group.  W waves share a
-// channel's states (each N / W of them) where there are few channels; then a wave
-// prepares one channel's positions for all of them and sums that channel's outputs.
-// The next part's loads are under way while a part is computed.
-template <typename E, int T, int W>
-__global__ __launch_bounds__(kThreads, 2) void scan_forward_kernel(ScanArgs a) {
-    constexpr int CB = 16 / W, P = 16 * T;   // P: positions of a part
-    constexpr int I = T / W;                 // positions that a thread prepares
+// What each forward kernel does with the states: read before the raster, kept for the
+// gradients every a.every lanes' runs, written after the row.
+__device__ inline float *kept_states(const ScanArgs &a, int b, int d, int part, int lane, int t0,
+                                     int n_pos) {
+    // a part that the row does not reach is not read either
+    if (!a.states || lane % a.every || t0 >= n_pos)
+        return nullptr;
+    return a.states + (((long long)b * a.D + d) * a.parts +
+                       (long long)part * (16 / a.every) + lane / a.every) * a.NP;
+}
+
+// Many channels: one block of 16 channels of one batch row and group, a row of lanes
+// for all the states of each.  The four rows of a wave read the same B and C.  The
+// next part's loads are under way while a part is computed.
+template <typename E, int T>
+__global__ __launch_bounds__(kThreads, 2) void scan_channels_kernel(ScanArgs a) {
+    constexpr int CB = 16, P = 16 * T;       // P: positions of a part
     constexpr int K = 4;                     // units of B and C loaded ahead
     extern __shared__ __attribute__((aligned(16))) float lds[];
     float *tb = lds, *tc = tb + a.N * P;
     float *hs = tc + a.N * P;                // the states between parts, CB x N
     float *As = hs + CB * a.N;               // A log2 e, CB x N
-    float *pre = As + CB * a.N;              // W > 1: delta, delta x of CB channels
-    float *red = pre + 2 * CB * P;           // W > 1: the waves' sums of y
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 15, rowi = (tid >> 4) & 3;
+    const int tid = threadIdx.x, lane = tid & 15, cl = tid >> 4;
     int blk = blockIdx.x;
     const int cb = blk % a.blocks;
     blk /= a.blocks;
     const int grp = blk % a.G, b = blk / a.G;
-    const int split = wave % W;
-    const int cl = W > 1 ? rowi : wave * 4 + rowi;   // the channel whose states it scans
-    const int cp = tid * I / P, pos = tid * I % P;   // the one whose positions it prepares
-    const bool live = cb * CB + cp < a.Dg;
-    const int d = grp * a.Dg + (live ? cb * CB + cp : 0);
-    const int n_pos = row_length(a.lengths, b, a.L);
+    const bool live = cb * CB + cl < a.Dg;
+    const bool all = (cb + 1) * CB <= a.Dg;  // the block's channels are all there
+    const int d = grp * a.Dg + (live ? cb * CB + cl : 0);
+    const int n_pos = __builtin_amdgcn_readfirstlane(row_length(a.lengths, b, a.L));
     const int units = 2 * a.N * (P / kUnit);
     for (int i = tid; i < CB * a.N; i += kThreads) {
         const int c = i / a.N, n = i - c * a.N, dd = cb * CB + c;
@@ -226,16 +287,16 @@ __global__ __launch_bounds__(kThreads, 2) void scan_forward_kernel(ScanArgs a) {
     }
     const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
     const float skip = a.Dskip ? a.Dskip[d] : 0.0f;
-    const E *xr = a.x.row<const E>(b, d) + pos, *dr = a.dt.row<const E>(b, d) + pos;
-    const E *zr = a.z.p ? a.z.row<const E>(b, d) + pos : nullptr;
-    E *yr = a.y.row<E>(b, d) + pos;
-    const int own = live ? n_pos - pos : 0;
+    const E *xr = a.x.row<const E>(b, d) + lane * T, *dr = a.dt.row<const E>(b, d) + lane * T;
+    const E *zr = a.z.p ? a.z.row<const E>(b, d) + lane * T : nullptr;
+    E *yr = a.y.row<E>(b, d) + lane * T;
+    const int own = live ? n_pos - lane * T : 0;
     const int parts = (n_pos + P - 1) / P;
-    typename Vec<E, I>::type nx, nd, nz;
+    typename Vec<E, T>::type nx, nd, nz;
     typename Vec<E, kUnit>::type nt[K];
     if (parts > 0) {
-        nx = load_raw<E, I>(xr, own);
-        nd = load_raw<E, I>(dr, own);
+        nx = load_raw<E, T>(xr, own, all && P <= n_pos);
+        nd = load_raw<E, T>(dr, own, all && P <= n_pos);
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (tid + k * kThreads < units)
@@ -247,87 +308,53 @@ __global__ __launch_bounds__(kThreads, 2) void scan_forward_kernel(ScanArgs a) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (tid + k * kThreads < units)
-                store_tile<E, T>(tb, tid + k * kThreads, nt[k]);
+                store_tile<E, T>(tb, tc, a.N, tid + k * kThreads, nt[k]);
         for (int u = tid + K * kThreads; u < units; u += kThreads)
-            store_tile<E, T>(tb, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
-        float x[I], delta[T], dx[T], y[T];
+            store_tile<E, T>(tb, tc, a.N, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
+        float x[T], delta[T], dx[T], y[T], sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
-            x[i] = (float)nx[i];
-            float v = (float)nd[i] + bias;
+        for (int j = 0; j < T; ++j) {
+            x[j] = (float)nx[j];
+            float v = (float)nd[j] + bias;
             if (a.softplus)
                 v = softplus(v);
-            delta[i] = keep_if(i < own - p0, v);
-            dx[i] = delta[i] * x[i];
-        }
-        if (W > 1) {
-            float *q = pre + cp * P + slot_at<T>(pos);
-#pragma unroll
-            for (int i = 0; i < I; ++i) {
-                q[i] = delta[i];
-                q[CB * P + i] = dx[i];
-            }
+            delta[j] = keep_if(j < own - p0, v);
+            dx[j] = delta[j] * x[j];
+            sum += delta[j];
+            y[j] = 0.0f;
         }
         __syncthreads();
         // under way until the part is done
         if (zr)
-            nz = load_raw<E, I>(zr + p0, own - p0);
+            nz = load_raw<E, T>(zr + p0, own - p0, all && p0 + P <= n_pos);
         if (part + 1 < parts) {
-            nx = load_raw<E, I>(xr + p0 + P, own - p0 - P);
-            nd = load_raw<E, I>(dr + p0 + P, own - p0 - P);
+            const bool whole = all && p0 + 2 * P <= n_pos;
+            nx = load_raw<E, T>(xr + p0 + P, own - p0 - P, whole);
+            nd = load_raw<E, T>(dr + p0 + P, own - p0 - P, whole);
 #pragma unroll
             for (int k = 0; k < K; ++k)
                 if (tid + k * kThreads < units)
                     nt[k] = load_tile<E, T>(a, b, grp, tid + k * kThreads, p0 + P, n_pos);
         }
-        float sum = 0.0f;
-#pragma unroll
-        for (int j4 = 0; j4 < T / 4; ++j4) {
-            if (W > 1) {
-                const float *q = pre + cl * P + (j4 * 16 + lane) * 4;
-                const float4 u = *(const float4 *)q, v = *(const float4 *)(q + CB * P);
-                delta[4 * j4] = u.x;
-                delta[4 * j4 + 1] = u.y;
-                delta[4 * j4 + 2] = u.z;
-                delta[4 * j4 + 3] = u.w;
-                dx[4 * j4] = v.x;
-                dx[4 * j4 + 1] = v.y;
-                dx[4 * j4 + 2] = v.z;
-                dx[4 * j4 + 3] = v.w;
-            }
-#pragma unroll
-            for (int j = 4 * j4; j < 4 * j4 + 4; ++j) {
-                sum += delta[j];
-                y[j] = 0.0f;
-            }
-        }
-        const int cs = cb * CB + cl;
-        // states are kept every a.every lanes' runs, for the gradients
-        float *kept = a.states && cs < a.Dg && lane % a.every == 0
-                          ? a.states + ((((long long)b * a.D + grp * a.Dg + cs) * a.parts +
-                                         (long long)part * (16 / a.every) + lane / a.every) *
-                                        a.N)
-                          : nullptr;
-        if (kept && p0 + lane * T >= n_pos)
-            kept = nullptr;   // its part is not in the row
+        float *kept = live ? kept_states(a, b, d, part, lane, p0 + lane * T, n_pos) : nullptr;
         float *hr = hs + cl * a.N;
         const float *Ar = As + cl * a.N;
-        int i = split;
-        for (; i + W < a.N; i += 2 * W) {
-            const int n[2] = {i, i + W};
-            const float A2[2] = {Ar[n[0]], Ar[n[1]]}, in[2] = {hr[n[0]], hr[n[1]]};
+        int i = 0;
+        for (; i + 1 < a.N; i += 2) {
+            const int n[2] = {i, i + 1};
+            const float A2[2] = {Ar[i], Ar[i + 1]}, in[2] = {hr[i], hr[i + 1]};
             float start[2], end[2];
             scan_states<T, 2>(tb, tc, n, A2, in, lane, delta, dx, sum, y, start, end);
             if (kept) {
-                kept[n[0]] = start[0];
-                kept[n[1]] = start[1];
+                kept[i] = start[0];
+                kept[i + 1] = start[1];
             }
             if (lane == 15) {
-                hr[n[0]] = end[0];
-                hr[n[1]] = end[1];
+                hr[i] = end[0];
+                hr[i + 1] = end[1];
             }
         }
-        for (; i < a.N; i += W) {
+        if (i < a.N) {
             const int n[1] = {i};
             const float A2[1] = {Ar[i]}, in[1] = {hr[i]};
             float start[1], end[1];
@@ -337,34 +364,18 @@ __global__ __launch_bounds__(kThreads, 2) void scan_forward_kernel(ScanArgs a) {
             if (lane == 15)
                 hr[i] = end[0];
         }
-        if (W > 1) {
-            float4 *r = (float4 *)red + (wave * (T / 4)) * 64 + (tid & 63);
-#pragma unroll
-            for (int j4 = 0; j4 < T / 4; ++j4)
-                r[j4 * 64] = make_float4(y[4 * j4], y[4 * j4 + 1], y[4 * j4 + 2], y[4 * j4 + 3]);
-            __syncthreads();
-            const float *q = red + cp * 64 + slot_at<T>(pos) % 64 + slot_at<T>(pos) / 64 * 256;
-#pragma unroll
-            for (int i = 0; i < I; ++i) {
-                y[i] = q[i];
-#pragma unroll
-                for (int w = 1; w < W; ++w)
-                    y[i] += q[w * (T / 4) * 256 + i];
-            }
-        }
         if (live) {
 #pragma unroll
-            for (int i = 0; i < I; ++i) {
-                float v = __builtin_fmaf(skip, x[i], y[i]);
+            for (int j = 0; j < T; ++j) {
+                float v = __builtin_fmaf(skip, x[j], y[j]);
                 if (zr)
-                    v *= silu((float)nz[i]);
-                y[i] = keep_if(i < own - p0, v);
+                    v *= silu((float)nz[j]);
+                y[j] = keep_if(j < own - p0, v);
             }
-            store_upto<E, I>(yr + p0, a.L - p0 - pos, y);
+            store_upto<E, T>(yr + p0, a.L - p0 - lane * T, y);
         }
-        // the next part's tile, and its positions, take the place of this one's
-        if (W == 1)
-            __syncthreads();
+        // the next part's tile takes the place of this one's
+        __syncthreads();
     }
     // padding
     for (int c = 0; c < CB; ++c) {
@@ -373,6 +384,195 @@ __global__ __launch_bounds__(kThreads, 2) void scan_forward_kernel(ScanArgs a) {
             break;
         E *r = a.y.row<E>(b, grp * a.Dg + dd);
         for (long long t = (long long)parts * P + tid; t < a.L; t += kThreads)
+            r[t] = (E)0.0f;
+    }
+    __syncthreads();
+    if (a.state_out)
+        for (int i = tid; i < CB * a.N; i += kThreads) {
+            const int c = i / a.N, n = i - c * a.N, dd = cb * CB + c;
+            if (dd < a.Dg)
+                a.state_out[((long long)b * a.D + grp * a.Dg + dd) * a.N + n] = hs[i];
+        }
+}
+
+// The sums over the four rows of T values a lane: row r gets those of positions
+// r T / 4 and on.
+__device__ inline float swap32(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a),
+                                                    __builtin_bit_cast(unsigned, b), false, false);
+    return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+__device__ inline float swap16(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a),
+                                                    __builtin_bit_cast(unsigned, b), false, false);
+    return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+template <int T>
+__device__ inline void sum_rows(const float (&v)[T], float (&out)[T / 4]) {
+    float u[T / 2];
+#pragma unroll
+    for (int j = 0; j < T / 2; ++j)
+        u[j] = swap32(v[j], v[j + T / 2]);
+#pragma unroll
+    for (int j = 0; j < T / 4; ++j)
+        out[j] = swap16(u[j], u[j + T / 4]);
+}
+
+// Few channels: a wave for a channel, whose four rows of lanes share the states (state
+// n in row n % 4) over the same positions.  Each row prepares a quarter of them and
+// hands them to the others through LDS; the sums over the states are sums over the
+// rows, and come back to the row that prepared the position.  The block's four waves
+// share the tile of B and C.
+template <typename E, int T>
+__global__ __launch_bounds__(kThreads, 2) void scan_rows_kernel(ScanArgs a) {
+    constexpr int CB = 4, P = 16 * T, I = T / 4;
+    constexpr int K = 4;                     // units of B and C loaded ahead
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    float *tb = lds, *tc = tb + a.N * P;
+    float *hs = tc + a.N * P;                // the states between parts, CB x N
+    float *As = hs + CB * a.N;               // A log2 e, CB x N
+    float *pre = As + CB * a.N;              // delta, delta x of every wave's channel
+    const int tid = threadIdx.x, lane = tid & 15, rowi = (tid >> 4) & 3;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int blk = blockIdx.x;
+    const int cb = blk % a.blocks;
+    blk /= a.blocks;
+    const int grp = blk % a.G, b = blk / a.G;
+    const bool live = cb * CB + wave < a.Dg;
+    const int d = grp * a.Dg + (live ? cb * CB + wave : 0);
+    const int n_pos = __builtin_amdgcn_readfirstlane(row_length(a.lengths, b, a.L));
+    const int units = 2 * a.N * (P / kUnit);
+    for (int i = tid; i < CB * a.N; i += kThreads) {
+        const int c = i / a.N, n = i - c * a.N, dd = cb * CB + c;
+        const bool ok = dd < a.Dg;
+        const long long at = (long long)(grp * a.Dg + (ok ? dd : 0)) * a.N + n;
+        As[i] = ok ? a.A[at] * kLog2e : 0.0f;
+        hs[i] = ok && a.state ? a.state[(long long)b * a.D * a.N + at] : 0.0f;
+    }
+    const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
+    const float skip = a.Dskip ? a.Dskip[d] : 0.0f;
+    const int pos = lane * T + rowi * I;     // the first that this lane prepares
+    float *mine = pre + wave * 2 * P;
+    const int parts = (n_pos + P - 1) / P;
+    typename Vec<E, I>::type nx, nd, nz;
+    typename Vec<E, kUnit>::type nt[K];
+    auto fetch = [&](int p0) {
+        const E *xr = a.x.row<const E>(b, d) + p0, *dr = a.dt.row<const E>(b, d) + p0;
+        const E *zr = a.z.p ? a.z.row<const E>(b, d) + p0 : xr;
+        if (p0 + P <= n_pos) {
+            nx = load_whole<E, I>(at(xr, pos));
+            nd = load_whole<E, I>(at(dr, pos));
+            nz = load_whole<E, I>(at(zr, pos));
+        } else {
+            const int left = n_pos - p0 - pos;
+            nx = load_part<E, I>(at(xr, pos), left);
+            nd = load_part<E, I>(at(dr, pos), left);
+            nz = load_part<E, I>(at(zr, pos), left);
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (tid + k * kThreads < units)
+                nt[k] = load_tile<E, T>(a, b, grp, tid + k * kThreads, p0, n_pos);
+    };
+    if (parts > 0)
+        fetch(0);
+    for (int part = 0; part < parts; ++part) {
+        const int p0 = part * P, left = n_pos - p0 - pos;
+        // positions past the row's length: delta 0 keeps the state, B and C are 0
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (tid + k * kThreads < units)
+                store_tile<E, T>(tb, tc, a.N, tid + k * kThreads, nt[k]);
+        for (int u = tid + K * kThreads; u < units; u += kThreads)
+            store_tile<E, T>(tb, tc, a.N, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
+        float x[I], z[I], delta[T], dx[T], y[T], sum = 0.0f;
+        float *q = mine + slot_at<T>(pos);   // I neighbours of one slot
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            x[i] = (float)nx[i];
+            z[i] = (float)nz[i];
+            float v = (float)nd[i] + bias;
+            if (a.softplus)
+                v = softplus(v);
+            v = keep_if(i < left, v);
+            q[i] = v;
+            q[P + i] = v * x[i];
+        }
+        __syncthreads();
+        // under way until the part is done
+        if (part + 1 < parts)
+            fetch(p0 + P);
+#pragma unroll
+        for (int j = 0; j < T; j += 4) {
+            lds_load<4>(mine + (j * 4 + lane) * 4, delta + j);
+            lds_load<4>(mine + P + (j * 4 + lane) * 4, dx + j);
+        }
+#pragma unroll
+        for (int j = 0; j < T; ++j) {
+            sum += delta[j];
+            y[j] = 0.0f;
+        }
+        float *kept = live ? kept_states(a, b, d, part, lane, p0 + lane * T, n_pos) : nullptr;
+        float *hr = hs + wave * a.N;
+        const float *Ar = As + wave * a.N;
+        int i = rowi;
+        for (int k = a.N / 8; k; --k, i += 8) {
+            const int n[2] = {i, i + 4};
+            const float A2[2] = {Ar[i], Ar[i + 4]}, in[2] = {hr[i], hr[i + 4]};
+            float start[2], end[2];
+            scan_states<T, 2>(tb, tc, n, A2, in, lane, delta, dx, sum, y, start, end);
+            if (kept) {
+                kept[i] = start[0];
+                kept[i + 4] = start[1];
+            }
+            if (lane == 15) {
+                hr[i] = end[0];
+                hr[i + 4] = end[1];
+            }
+        }
+        for (int k = a.N % 8; k > 0; k -= 4, i += 4) {
+            // a row without this state adds nothing
+            const bool has = i < a.N;
+            const int n[1] = {has ? i : 0};
+            const float A2[1] = {has ? Ar[i] : 0.0f}, in[1] = {has ? hr[i] : 0.0f};
+            float start[1], end[1], more[T], part_dx[T];
+#pragma unroll
+            for (int j = 0; j < T; ++j) {
+                more[j] = 0.0f;
+                part_dx[j] = keep_if(has, dx[j]);
+            }
+            scan_states<T, 1>(tb, tc, n, A2, in, lane, delta, part_dx, sum, more, start, end);
+#pragma unroll
+            for (int j = 0; j < T; ++j)
+                y[j] += keep_if(has, more[j]);
+            if (kept && has)
+                kept[i] = start[0];
+            if (lane == 15 && has)
+                hr[i] = end[0];
+        }
+        float v[I];
+        sum_rows<T>(y, v);
+#pragma unroll
+        for (int j = 0; j < I; ++j) {
+            v[j] = __builtin_fmaf(skip, x[j], v[j]);
+            if (a.z.p)
+                v[j] *= silu(z[j]);
+            v[j] = keep_if(j < left, v[j]);
+        }
+        if (live) {
+            E *yr = a.y.row<E>(b, d) + p0;
+            if (p0 + P <= a.L)
+                store_vec<E, I>(at(yr, pos), v);
+            else
+                store_upto<E, I>(at(yr, pos), a.L - p0 - pos, v);
+        }
+        // the next part's tile takes the place of this one's
+        __syncthreads();
+    }
+    // padding
+    if (live) {
+        E *r = a.y.row<E>(b, d);
+        for (long long t = (long long)parts * P + (tid & 63); t < a.L; t += 64)
             r[t] = (E)0.0f;
     }
     __syncthreads();
@@ -412,46 +612,41 @@ constexpr int kGradWaves = 8;
 template <int T>
 constexpr int kSwap = 32 / T;
 
-inline size_t backward_lds(int N, int T, int set) {
-    return ((size_t)2 * N * 16 * T + kGradWaves * 3 * 16 * T + (size_t)3 * set * N +
-            (size_t)2 * set + (size_t)2 * 32 * 64 * (kGradWaves / 2)) * 4;
+inline size_t backward_lds(int NP, int T, int set) {
+    return ((size_t)2 * NP * 16 * T + kGradWaves * 3 * 16 * T + (size_t)3 * set * NP +
+            (size_t)10 * set + (size_t)2 * 32 * 64 * (kGradWaves / 2)) * 4;
 }
 
-// The sums over the four rows of T values a lane: row r gets those of positions
-// r T / 4 and on.
-__device__ inline float swap32(float a, float b) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a),
-                                                    __builtin_bit_cast(unsigned, b), false, false);
-    return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+// The sums over a row's lanes of four values: that of value s in lanes 4 s to 4 s + 3.
+// Lanes change halves with their mirror image, each keeping one of two values.
+template <int CTRL>
+__device__ inline float dpp(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
+                                         0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
-__device__ inline float swap16(float a, float b) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a),
-                                                    __builtin_bit_cast(unsigned, b), false, false);
-    return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
-}
-template <int T>
-__device__ inline void sum_rows(const float (&v)[T], float (&out)[T / 4]) {
-    float u[T / 2];
-#pragma unroll
-    for (int j = 0; j < T / 2; ++j)
-        u[j] = swap32(v[j], v[j + T / 2]);
-#pragma unroll
-    for (int j = 0; j < T / 4; ++j)
-        out[j] = swap16(u[j], u[j + T / 4]);
+__device__ inline float row_sum4(float v0, float v1, float v2, float v3, int lane) {
+    const bool hi = lane & 8, odd = lane & 4;
+    const float h0 = (hi ? v2 : v0) + dpp<0x140>(hi ? v0 : v2);   // row_mirror
+    const float h1 = (hi ? v3 : v1) + dpp<0x140>(hi ? v1 : v3);
+    float u = (odd ? h1 : h0) + dpp<0x141>(odd ? h0 : h1);        // row_half_mirror
+    u += dpp<0xb1>(u);                                            // the neighbours of a quad
+    return u + dpp<0x4e>(u);
 }
 
 template <typename E, int T, int S>
 __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs ga) {
     constexpr int P = 16 * T, I = T / 4, TH = 64 * kGradWaves, SW = S < kSwap<T> ? S : kSwap<T>;
+    constexpr int NP = 4 * S;                      // states with those that fill the rows
     const ScanArgs &a = ga.f;
     extern __shared__ __attribute__((aligned(16))) float lds[];
-    float *tb = lds, *tc = tb + a.N * P;
-    float *pre = tc + a.N * P;                     // delta, delta x, dy of a wave's channel
+    float *tb = lds, *tc = tb + NP * P;
+    float *pre = tc + NP * P;                      // delta, delta x, dy of a wave's channel
     float *swp = pre + kGradWaves * 3 * P;         // half the waves' gradients of B and C
-    float *carry = swp + 2 * 32 * 64 * (kGradWaves / 2);   // G at the part's end, set x N
-    float *As = carry + ga.set * a.N;              // A log2 e
-    float *dAs = As + ga.set * a.N;                // dA
-    float *ps = dAs + ga.set * a.N;                // dDskip, ddt_bias: set x 2
+    float *carry = swp + 2 * 32 * 64 * (kGradWaves / 2);   // G at the part's end, set x NP
+    float *As = carry + ga.set * NP;               // A log2 e
+    float *dAs = As + ga.set * NP;                 // dA
+    float *ps = dAs + ga.set * NP;                 // dDskip, ddt_bias by rows: set x 4 x 2
+    float *vec = ps + ga.set * 8;                  // dt_bias, Dskip: set x 2
     const int tid = threadIdx.x, lane = tid & 15, rowi = (tid >> 4) & 3;
     // uniform: a wave's rows of activations have their addresses in scalar registers
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -463,17 +658,25 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
     const int c0 = set * ga.set;                   // the set's first channel in the group
     const int count = min(ga.set, a.Dg - c0);
     const long long first = (long long)grp * a.Dg + c0;
-    const int n_pos = row_length(a.lengths, b, a.L);
+    const int n_pos = __builtin_amdgcn_readfirstlane(row_length(a.lengths, b, a.L));
     const int parts = (n_pos + P - 1) / P;
-    const int units = 2 * a.N * (P / kUnit);
-    for (int i = tid; i < ga.set * a.N; i += TH) {
-        const bool ok = i < count * a.N;
-        As[i] = ok ? a.A[first * a.N + i] * kLog2e : 0.0f;
-        carry[i] = ok && ga.dstate_out ? ga.dstate_out[((long long)b * a.D + first) * a.N + i] : 0.0f;
+    for (int i = tid; i < ga.set * NP; i += TH) {
+        const int c = i / NP, n = i % NP;
+        const bool ok = c < count && n < a.N;
+        const long long at = (first + (ok ? c : 0)) * a.N + (ok ? n : 0);
+        As[i] = ok ? a.A[at] * kLog2e : 0.0f;
+        carry[i] = ok && ga.dstate_out ? ga.dstate_out[(long long)b * a.D * a.N + at] : 0.0f;
         dAs[i] = 0.0f;
     }
-    for (int i = tid; i < count * 2; i += TH)
+    for (int i = tid; i < ga.set * 8; i += TH)
         ps[i] = 0.0f;
+    for (int i = tid; i < count; i += TH) {
+        vec[2 * i] = a.dt_bias ? a.dt_bias[first + i] : 0.0f;
+        vec[2 * i + 1] = a.Dskip ? a.Dskip[first + i] : 0.0f;
+    }
+    // the states that fill the rows read 0
+    for (int i = tid; i < (NP - a.N) * P; i += TH)
+        tb[a.N * P + i] = tc[a.N * P + i] = 0.0f;
     // the positions of a part that this lane prepares, and the wave's place for them
     const int pos = lane * T + rowi * I;
     float *mine = pre + wave * 3 * P;
@@ -482,23 +685,39 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
     float nin[S];
     auto fetch = [&](int c, int part) {
         const int d = (int)first + c, p0 = part * P, left = n_pos - p0 - pos;
-        nx = load_raw<E, I>(a.x.row<const E>(b, d) + p0 + pos, left);
-        nd = load_raw<E, I>(a.dt.row<const E>(b, d) + p0 + pos, left);
-        ng = load_raw<E, I>(ga.dy.row<const E>(b, d) + p0 + pos, left);
-        if (a.z.p)
-            nz = load_raw<E, I>(a.z.row<const E>(b, d) + p0 + pos, left);
-        const float *st = a.states + (((long long)b * a.D + d) * a.parts + part) * a.N;
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-            nin[s] = n0 + s < a.N ? st[n0 + s] : 0.0f;
+        const E *xr = a.x.row<const E>(b, d) + p0, *dr = a.dt.row<const E>(b, d) + p0;
+        const E *gr = ga.dy.row<const E>(b, d) + p0;
+        const E *zr = a.z.p ? a.z.row<const E>(b, d) + p0 : gr;
+        if (p0 + P <= n_pos) {
+            nx = load_whole<E, I>(at(xr, pos));
+            nd = load_whole<E, I>(at(dr, pos));
+            ng = load_whole<E, I>(at(gr, pos));
+            nz = load_whole<E, I>(at(zr, pos));
+        } else {
+            nx = load_part<E, I>(at(xr, pos), left);
+            nd = load_part<E, I>(at(dr, pos), left);
+            ng = load_part<E, I>(at(gr, pos), left);
+            nz = load_part<E, I>(at(zr, pos), left);
+        }
+        load_vec<float, S>(at(a.states + (((long long)b * a.D + d) * a.parts + part) * NP, n0), nin);
     };
-    if (parts > 0 && wave < count)
-        fetch(wave, parts - 1);
+    const int units = 2 * a.N * (P / kUnit);
+    typename Vec<E, kUnit>::type nt;
+    if (parts > 0) {
+        if (wave < count)
+            fetch(wave, parts - 1);
+        if (tid < units)
+            nt = load_tile<E, T>(a, b, grp, tid, (parts - 1) * P, n_pos);
+    }
     for (int part = parts - 1; part >= 0; --part) {
         const int p0 = part * P;
-        for (int u = tid; u < units; u += TH)
-            store_tile<E, T>(tb, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
+        if (tid < units)
+            store_tile<E, T>(tb, tc, a.N, tid, nt);
+        for (int u = tid + TH; u < units; u += TH)
+            store_tile<E, T>(tb, tc, a.N, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
         __syncthreads();
+        if (part > 0 && tid < units)
+            nt = load_tile<E, T>(a, b, grp, tid, p0 - P, n_pos);
         float dB[S][T], dC[S][T];
 #pragma unroll
         for (int s = 0; s < S; ++s)
@@ -507,9 +726,8 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
                 dB[s][j] = dC[s][j] = 0.0f;
         for (int c = wave; c < count; c += kGradWaves) {
             const int d = (int)first + c, left = n_pos - p0 - pos;
-            float x[I], delta[I], slope[I], z[I], dout[I], dy[I], in[S];
-            const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
-            const float skip = a.Dskip ? a.Dskip[d] : 0.0f;
+            float x[I], delta[I], slope[I], z[I], dout[I], dy[I], in[S], A2[S], end[S], dA[S];
+            const float bias = vec[2 * c], skip = vec[2 * c + 1];
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const float v = (float)nd[i] + bias;
@@ -524,9 +742,12 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
                 q[P] = delta[i] * x[i];
                 q[2 * P] = dy[i];
             }
+            float *own = carry + c * NP + n0;
+            lds_load<S>(As + c * NP + n0, A2);
+            lds_load<S>(own, end);
 #pragma unroll
             for (int s = 0; s < S; ++s)
-                in[s] = nin[s];
+                in[s] = n0 + s < a.N ? nin[s] : 0.0f;
             // the next channel's, under way
             if (c + kGradWaves < count)
                 fetch(c + kGradWaves, part);
@@ -535,70 +756,47 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
             __builtin_amdgcn_wave_barrier();
             float de[T], dx[T], g[T], gB[T], sA[T], yv[T], sum = 0.0f;
 #pragma unroll
-            for (int j4 = 0; j4 < T / 4; ++j4) {
-                const float *q = mine + (j4 * 16 + lane) * 4;
-                const float4 u = *(const float4 *)q, v = *(const float4 *)(q + P);
-                const float4 e = *(const float4 *)(q + 2 * P);
-                const float uu[4] = {u.x, u.y, u.z, u.w}, vv[4] = {v.x, v.y, v.z, v.w};
-                const float ee[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int j = 4 * j4 + i;
-                    de[j] = uu[i];
-                    dx[j] = vv[i];
-                    g[j] = ee[i];
-                    sum += uu[i];
-                    gB[j] = sA[j] = yv[j] = 0.0f;
-                }
+            for (int j = 0; j < T; j += 4) {
+                const float *q = mine + (j * 4 + lane) * 4;
+                lds_load<4>(q, de + j);
+                lds_load<4>(q + P, dx + j);
+                lds_load<4>(q + 2 * P, g + j);
             }
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
+            for (int j = 0; j < T; ++j) {
+                sum += de[j];
+                gB[j] = sA[j] = yv[j] = 0.0f;
+            }
+#pragma unroll
             for (int s = 0; s < S; ++s) {
-                const bool has = n0 + s < a.N;
-                const int n = has ? n0 + s : 0;
-                const float A2 = has ? As[c * a.N + n] : 0.0f;
-                const float after = has ? carry[c * a.N + n] : 0.0f;
-                float av[T], h[T], Bv[T], Cv[T], m[1], e[1] = {0.0f};
+                float av[T], h[T], Bv[T], Cv[T];
 #pragma unroll
-                for (int j4 = 0; j4 < T / 4; ++j4) {
-                    const float4 u = *(const float4 *)(tb + tile_at<T>(n, j4, lane));
-                    const float4 v = *(const float4 *)(tc + tile_at<T>(n, j4, lane));
-                    Bv[4 * j4] = u.x;
-                    Bv[4 * j4 + 1] = u.y;
-                    Bv[4 * j4 + 2] = u.z;
-                    Bv[4 * j4 + 3] = u.w;
-                    Cv[4 * j4] = v.x;
-                    Cv[4 * j4 + 1] = v.y;
-                    Cv[4 * j4 + 2] = v.z;
-                    Cv[4 * j4 + 3] = v.w;
+                for (int j = 0; j < T; j += 4) {
+                    lds_load<4>(tb + tile_at<T>(n0 + s, j / 4, lane), Bv + j);
+                    lds_load<4>(tc + tile_at<T>(n0 + s, j / 4, lane), Cv + j);
                 }
-                if (!has) {   // a lane without this state adds nothing
-#pragma unroll
-                    for (int j = 0; j < T; ++j)
-                        Bv[j] = Cv[j] = 0.0f;
-                }
+                // the run's own map of h upwards, and of G downwards
+                float e = 0.0f, f = 0.0f;
 #pragma unroll
                 for (int j = 0; j < T; ++j) {
-                    av[j] = __builtin_amdgcn_exp2f(A2 * de[j]);
-                    e[0] = __builtin_fmaf(av[j], e[0], dx[j] * Bv[j]);
+                    av[j] = __builtin_amdgcn_exp2f(A2[s] * de[j]);
+                    e = j ? __builtin_fmaf(av[j], e, dx[j] * Bv[j]) : dx[j] * Bv[j];
                 }
-                const float run = m[0] = __builtin_amdgcn_exp2f(A2 * sum);
-                scan_up(m, e);
-                const float start =
-                    neighbour<kFromLower>(in[s], __builtin_fmaf(m[0], in[s], e[0]));
+#pragma unroll
+                for (int j = T - 1; j >= 0; --j)
+                    f = av[j] * (j < T - 1 ? __builtin_fmaf(Cv[j], g[j], f) : Cv[j] * g[j]);
+                float up = __builtin_amdgcn_exp2f(A2[s] * sum), down = up;
+                scan_both(up, e, down, f);
+                const float start = neighbour<kFromLower>(in[s], __builtin_fmaf(up, in[s], e));
+                const float low = __builtin_fmaf(down, end[s], f);
+                float G = neighbour<kFromUpper>(end[s], low);
+                end[s] = low;
                 float prev = start;
 #pragma unroll
                 for (int j = 0; j < T; ++j)
                     prev = h[j] = __builtin_fmaf(av[j], prev, dx[j] * Bv[j]);
-                // G below the lane's run, from 0 above it, then from the lanes above
-                e[0] = 0.0f;
-#pragma unroll
-                for (int j = T - 1; j >= 0; --j)
-                    e[0] = av[j] * __builtin_fmaf(Cv[j], g[j], e[0]);
-                m[0] = run;
-                scan_down(m, e);
-                const float low = __builtin_fmaf(m[0], after, e[0]);
-                float G = neighbour<kFromUpper>(after, low), dA = 0.0f;
+                dA[s] = 0.0f;
 #pragma unroll
                 for (int j = T - 1; j >= 0; --j) {
                     const float gt = __builtin_fmaf(Cv[j], g[j], G);
@@ -608,22 +806,25 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
                     gB[j] = __builtin_fmaf(gt, Bv[j], gB[j]);
                     yv[j] = __builtin_fmaf(Cv[j], h[j], yv[j]);
                     const float t = G * (j ? h[j ? j - 1 : 0] : start);
-                    sA[j] = __builtin_fmaf(A2, t, sA[j]);
-                    dA = __builtin_fmaf(de[j], t, dA);
-                }
-                dA = row_sum(dA);
-                if (has) {
-                    if (lane == 15)
-                        dAs[c * a.N + n] += dA;
-                    if (lane == 0)
-                        carry[c * a.N + n] = low;
+                    sA[j] = __builtin_fmaf(A2[s], t, sA[j]);
+                    dA[s] = __builtin_fmaf(de[j], t, dA[s]);
                 }
                 // one state's values at a time: sums put off to the end would keep every
                 // state's h and g in registers
 #pragma unroll
                 for (int j = 0; j < T; ++j)
                     asm volatile("" : "+v"(dB[s][j]), "+v"(dC[s][j]), "+v"(gB[j]), "+v"(sA[j]),
-                                 "+v"(yv[j]));
+                                 "+v"(yv[j]), "+v"(dA[s]));
+            }
+            if (lane == 0)
+                lds_store<S>(own, end);
+#pragma unroll
+            for (int s = 0; s < S; s += 4) {
+                const float u = row_sum4(dA[s], s + 1 < S ? dA[s + 1 < S ? s + 1 : 0] : 0.0f,
+                                         s + 2 < S ? dA[s + 2 < S ? s + 2 : 0] : 0.0f,
+                                         s + 3 < S ? dA[s + 3 < S ? s + 3 : 0] : 0.0f, lane);
+                if ((lane & 3) == 0 && s + (lane >> 2) < S)
+                    dAs[c * NP + n0 + s + (lane >> 2)] += u;
             }
             // the gradients of the positions that this lane prepared
             float v0[I], v1[I], v2[I], ox[I], ot[I], oz[I], sD = 0.0f, sb = 0.0f;
@@ -642,16 +843,22 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
                 sD = __builtin_fmaf(dy[i], x[i], sD);
             }
             const int room = a.L - p0 - pos;
-            store_upto<E, I>(ga.dx.row<E>(b, d) + p0 + pos, room, ox);
-            store_upto<E, I>(ga.ddt.row<E>(b, d) + p0 + pos, room, ot);
-            if (a.z.p)
-                store_upto<E, I>(ga.dz.row<E>(b, d) + p0 + pos, room, oz);
-            sD = wave_sum(sD);
-            sb = wave_sum(sb);
-            if ((tid & 63) == 0) {
-                ps[2 * c] += sD;
-                ps[2 * c + 1] += sb;
+            E *xo = ga.dx.row<E>(b, d) + p0, *to = ga.ddt.row<E>(b, d) + p0;
+            E *zo = a.z.p ? ga.dz.row<E>(b, d) + p0 : nullptr;
+            if (p0 + P <= a.L) {
+                store_vec<E, I>(at(xo, pos), ox);
+                store_vec<E, I>(at(to, pos), ot);
+                if (zo)
+                    store_vec<E, I>(at(zo, pos), oz);
+            } else {
+                store_upto<E, I>(at(xo, pos), room, ox);
+                store_upto<E, I>(at(to, pos), room, ot);
+                if (zo)
+                    store_upto<E, I>(at(zo, pos), room, oz);
             }
+            const float u = row_sum4(sD, sb, 0.0f, 0.0f, lane);
+            if ((lane & 3) == 0 && lane < 8)
+                ps[(c * 4 + rowi) * 2 + (lane >> 2)] += u;
         }
         // dB and dC of the part: the upper half of the waves to the lower, by halves
 #pragma unroll
@@ -713,13 +920,14 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
         }
     float *out = ga.params + (long long)b * a.D * (a.N + 2);
     for (int i = tid; i < count * a.N; i += TH) {
-        out[first * a.N + i] = dAs[i];
+        const int at = i / a.N * NP + i % a.N;
+        out[first * a.N + i] = dAs[at];
         if (ga.dstate)
-            ga.dstate[((long long)b * a.D + first) * a.N + i] = carry[i];
+            ga.dstate[((long long)b * a.D + first) * a.N + i] = carry[at];
     }
-    for (int c = tid; c < count; c += TH) {
-        out[(long long)a.D * a.N + first + c] = ps[2 * c];
-        out[(long long)a.D * (a.N + 1) + first + c] = ps[2 * c + 1];
+    for (int i = tid; i < count * 2; i += TH) {
+        const float *q = ps + i / 2 * 8 + i % 2;
+        out[(long long)a.D * (a.N + i % 2) + first + i / 2] = (q[0] + q[2]) + (q[4] + q[6]);
     }
 }
 
@@ -857,28 +1065,28 @@ inline bool scan_shape(int type, int B, int D, int L, int N, int G) {
 // Positions a lane: the gradients' parts and the states' layout depend on it.
 // More than 16 states leave the gradients' registers room for four.
 inline int lane_positions(int L, int N) { return L <= 64 || N > 16 ? 4 : 8; }
+// States a lane of a row in the gradients, a quarter of them all.
+inline int row_states(int N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 inline long long part_count(int L, int N) {
     return cdivll(L > 0 ? L : 1, 16 * lane_positions(L, N));
 }
 
-inline size_t forward_lds(int N, int T, int W) {
-    return ((size_t)2 * N * 16 * T + 2 * (16 / W) * N + (W > 1 ? (2 * 4 * 16 + 4 * 64) * T : 0)) * 4;
-}
-
-template <typename E, int T, int W>
+template <typename E, int T, bool ROWS>
 int launch_forward(ScanArgs &c, hipStream_t s) {
-    c.blocks = (int)cdivll(c.Dg, 16 / W);
+    constexpr int CB = ROWS ? 4 : 16;
+    c.blocks = (int)cdivll(c.Dg, CB);
     c.every = lane_positions(c.L, c.N) * 16 / T;
     const long long grid = (long long)c.blocks * c.G * c.B;
-    const size_t lds = forward_lds(c.N, T, W);
+    const size_t lds =
+        ((size_t)2 * c.N * 16 * T + 2 * CB * c.N + (ROWS ? 4 * 2 * 16 * T : 0)) * sizeof(float);
+    const auto kernel = ROWS ? scan_rows_kernel<E, T> : scan_channels_kernel<E, T>;
     if (grid >= (1ll << 31) || lds > (size_t)kLds)
         return FINC_EUNSUPPORTED;
     if (lds > 64 * 1024)
-        (void)hipFuncSetAttribute((const void *)scan_forward_kernel<E, T, W>,
+        (void)hipFuncSetAttribute((const void *)kernel,
                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     (void)hipGetLastError();   // the launch check decides
-    hipLaunchKernelGGL((scan_forward_kernel<E, T, W>), dim3((unsigned)grid), dim3(kThreads),
-                       (unsigned)lds, s, c);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), (unsigned)lds, s, c);
     return launched();
 }
 
@@ -903,6 +1111,7 @@ bool scan_common(const finc_scan_args *a, ScanArgs &c) {
     c.Dg = a->D / a->G;
     c.softplus = a->softplus;
     c.parts = (int)part_count(a->L, a->N);
+    c.NP = 4 * row_states(a->N);
     return true;
 }
 
@@ -918,7 +1127,7 @@ inline int set_channels(int B, int D, int G) {
 template <typename E, int T, int S>
 int launch_backward(GradArgs &c, hipStream_t s) {
     const long long grid = (long long)c.sets * c.f.G * c.f.B;
-    const size_t lds = backward_lds(c.f.N, T, c.set);
+    const size_t lds = backward_lds(4 * S, T, c.set);
     if (grid >= (1ll << 31) || lds > (size_t)kLds)
         return FINC_EUNSUPPORTED;
     (void)hipFuncSetAttribute((const void *)scan_backward_kernel<E, T, S>,
@@ -929,18 +1138,17 @@ int launch_backward(GradArgs &c, hipStream_t s) {
     return launched();
 }
 
-// S states a lane, a quarter of them all.
 template <typename E>
 int dispatch_backward(GradArgs &c, hipStream_t s) {
-    const int N = c.f.N;
-    if (lane_positions(c.f.L, N) == 4)
-        return N <= 4    ? launch_backward<E, 4, 1>(c, s)
-               : N <= 8  ? launch_backward<E, 4, 2>(c, s)
-               : N <= 16 ? launch_backward<E, 4, 4>(c, s)
-               : N <= 32 ? launch_backward<E, 4, 8>(c, s)
-                         : launch_backward<E, 4, 16>(c, s);
-    return N <= 4   ? launch_backward<E, 8, 1>(c, s)
-           : N <= 8 ? launch_backward<E, 8, 2>(c, s)
+    const int S = row_states(c.f.N);
+    if (lane_positions(c.f.L, c.f.N) == 4)
+        return S == 1   ? launch_backward<E, 4, 1>(c, s)
+               : S == 2 ? launch_backward<E, 4, 2>(c, s)
+               : S == 4 ? launch_backward<E, 4, 4>(c, s)
+               : S == 8 ? launch_backward<E, 4, 8>(c, s)
+                        : launch_backward<E, 4, 16>(c, s);
+    return S == 1   ? launch_backward<E, 8, 1>(c, s)
+           : S == 2 ? launch_backward<E, 8, 2>(c, s)
                     : launch_backward<E, 8, 4>(c, s);
 }
 
@@ -956,7 +1164,7 @@ extern "C" {
 size_t finc_selective_scan_states_bytes(int B, int D, int L, int N) {
     if (!scan_shape(FINC_F32, B, D, L, N, 1))
         return 0;
-    return ((size_t)B * D * part_count(L, N) * N * 4 + 255) / 256 * 256;
+    return ((size_t)B * D * part_count(L, N) * 4 * row_states(N) * 4 + 255) / 256 * 256;
 }
 
 int finc_selective_scan_forward(const finc_scan_args *a, hipStream_t stream) {
@@ -992,19 +1200,24 @@ int finc_selective_scan_forward(const finc_scan_args *a, hipStream_t stream) {
     c.state = a->state;
     c.state_out = a->state_out;
     int rc = FINC_EINVAL;
-    // 2048 waves are two a SIMD
-    const bool few = (long long)B * D < 4 * 2048;
-    const int T = L <= 64 ? 4 : L <= 128 || a->N > 32 ? 8 : 16;
+    // A wave for a channel up to 8192 of them, a row of lanes from there on, where the
+    // rows of a wave share their reads of B and C and nothing is handed over: 2048 x
+    // 4096 positions at batch 4 take 230 us by waves and 180 by rows, 6000 channels x
+    // 1531 positions 32 us by waves and 71 by rows (too few of them).  Sixteen
+    // positions a lane halve the scans over lanes and the barriers, but their
+    // registers leave two waves a SIMD: where no more are there (2048 x 4096
+    // positions: 71 us against 82 with eight; 6000 x 1531: 42 against 32).
+    const long long channels = (long long)B * D;
+    const bool sixteen = L > 128 && a->N <= 32 && channels <= 2048;
     with_type(a->type, [&](auto e) {
         typedef decltype(e) E;
-        if (few)
-            rc = T == 4   ? launch_forward<E, 4, 4>(c, stream)
-                 : T == 8 ? launch_forward<E, 8, 4>(c, stream)
-                          : launch_forward<E, 16, 4>(c, stream);
+        if (channels < 8192)
+            rc = L <= 64   ? launch_forward<E, 4, true>(c, stream)
+                 : sixteen ? launch_forward<E, 16, true>(c, stream)
+                           : launch_forward<E, 8, true>(c, stream);
         else
-            rc = T == 4   ? launch_forward<E, 4, 1>(c, stream)
-                 : T == 8 ? launch_forward<E, 8, 1>(c, stream)
-                          : launch_forward<E, 16, 1>(c, stream);
+            rc = L <= 64 ? launch_forward<E, 4, false>(c, stream)
+                         : launch_forward<E, 8, false>(c, stream);
     });
     return rc;
 }
