@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 
 import torch
 
@@ -30,34 +31,16 @@ F32, BF16, F16 = 0, 1, 2
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 MAX_TAPS, MAX_STATE, MAX_ROW = 8, 64, 16384
 
-
-def _struct(name, fields):
-    """A ctypes structure of "kind: names" lines, in the header's order."""
-    kinds = {"int": _i, "ll": _ll, "ull": _ull, "double": _d, "ptr": _vp}
-    out = []
-    for line in fields:
-        kind, names = line.split(":")
-        out += [(n, kinds.get(kind) or globals()[kind]) for n in names.split()]
-    return type(name, (ctypes.Structure,), {"_fields_": out})
-
-
-Raster = _struct("Raster", ["ptr: p", "ll: sb sd"])
-ConvArgs = _struct("ConvArgs", ["int: type B D L K silu", "Raster: x y",
-                                "ptr: w bias state state_out lengths"])
-ConvGrads = _struct("ConvGrads", ["Raster: dy dx", "ptr: dw dbias dstate_out dstate workspace"])
-ScanArgs = _struct("ScanArgs", ["int: type B D L N G softplus", "Raster: x dt z Bm Cm y",
-                                "ptr: A Dskip dt_bias state state_out states lengths"])
-ScanGrads = _struct("ScanGrads", ["Raster: dy dx ddt dz dBm dCm",
-                                  "ptr: dA dDskip ddt_bias dstate_out dstate workspace"])
-ScanStepArgs = _struct("ScanStepArgs", ["int: type B S D N G softplus", "ptr: x dt z Bm Cm",
-                                        "ll: sx sdt sz sB sC sy",
-                                        "ptr: y A Dskip dt_bias state slots"])
-NormArgs = _struct("NormArgs", ["int: type rtype M D", "ptr: x residual y r",
-                                "ll: sx sres sy sr", "ptr: w scale", "double: eps p",
-                                "ull: seed offset"])
-NormGradArgs = _struct("NormGradArgs", ["int: type rtype M D", "ptr: dy r dr dx dresidual",
-                                        "ll: sdy sr sdr sdx sdres", "ptr: w dw", "double: eps p",
-                                        "ull: seed offset", "ptr: workspace"])
+# The sequence operators' argument structures, in the header's order of fields and
+# with the platform's alignment (packing takes a fraction of a ctypes structure's
+# time, which counts where a call takes a few microseconds).  A raster is "Pqq".
+CONV_ARGS = struct.Struct("@6i Pqq Pqq 5P")
+CONV_GRADS = struct.Struct("@Pqq Pqq 5P")
+SCAN_ARGS = struct.Struct("@7i Pqq Pqq Pqq Pqq Pqq Pqq 7P")
+SCAN_GRADS = struct.Struct("@Pqq Pqq Pqq Pqq Pqq Pqq 6P")
+SCAN_STEP_ARGS = struct.Struct("@7i 5P 6q 6P")
+NORM_ARGS = struct.Struct("@4i 4P 4q 2P 2d 2Q")
+NORM_GRAD_ARGS = struct.Struct("@4i 5P 5q 2P 2d 2Q P")
 
 # name -> (restype, argtypes); mirrors include/finc.h
 SIGNATURES = {
@@ -128,22 +111,22 @@ SIGNATURES = {
     "finc_conv1x1_workspace_bytes": (_sz, [_i]),
     "finc_conv1x1_forward": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp]),
     "finc_conv1x1_inverse": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp]),
-    "finc_causal_conv_forward": (_i, [ctypes.POINTER(ConvArgs), _vp]),
+    "finc_causal_conv_forward": (_i, [_vp, _vp]),
     "finc_causal_conv_workspace_bytes": (_sz, [_i, _i, _i, _i]),
-    "finc_causal_conv_backward": (_i, [ctypes.POINTER(ConvArgs), ctypes.POINTER(ConvGrads), _vp]),
+    "finc_causal_conv_backward": (_i, [_vp, _vp, _vp]),
     "finc_causal_conv_step": (_i, [_i, _vp, _ll, _vp, _ll, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i,
                                    _vp]),
     "finc_selective_scan_states_bytes": (_sz, [_i, _i, _i, _i]),
-    "finc_selective_scan_forward": (_i, [ctypes.POINTER(ScanArgs), _vp]),
+    "finc_selective_scan_forward": (_i, [_vp, _vp]),
     "finc_selective_scan_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
-    "finc_selective_scan_backward": (_i, [ctypes.POINTER(ScanArgs), ctypes.POINTER(ScanGrads),
+    "finc_selective_scan_backward": (_i, [_vp, _vp,
                                           _vp]),
-    "finc_selective_scan_step": (_i, [ctypes.POINTER(ScanStepArgs), _vp]),
+    "finc_selective_scan_step": (_i, [_vp, _vp]),
     "finc_dropout_counters": (_ull, [_i, _i]),
     "finc_dropout": (_i, [_i, _vp, _ll, _vp, _ll, _vp, _ll, _i, _i, _d, _ull, _ull, _vp]),
-    "finc_add_norm_forward": (_i, [ctypes.POINTER(NormArgs), _vp]),
+    "finc_add_norm_forward": (_i, [_vp, _vp]),
     "finc_add_norm_workspace_bytes": (_sz, [_i, _i]),
-    "finc_add_norm_backward": (_i, [ctypes.POINTER(NormGradArgs), _vp]),
+    "finc_add_norm_backward": (_i, [_vp, _vp]),
 }
 
 
@@ -187,8 +170,15 @@ def _ptr(t: torch.Tensor | None):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+# torch's current stream and device without the objects around them (2.8 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_current_device())
 
 
 def _dev(t: torch.Tensor, name: str, shape=None):
@@ -912,70 +902,93 @@ def flow_sample(z, params: torch.Tensor, prepared: torch.Tensor, L: int, K: int,
 # Activations are float32, bfloat16 or float16, parameters and scan states float32.
 
 
-def _act(t: torch.Tensor, name: str, shape=None, dtype=None):
-    """A device tensor of activations with contiguous last dimension."""
-    if not t.is_cuda:
+_NO_RASTER = (0, 0, 0)
+
+
+def _type(x: torch.Tensor, name: str = "x"):
+    """(device, type id) of a call's first activations."""
+    if not x.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.device.index != torch.cuda.current_device():
+    dev = x.get_device()
+    if dev != _current_device():
         raise ValueError(f"{name} must be on the current device")
-    if t.dtype not in _TYPES:
+    kind = _TYPES.get(x.dtype)
+    if kind is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name} must be contiguous in its last dimension")
-    return t
+    return dev, kind
 
 
-def _param(t, name, shape, dtype=torch.float32):
-    """A contiguous device tensor, or None."""
-    if t is None:
-        return None
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be a tensor on the current device")
+def _act(t: torch.Tensor, name: str, dev: int, dtype, shape):
+    """A tensor of activations, contiguous in its last dimension."""
+    if t.get_device() == dev and t.dtype == dtype and t.shape == shape \
+            and (t.is_contiguous() or t.stride(-1) == 1 or shape[-1] <= 1):
+        return t
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the device of the other tensors")
     if t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}")
-    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t
+    raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+def _param(t: torch.Tensor | None, name: str, dev: int, shape, dtype=torch.float32) -> int:
+    """The address of a contiguous tensor, or 0 for None."""
+    if t is None:
+        return 0
+    if t.get_device() == dev and t.dtype == dtype and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the device of the other tensors")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _raster(t: torch.Tensor | None):
     """A (B, D, L) or (B, G, N, L) tensor as the ABI's finc_raster."""
     if t is None:
-        return Raster(None, 0, 0)
-    if t.dim() == 4 and t.shape[1] > 1 and t.shape[2] > 1 \
-            and t.stride(1) != t.shape[2] * t.stride(2):
+        return _NO_RASTER
+    st = t.stride()
+    if len(st) == 3:
+        return t.data_ptr(), st[0], st[1]
+    G, N = t.shape[1], t.shape[2]
+    if G > 1 and N > 1 and st[1] != N * st[2]:
         raise ValueError("the groups of a (B, G, N, L) tensor must follow each other")
-    row = t.stride(2) if t.dim() == 4 and t.shape[2] > 1 else t.stride(1)
-    return Raster(t.data_ptr(), t.stride(0), row)
+    return t.data_ptr(), st[0], st[2] if N > 1 else st[1]
 
 
-def _like(x: torch.Tensor, shape=None):
-    """A contiguous output of x's type."""
-    return torch.empty(x.shape if shape is None else shape, dtype=x.dtype, device=x.device)
+def _out(t: torch.Tensor | None, like: torch.Tensor, name: str, dev: int):
+    """An output of the shape and type of `like`, contiguous unless given."""
+    if t is None:
+        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    return _act(t, name, dev, like.dtype, like.shape)
 
 
-def _conv_args(x, w, bias, silu, state, lengths):
-    if x.dim() != 3:
-        raise ValueError(f"x has shape {tuple(x.shape)}, expected (B, D, L)")
-    B, D, L = x.shape
-    _act(x, "x")
-    if w.dim() != 2:
-        raise ValueError(f"w has shape {tuple(w.shape)}, expected (D, K)")
-    K = w.shape[1]
+def _space(t: torch.Tensor | None, nbytes: int, dev: int, name: str = "workspace"):
+    """A buffer of at least nbytes."""
+    if t is None:
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=f"cuda:{dev}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the device of the other tensors")
+    return _bytes_buf(t, nbytes, name)
+
+
+def _dims(t: torch.Tensor, name: str, form: str):
+    """The shape of t, which is of the form "(B, D, L)"."""
+    if t.dim() != form.count(",") + 1:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {form}")
+    return t.shape
+
+
+def _conv_dims(x, w):
+    B, D, L = _dims(x, "x", "(B, D, L)")
+    K = _dims(w, "w", "(D, K)")[1]
     if not 1 <= K <= MAX_TAPS:
         raise ValueError(f"w has {K} taps, expected 1 to {MAX_TAPS}")
-    _param(w, "w", (D, K))
-    _param(bias, "bias", (D,))
-    _param(state, "state", (B, D, K - 1), x.dtype)
-    _param(lengths, "lengths", (B,), torch.int32)
-    return ConvArgs(_TYPES[x.dtype], B, D, L, K, int(silu), _raster(x), _raster(None), _ptr(w),
-                    _ptr(bias), _ptr(state), None, _ptr(lengths))
+    return B, D, L, K
 
 
 def causal_conv_forward(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, *,
@@ -985,11 +998,17 @@ def causal_conv_forward(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | N
     """y = act(bias + the causal convolution of x (B, D, L) with w (D, K)) (see
     finc_causal_conv_forward); state_out (B, D, K - 1) is written if given."""
     lib_ = _require_lib()
-    a = _conv_args(x, w, bias, silu, state, lengths)
-    y = _like(x) if out is None else _act(out, "out", x.shape, x.dtype)
-    a.y = _raster(y)
-    a.state_out = _ptr(_param(state_out, "state_out", (a.B, a.D, a.K - 1), x.dtype))
-    _check(lib_.finc_causal_conv_forward(ctypes.byref(a), _stream()), "finc_causal_conv_forward")
+    B, D, L, K = _conv_dims(x, w)
+    dev, kind = _type(x)
+    _act(x, "x", dev, x.dtype, x.shape)
+    y = _out(out, x, "out", dev)
+    st = (B, D, K - 1)
+    a = CONV_ARGS.pack(kind, B, D, L, K, bool(silu), *_raster(x), *_raster(y),
+                       _param(w, "w", dev, (D, K)), _param(bias, "bias", dev, (D,)),
+                       _param(state, "state", dev, st, x.dtype),
+                       _param(state_out, "state_out", dev, st, x.dtype),
+                       _param(lengths, "lengths", dev, (B,), torch.int32))
+    _check(lib_.finc_causal_conv_forward(a, _stream()), "finc_causal_conv_forward")
     return y
 
 
@@ -1001,27 +1020,32 @@ def causal_conv_backward(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor,
     """(dx, dw, dbias, dstate) of causal_conv_forward for the gradients dy and
     dstate_out of its outputs; dbias and dstate are None without bias and state."""
     lib_ = _require_lib()
-    a = _conv_args(x, w, bias, silu, state, lengths)
-    B, D, L, K = a.B, a.D, a.L, a.K
-    _act(dy, "dy", x.shape, x.dtype)
-    _param(dstate_out, "dstate_out", (B, D, K - 1), x.dtype)
-    dx = _like(x) if dx is None else _act(dx, "dx", x.shape, x.dtype)
+    B, D, L, K = _conv_dims(x, w)
+    dev, kind = _type(x)
+    _act(x, "x", dev, x.dtype, x.shape)
+    _act(dy, "dy", dev, x.dtype, x.shape)
+    st = (B, D, K - 1)
+    a = CONV_ARGS.pack(kind, B, D, L, K, bool(silu), *_raster(x), *_NO_RASTER,
+                       _param(w, "w", dev, (D, K)), _param(bias, "bias", dev, (D,)),
+                       _param(state, "state", dev, st, x.dtype), 0,
+                       _param(lengths, "lengths", dev, (B,), torch.int32))
+    dx = _out(dx, x, "dx", dev)
     dw = torch.empty_like(w)
     dbias = None if bias is None else torch.empty_like(bias)
     dstate = None if state is None else torch.empty_like(state)
-    ws = _workspace(int(lib_.finc_causal_conv_workspace_bytes(B, D, L, K)), x.device, workspace)
-    g = ConvGrads(_raster(dy), _raster(dx), _ptr(dw), _ptr(dbias), _ptr(dstate_out), _ptr(dstate),
-                  _ptr(ws))
-    _check(lib_.finc_causal_conv_backward(ctypes.byref(a), ctypes.byref(g), _stream()),
-           "finc_causal_conv_backward")
+    ws = _space(workspace, lib_.finc_causal_conv_workspace_bytes(B, D, L, K), dev)
+    g = CONV_GRADS.pack(*_raster(dy), *_raster(dx), dw.data_ptr(),
+                        0 if dbias is None else dbias.data_ptr(),
+                        _param(dstate_out, "dstate_out", dev, st, x.dtype),
+                        0 if dstate is None else dstate.data_ptr(), ws.data_ptr())
+    _check(lib_.finc_causal_conv_backward(a, g, _stream()), "finc_causal_conv_backward")
     return dx, dw, dbias, dstate
 
 
-def _slots(slots, B, S):
-    _param(slots, "slots", (B,), torch.int32)
+def _slots(slots, dev, B, S):
     if slots is None and S < B:
         raise ValueError(f"state has {S} entries for {B} rows")
-    return slots
+    return _param(slots, "slots", dev, (B,), torch.int32)
 
 
 def causal_conv_step(x: torch.Tensor, w: torch.Tensor, state: torch.Tensor,
@@ -1031,49 +1055,51 @@ def causal_conv_step(x: torch.Tensor, w: torch.Tensor, state: torch.Tensor,
     slots[b] (or b) of state (S, D, K - 1), which takes the new one in place.  A
     slot outside [0, S) is an idle row (y 0)."""
     lib_ = _require_lib()
-    _act(x, "x")
-    if x.dim() != 2 or w.dim() != 2 or state.dim() != 3:
-        raise ValueError("x, w and state must be (B, D), (D, K) and (S, D, K - 1)")
-    B, D = x.shape
-    K, S = w.shape[1], state.shape[0]
-    _param(w, "w", (D, K))
-    _param(bias, "bias", (D,))
-    _param(state, "state", (S, D, K - 1), x.dtype)
-    _slots(slots, B, S)
-    y = _like(x) if out is None else _act(out, "out", x.shape, x.dtype)
-    _check(lib_.finc_causal_conv_step(_TYPES[x.dtype], _ptr(x), x.stride(0), _ptr(y), y.stride(0),
-                                      _ptr(w), _ptr(bias), _ptr(state), _ptr(slots), B, S, D, K,
-                                      int(silu), _stream()), "finc_causal_conv_step")
+    B, D = _dims(x, "x", "(B, D)")
+    K, S = _dims(w, "w", "(D, K)")[1], _dims(state, "state", "(S, D, K - 1)")[0]
+    dev, kind = _type(x)
+    _act(x, "x", dev, x.dtype, x.shape)
+    y = _out(out, x, "out", dev)
+    _check(lib_.finc_causal_conv_step(
+        kind, x.data_ptr(), x.stride(0), y.data_ptr(), y.stride(0), _param(w, "w", dev, (D, K)),
+        _param(bias, "bias", dev, (D,)), _param(state, "state", dev, (S, D, K - 1), x.dtype),
+        _slots(slots, dev, B, S), B, S, D, K, bool(silu), _stream()), "finc_causal_conv_step")
     return y
 
 
-def _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias, softplus, lengths):
-    if x.dim() != 3 or A.dim() != 2 or Bm.dim() != 4:
-        raise ValueError("x, A and Bm must be (B, D, L), (D, N) and (B, G, N, L)")
-    B, C, L = x.shape
-    N, G = A.shape[1], Bm.shape[1]
-    _act(x, "x")
-    _act(dt, "dt", x.shape, x.dtype)
-    _param(A, "A", (C, N))
-    _act(Bm, "Bm", (B, G, N, L), x.dtype)
-    _act(Cm, "Cm", (B, G, N, L), x.dtype)
-    if z is not None:
-        _act(z, "z", x.shape, x.dtype)
-    _param(D, "D", (C,))
-    _param(dt_bias, "dt_bias", (C,))
-    _param(lengths, "lengths", (B,), torch.int32)
+def _scan_counts(A, Bm, C):
+    """(states, groups)."""
+    N, G = _dims(A, "A", "(D, N)")[1], Bm.shape[1]
     if not 1 <= N <= MAX_STATE:
         raise ValueError(f"A has {N} states, expected 1 to {MAX_STATE}")
     if G < 1 or C % G:
         raise ValueError(f"{G} groups do not divide {C} channels")
-    return ScanArgs(_TYPES[x.dtype], B, C, L, N, G, int(softplus), _raster(x), _raster(dt),
-                    _raster(z), _raster(Bm), _raster(Cm), _raster(None), _ptr(A), _ptr(D),
-                    _ptr(dt_bias), None, None, None, _ptr(lengths))
+    return N, G
+
+
+def _scan_inputs(x, dt, A, Bm, Cm, D, z, dt_bias, softplus, lengths):
+    """(device, sizes, SCAN_ARGS' fields up to y, those after it up to dt_bias, lengths)."""
+    B, C, L = _dims(x, "x", "(B, D, L)")
+    _dims(Bm, "Bm", "(B, G, N, L)")
+    N, G = _scan_counts(A, Bm, C)
+    dev, kind = _type(x)
+    T, shape, shared = x.dtype, x.shape, (B, G, N, L)
+    _act(x, "x", dev, T, shape)
+    _act(dt, "dt", dev, T, shape)
+    _act(Bm, "Bm", dev, T, shared)
+    _act(Cm, "Cm", dev, T, shared)
+    if z is not None:
+        _act(z, "z", dev, T, shape)
+    head = (kind, B, C, L, N, G, bool(softplus), *_raster(x), *_raster(dt), *_raster(z),
+            *_raster(Bm), *_raster(Cm))
+    params = (_param(A, "A", dev, (C, N)), _param(D, "D", dev, (C,)),
+              _param(dt_bias, "dt_bias", dev, (C,)))
+    return dev, (B, C, L, N, G), head, params, _param(lengths, "lengths", dev, (B,), torch.int32)
 
 
 def selective_scan_states(B: int, D: int, L: int, N: int, device) -> torch.Tensor:
     """A buffer for the states that a forward keeps for its backward."""
-    n = int(_require_lib().finc_selective_scan_states_bytes(B, D, L, N))
+    n = _require_lib().finc_selective_scan_states_bytes(B, D, L, N)
     return torch.empty(max(n, 256) // 4, dtype=torch.float32, device=device)
 
 
@@ -1089,17 +1115,16 @@ def selective_scan_forward(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B
     state_out (B, D, N) is written if given, and may be state; states
     (selective_scan_states) is what selective_scan_backward reads."""
     lib_ = _require_lib()
-    a = _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias, softplus, lengths)
-    shape = (a.B, a.D, a.N)
-    a.state = _ptr(_param(state, "state", shape))
-    a.state_out = _ptr(_param(state_out, "state_out", shape))
-    y = _like(x) if out is None else _act(out, "out", x.shape, x.dtype)
-    a.y = _raster(y)
+    dev, (B, C, L, N, G), head, params, rows = _scan_inputs(x, dt, A, Bm, Cm, D, z, dt_bias,
+                                                            softplus, lengths)
+    y = _out(out, x, "out", dev)
+    keep = 0
     if states is not None:
-        n = int(lib_.finc_selective_scan_states_bytes(a.B, a.D, a.L, a.N))
-        a.states = _ptr(_bytes_buf(states, n, "states"))
-    _check(lib_.finc_selective_scan_forward(ctypes.byref(a), _stream()),
-           "finc_selective_scan_forward")
+        n = lib_.finc_selective_scan_states_bytes(B, C, L, N)
+        keep = _space(states, n, dev, "states").data_ptr()
+    a = SCAN_ARGS.pack(*head, *_raster(y), *params, _param(state, "state", dev, (B, C, N)),
+                       _param(state_out, "state_out", dev, (B, C, N)), keep, rows)
+    _check(lib_.finc_selective_scan_forward(a, _stream()), "finc_selective_scan_forward")
     return y
 
 
@@ -1116,28 +1141,26 @@ def selective_scan_backward(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, 
     gradients dy and dstate_out of its outputs: a dict of dx, ddt, dA, dB, dC, dD,
     dz, ddt_bias (None without D, z, dt_bias) and dstate."""
     lib_ = _require_lib()
-    a = _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias, softplus, lengths)
-    _act(dy, "dy", x.shape, x.dtype)
-    _param(dstate_out, "dstate_out", (a.B, a.D, a.N))
-    n = int(lib_.finc_selective_scan_states_bytes(a.B, a.D, a.L, a.N))
-    a.states = _ptr(_bytes_buf(states, n, "states"))
-    dx = _like(x) if dx is None else _act(dx, "dx", x.shape, x.dtype)
-    ddt = _like(x) if ddt is None else _act(ddt, "ddt", x.shape, x.dtype)
-    if z is None:
-        dz = None
-    else:
-        dz = _like(x) if dz is None else _act(dz, "dz", x.shape, x.dtype)
-    dB, dC = _like(Bm), _like(Cm)
+    dev, (B, C, L, N, G), head, params, rows = _scan_inputs(x, dt, A, Bm, Cm, D, z, dt_bias,
+                                                            softplus, lengths)
+    _act(dy, "dy", dev, x.dtype, x.shape)
+    n = lib_.finc_selective_scan_states_bytes(B, C, L, N)
+    keep = _space(states, n, dev, "states").data_ptr()
+    dx, ddt = _out(dx, x, "dx", dev), _out(ddt, x, "ddt", dev)
+    dz = None if z is None else _out(dz, x, "dz", dev)
+    dB, dC = _out(None, Bm, "dB", dev), _out(None, Cm, "dC", dev)
     dA = torch.empty_like(A)
     dD = None if D is None else torch.empty_like(D)
     db = None if dt_bias is None else torch.empty_like(dt_bias)
-    dstate = torch.empty(a.B, a.D, a.N, dtype=torch.float32, device=x.device)
-    ws = _workspace(int(lib_.finc_selective_scan_workspace_bytes(a.B, a.D, a.L, a.N, a.G)),
-                    x.device, workspace)
-    g = ScanGrads(_raster(dy), _raster(dx), _raster(ddt), _raster(dz), _raster(dB), _raster(dC),
-                  _ptr(dA), _ptr(dD), _ptr(db), _ptr(dstate_out), _ptr(dstate), _ptr(ws))
-    _check(lib_.finc_selective_scan_backward(ctypes.byref(a), ctypes.byref(g), _stream()),
-           "finc_selective_scan_backward")
+    dstate = torch.empty((B, C, N), dtype=torch.float32, device=x.device)
+    ws = _space(workspace, lib_.finc_selective_scan_workspace_bytes(B, C, L, N, G), dev)
+    a = SCAN_ARGS.pack(*head, *_NO_RASTER, *params, 0, 0, keep, rows)
+    g = SCAN_GRADS.pack(*_raster(dy), *_raster(dx), *_raster(ddt), *_raster(dz), *_raster(dB),
+                        *_raster(dC), dA.data_ptr(), 0 if dD is None else dD.data_ptr(),
+                        0 if db is None else db.data_ptr(),
+                        _param(dstate_out, "dstate_out", dev, (B, C, N)), dstate.data_ptr(),
+                        ws.data_ptr())
+    _check(lib_.finc_selective_scan_backward(a, g, _stream()), "finc_selective_scan_backward")
     return dict(dx=dx, ddt=ddt, dA=dA, dB=dB, dC=dC, dD=dD, dz=dz, ddt_bias=db, dstate=dstate)
 
 
@@ -1150,60 +1173,58 @@ def selective_scan_step(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, Bm: 
     state is entry slots[b] (or b) of state (S, D, N), updated in place.  A slot
     outside [0, S) is an idle row (y 0)."""
     lib_ = _require_lib()
-    if x.dim() != 2 or A.dim() != 2 or Bm.dim() != 3 or state.dim() != 3:
-        raise ValueError("x, A, Bm and state must be (B, D), (D, N), (B, G, N) and (S, D, N)")
-    B, C = x.shape
-    N, G, S = A.shape[1], Bm.shape[1], state.shape[0]
-    _act(x, "x")
-    _act(dt, "dt", x.shape, x.dtype)
-    _param(A, "A", (C, N))
+    B, C = _dims(x, "x", "(B, D)")
+    _dims(Bm, "Bm", "(B, G, N)")
+    N, G = _scan_counts(A, Bm, C)
+    S = _dims(state, "state", "(S, D, N)")[0]
+    dev, kind = _type(x)
+    T, shape = x.dtype, x.shape
+    _act(x, "x", dev, T, shape)
+    _act(dt, "dt", dev, T, shape)
+    zp = zs = 0
+    if z is not None:
+        zp, zs = _act(z, "z", dev, T, shape).data_ptr(), z.stride(0)
     for t, name in ((Bm, "Bm"), (Cm, "Cm")):
-        _act(t, name, (B, G, N), x.dtype)
+        _act(t, name, dev, T, (B, G, N))
         if G > 1 and t.stride(1) != N:
             raise ValueError(f"the groups of {name} must follow each other")
-    if z is not None:
-        _act(z, "z", x.shape, x.dtype)
-    _param(D, "D", (C,))
-    _param(dt_bias, "dt_bias", (C,))
-    _param(state, "state", (S, C, N))
-    _slots(slots, B, S)
-    if not 1 <= N <= MAX_STATE:
-        raise ValueError(f"A has {N} states, expected 1 to {MAX_STATE}")
-    if G < 1 or C % G:
-        raise ValueError(f"{G} groups do not divide {C} channels")
-    y = _like(x) if out is None else _act(out, "out", x.shape, x.dtype)
-    a = ScanStepArgs(_TYPES[x.dtype], B, S, C, N, G, int(softplus), _ptr(x), _ptr(dt), _ptr(z),
-                     _ptr(Bm), _ptr(Cm), x.stride(0), dt.stride(0),
-                     0 if z is None else z.stride(0), Bm.stride(0), Cm.stride(0), y.stride(0),
-                     _ptr(y), _ptr(A), _ptr(D), _ptr(dt_bias), _ptr(state), _ptr(slots))
-    _check(lib_.finc_selective_scan_step(ctypes.byref(a), _stream()), "finc_selective_scan_step")
+    y = _out(out, x, "out", dev)
+    a = SCAN_STEP_ARGS.pack(kind, B, S, C, N, G, bool(softplus), x.data_ptr(), dt.data_ptr(), zp,
+                            Bm.data_ptr(), Cm.data_ptr(), x.stride(0), dt.stride(0), zs,
+                            Bm.stride(0), Cm.stride(0), y.stride(0), y.data_ptr(),
+                            _param(A, "A", dev, (C, N)), _param(D, "D", dev, (C,)),
+                            _param(dt_bias, "dt_bias", dev, (C,)),
+                            _param(state, "state", dev, (S, C, N)), _slots(slots, dev, B, S))
+    _check(lib_.finc_selective_scan_step(a, _stream()), "finc_selective_scan_step")
     return y
 
 
-def _rows(t: torch.Tensor, name: str):
-    """(rows, step between them) of a (..., D) tensor whose rows lie evenly."""
-    if t.dim() < 1:
-        raise ValueError(f"{name} must have a last dimension")
-    M = 1
-    for n in t.shape[:-1]:
-        M *= n
-    step = t.shape[-1]
+def _rows(t: torch.Tensor, name: str) -> int:
+    """The step between the rows of a (..., D) tensor, which lie evenly."""
+    if t.is_contiguous():
+        return t.shape[-1]
     outer = [(n, st) for n, st in zip(t.shape[:-1], t.stride()[:-1]) if n != 1]
-    if outer and M > 0:
-        step = outer[-1][1]
-        for (n, st), (inner, ist) in zip(outer, outer[1:]):
-            if st != inner * ist:
-                raise ValueError(f"the rows of {name} must lie evenly")
-    return M, step
+    for (_, st), (n, inner) in zip(outer, outer[1:]):
+        if st != n * inner:
+            raise ValueError(f"the rows of {name} must lie evenly")
+    return outer[-1][1] if outer else t.shape[-1]
+
+
+def _row_dims(x, name="x"):
+    """(rows, columns) of a (..., D) tensor."""
+    if x.dim() < 1:
+        raise ValueError(f"{name} must have a last dimension")
+    D = x.shape[-1]
+    return (x.numel() // D if D else 0), D
 
 
 def _philox_args(p, seed, offset):
     if not 0.0 <= p < 1.0 or round(p * 65536) > 65535:
         raise ValueError(f"p is {p}, expected 0 <= p <= 65535 / 65536")
-    for v, name in ((seed, "seed"), (offset, "offset")):
-        if not 0 <= v < 1 << 64:
-            raise ValueError(f"{name} must be an unsigned 64-bit number")
-    return float(p), int(seed), int(offset)
+    if not 0 <= seed < 1 << 64:
+        raise ValueError("seed must be an unsigned 64-bit number")
+    if not 0 <= offset < 1 << 64:
+        raise ValueError("offset must be an unsigned 64-bit number")
 
 
 def dropout_counters(rows: int, D: int) -> int:
@@ -1217,24 +1238,24 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0,
     kept follows from seed, offset and the element's place alone (see finc_dropout),
     so the gradient is the same call on dy.  out may be x or residual."""
     lib_ = _require_lib()
-    _act(x, "x")
-    p, seed, offset = _philox_args(p, seed, offset)
-    y = _like(x) if out is None else _act(out, "out", x.shape, x.dtype)
-    M, sx = _rows(x, "x")
-    sr = 0
+    M, D = _row_dims(x)
+    dev, kind = _type(x)
+    _act(x, "x", dev, x.dtype, x.shape)
+    _philox_args(p, seed, offset)
+    y = _out(out, x, "out", dev)
+    rp = rs = 0
     if residual is not None:
-        sr = _rows(_act(residual, "residual", x.shape, x.dtype), "residual")[1]
-    _check(lib_.finc_dropout(_TYPES[x.dtype], _ptr(x), sx, _ptr(residual), sr, _ptr(y),
-                             _rows(y, "out")[1], M, x.shape[-1], p, seed, offset, _stream()),
-           "finc_dropout")
+        rp = _act(residual, "residual", dev, x.dtype, x.shape).data_ptr()
+        rs = _rows(residual, "residual")
+    _check(lib_.finc_dropout(kind, x.data_ptr(), _rows(x, "x"), rp, rs, y.data_ptr(),
+                             _rows(y, "out"), M, D, p, seed, offset, _stream()), "finc_dropout")
     return y
 
 
-def _residual_type(t, name, shape, dtype):
-    _act(t, name, shape)
-    if t.dtype not in (dtype, torch.float32):
-        raise ValueError(f"{name} must be {dtype} or float32")
-    return t
+def _residual_type(t, name, dtype):
+    if t.dtype != dtype and t.dtype != torch.float32:
+        raise ValueError(f"{name} must be {dtype} or float32, not {t.dtype}")
+    return t.dtype
 
 
 def add_norm_forward(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = None, *,
@@ -1247,37 +1268,39 @@ def add_norm_forward(x: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | 
     one); residual_out may be residual, and out x.  fp8: (q, scale, r) with y as
     float8_e4m3fn and a float32 scale a row (see finc_add_norm_forward)."""
     lib_ = _require_lib()
-    _act(x, "x")
-    p, seed, offset = _philox_args(p, seed, offset)
-    D = x.shape[-1]
-    _param(w, "w", (D,))
-    M, sx = _rows(x, "x")
+    M, D = _row_dims(x)
+    dev, kind = _type(x)
+    shape = x.shape
+    _act(x, "x", dev, x.dtype, shape)
+    _philox_args(p, seed, offset)
+    R, sp, ss = x.dtype, 0, 0
     if residual is not None:
-        _residual_type(residual, "residual", x.shape, x.dtype)
+        R = _residual_type(residual, "residual", x.dtype)
+        sp = _act(residual, "residual", dev, R, shape).data_ptr()
+        ss = _rows(residual, "residual")
+    elif residual_out is not None:
+        R = _residual_type(residual_out, "residual_out", x.dtype)
     if residual_out is None:
-        residual_out = torch.empty(x.shape, device=x.device,
-                                   dtype=x.dtype if residual is None else residual.dtype)
-    r = _residual_type(residual_out, "residual_out", x.shape, x.dtype)
-    if residual is not None and residual.dtype != r.dtype:
-        raise ValueError("residual_out must be of residual's type")
+        residual_out = torch.empty(shape, dtype=R, device=x.device)
+    r = _act(residual_out, "residual_out", dev, R, shape)
+    T, cp = x.dtype, 0
     if fp8:
-        if out is None:
-            out = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
-        elif not out.is_cuda or out.dtype != torch.float8_e4m3fn or out.shape != x.shape \
-                or (D > 1 and out.stride(-1) != 1):
-            raise ValueError("out must be a float8_e4m3fn device tensor of x's shape")
+        T = torch.float8_e4m3fn
         if scale is None:
-            scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-        _param(scale, "scale", x.shape[:-1])
+            scale = torch.empty(shape[:-1], dtype=torch.float32, device=x.device)
+        cp = _param(scale, "scale", dev, shape[:-1])
+    elif scale is not None:
+        raise ValueError("scale goes with fp8")
+    if out is None:
+        out = torch.empty(shape, dtype=T, device=x.device)
     else:
-        if scale is not None:
-            raise ValueError("scale goes with fp8")
-        out = _like(x) if out is None else _act(out, "out", x.shape, x.dtype)
-    a = NormArgs(_TYPES[x.dtype], _TYPES[r.dtype], M, D, _ptr(x), _ptr(residual), _ptr(out),
-                 _ptr(r), sx, 0 if residual is None else _rows(residual, "residual")[1],
-                 _rows(out, "out")[1], _rows(r, "residual_out")[1], _ptr(w), _ptr(scale),
-                 float(eps), p, seed, offset)
-    _check(lib_.finc_add_norm_forward(ctypes.byref(a), _stream()), "finc_add_norm_forward")
+        _act(out, "out", dev, T, shape)
+    a = NORM_ARGS.pack(kind, _TYPES[R], M, D, x.data_ptr(), sp, out.data_ptr(), r.data_ptr(),
+                       _rows(x, "x"), ss, _rows(out, "out"), _rows(r, "residual_out"),
+                       _param(w, "w", dev, (D,)), cp, eps, p, seed, offset)
+    # the ABI takes a scale's presence for the 8-bit output: an empty one has no address
+    if M > 0:
+        _check(lib_.finc_add_norm_forward(a, _stream()), "finc_add_norm_forward")
     return (out, scale, r) if fp8 else (out, r)
 
 
@@ -1290,31 +1313,34 @@ def add_norm_backward(dy: torch.Tensor, r: torch.Tensor, w: torch.Tensor,
     and dr (or None for 0) of r.  Without dropout and with one type dx and dresidual
     are the same values: one tensor, unless both are given."""
     lib_ = _require_lib()
-    _act(dy, "dy")
-    p, seed, offset = _philox_args(p, seed, offset)
-    D = dy.shape[-1]
-    _param(w, "w", (D,))
-    _residual_type(r, "r", dy.shape, dy.dtype)
-    M, sdy = _rows(dy, "dy")
+    M, D = _row_dims(dy, "dy")
+    dev, kind = _type(dy, "dy")
+    shape = dy.shape
+    _act(dy, "dy", dev, dy.dtype, shape)
+    _philox_args(p, seed, offset)
+    R = _residual_type(r, "r", dy.dtype)
+    _act(r, "r", dev, R, shape)
+    gp = gs = 0
     if dr is not None:
-        _act(dr, "dr", dy.shape, r.dtype)
-    if dx is not None:
-        _act(dx, "dx", dy.shape, dy.dtype)
-    if dresidual is not None:
-        _act(dresidual, "dresidual", dy.shape, r.dtype)
-    one = p == 0.0 and dy.dtype == r.dtype and (dx is None or dresidual is None)
-    if one:
-        dx = dresidual = _like(r) if dx is None and dresidual is None else (
-            dresidual if dx is None else dx)
+        gp, gs = _act(dr, "dr", dev, R, shape).data_ptr(), _rows(dr, "dr")
+    one = p == 0.0 and dy.dtype == R and (dx is None or dresidual is None)
+    xp = xs = rp = rs = 0
+    if one and dx is None:
+        dx = dresidual = _out(dresidual, r, "dresidual", dev)
+        rp, rs = dresidual.data_ptr(), _rows(dresidual, "dresidual")
     else:
-        dx = _like(dy) if dx is None else dx
-        dresidual = _like(r) if dresidual is None else dresidual
+        dx = _out(dx, dy, "dx", dev)
+        xp, xs = dx.data_ptr(), _rows(dx, "dx")
+        if one:
+            dresidual = dx
+        else:
+            dresidual = _out(dresidual, r, "dresidual", dev)
+            rp, rs = dresidual.data_ptr(), _rows(dresidual, "dresidual")
     dw = torch.empty_like(w)
-    ws = _workspace(int(lib_.finc_add_norm_workspace_bytes(M, D)), dy.device, workspace)
-    a = NormGradArgs(_TYPES[dy.dtype], _TYPES[r.dtype], M, D, _ptr(dy), _ptr(r), _ptr(dr),
-                     None if one else _ptr(dx), _ptr(dresidual), sdy, _rows(r, "r")[1],
-                     0 if dr is None else _rows(dr, "dr")[1], 0 if one else _rows(dx, "dx")[1],
-                     _rows(dresidual, "dresidual")[1], _ptr(w), _ptr(dw), float(eps), p, seed,
-                     offset, _ptr(ws))
-    _check(lib_.finc_add_norm_backward(ctypes.byref(a), _stream()), "finc_add_norm_backward")
+    ws = _space(workspace, lib_.finc_add_norm_workspace_bytes(M, D), dev)
+    a = NORM_GRAD_ARGS.pack(kind, _TYPES[R], M, D, dy.data_ptr(), r.data_ptr(), gp, xp,
+                            rp, _rows(dy, "dy"), _rows(r, "r"), gs, xs, rs,
+                            _param(w, "w", dev, (D,)), dw.data_ptr(), eps, p, seed, offset,
+                            ws.data_ptr())
+    _check(lib_.finc_add_norm_backward(a, _stream()), "finc_add_norm_backward")
     return dx, dresidual, dw

@@ -424,6 +424,16 @@ def test_norm_in_place():
     dy2, dr2 = dy.clone(), dr.clone()
     _, _, dw2 = finc.add_norm_backward(dy2, s, w, dr2, p=0.2, seed=3, dx=dy2, dresidual=dr2)
     assert torch.equal(dy2, dx) and torch.equal(dr2, dres) and torch.equal(dw2, dw)
+    # without dropout the two gradients are one tensor: over dy, over dr, or new
+    want, same, _ = finc.add_norm_backward(dy, s, w, dr)
+    assert want is same
+    dy3, dr3 = dy.clone(), dr.clone()
+    assert torch.equal(finc.add_norm_backward(dy3, s, w, dr, dx=dy3)[1], want)
+    assert torch.equal(finc.add_norm_backward(dy, s, w, dr3, dresidual=dr3)[0], want)
+    assert torch.equal(dy3, want) and torch.equal(dr3, want)
+    a, b, _ = finc.add_norm_backward(dy, s, w, dr, dx=torch.empty_like(dy),
+                                     dresidual=torch.empty_like(dy))
+    assert a is not b and torch.equal(a, want) and torch.equal(b, want)
 
 
 @pytest.mark.parametrize("M,D,kind", [(1, 5, F32), (40, 64, BF16), (9, 1000, BF16), (7, 2048, F16),
