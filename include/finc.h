@@ -537,7 +537,10 @@ int finc_conv1x1_inverse(const float *y, float *x, const float *Wm, int B, int C
  *    differ from each other.
  *  - Outputs overlapping inputs, the workspace or each other: FINC_EINVAL,
  *    except where a call names an alias it takes.
- *  - Deterministic: fixed summation orders, no atomics. */
+ *  - Deterministic: fixed summation orders, no atomics.  A row's outputs and the
+ *    gradients of its own inputs do not depend on the other rows or their number
+ *    (those of the parameters, sums over the batch, depend on it through their
+ *    fixed order, as do dBm and dCm, whose order over the channels it sets). */
 enum { FINC_F32 = 0, FINC_BF16 = 1, FINC_F16 = 2 };
 
 #define FINC_MAX_TAPS 8

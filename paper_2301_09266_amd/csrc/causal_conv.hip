@@ -20,6 +20,13 @@ constexpr int kThreads = 256;
 template <int K>
 constexpr int kHalo = K <= 1 ? 1 : K <= 2 ? 1 : K <= 3 ? 2 : K <= 5 ? 4 : 8;
 
+// Elements a thread takes: 16 bytes forward; twice that for the gradients, which
+// recompute K - 1 gradients beside them (8 x 2048 x 4096 in bf16, K 4: 113 us, and 132
+// with 16 bytes; 300 x 9000, where few threads are left, 11.2 and 9.4).
+constexpr int kTileBytes(bool back) { return back ? 32 : 16; }
+template <typename E, bool BACK>
+constexpr int kTile = kTileBytes(BACK) / (int)sizeof(E);
+
 struct ConvArgs {
     const void *x, *dy, *state, *dstate_out;
     void *y, *dx, *state_out, *dstate;
@@ -53,7 +60,7 @@ __device__ inline void load_before(const E *x, const E *state, int t0, float *v)
 
 template <typename E, int K, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_forward_kernel(ConvArgs a) {
-    constexpr int V = kPer16<E>, H = kHalo<K>;
+    constexpr int V = kTile<E, false>, H = kHalo<K>;
     const int tx = 1 << a.txl;
     const int rt = fdiv(blockIdx.x, a.div_t), tt = blockIdx.x - rt * a.tiles_t;
     const long long row = (long long)rt * (kThreads >> a.txl) + (threadIdx.x >> a.txl);
@@ -98,7 +105,7 @@ __global__ __launch_bounds__(kThreads) void conv_forward_kernel(ConvArgs a) {
 // sums for dw and dbias.
 template <typename E, int K, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
-    constexpr int V = kPer16<E>, H = kHalo<K>, Q = K - 1;
+    constexpr int V = kTile<E, true>, H = kHalo<K>, Q = K - 1;
     __shared__ float red[K + 1][kThreads / 64];
     const int tx = 1 << a.txl, ty = kThreads >> a.txl;
     const int d = blockIdx.x, lx = threadIdx.x & (tx - 1), ly = threadIdx.x >> a.txl;
@@ -130,12 +137,14 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
         load_upto<E, V>(dy + t0, a.L - t0, g);
         load_upto<E, H>(dy + t0 + V, a.L - t0 - V, g + V);
         // padding may hold anything, also to the left of a tile that lies in it
+        if (t0 + V + H > n) {
 #pragma unroll
-        for (int i = 0; i < H + V + H; ++i)
-            v[i] = keep_if(t0 - H + i < n, v[i]);
+            for (int i = 0; i < H + V + H; ++i)
+                v[i] = keep_if(t0 - H + i < n, v[i]);
 #pragma unroll
-        for (int i = 0; i < V + H; ++i)
-            g[i] = keep_if(t0 + i < n, g[i]);
+            for (int i = 0; i < V + H; ++i)
+                g[i] = keep_if(t0 + i < n, g[i]);
+        }
         if (SILU) {
 #pragma unroll
             for (int i = 0; i < V + Q; ++i) {
@@ -143,8 +152,12 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
 #pragma unroll
                 for (int j = 0; j < K; ++j)
                     p = __builtin_fmaf(w[j], v[H - Q + i + j], p);
-                g[i] = keep_if(t0 + i < n, g[i] * silu_grad(p, sigmoid(p)));
+                g[i] *= silu_grad(p, sigmoid(p));
             }
+            if (t0 + V + H > n)   // 0 times a gradient that has no value
+#pragma unroll
+                for (int i = 0; i < V + Q; ++i)
+                    g[i] = keep_if(t0 + i < n, g[i]);
         }
         float dx[V];
 #pragma unroll
@@ -159,12 +172,14 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
             for (int j = 0; j < K; ++j)
                 dw[j] = __builtin_fmaf(g[i], v[H - Q + i + j], dw[j]);
         }
+        if (t0 + V + Q > n) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int t = t0 + i;
-            if (dso && t < n && t + Q >= n)
-                dx[i] += (float)dso[t + Q - n];
-            dx[i] = keep_if(t < n, dx[i]);
+            for (int i = 0; i < V; ++i) {
+                const int t = t0 + i;
+                if (dso && t < n && t + Q >= n)
+                    dx[i] += (float)dso[t + Q - n];
+                dx[i] = keep_if(t < n, dx[i]);
+            }
         }
         store_upto<E, V>((E *)a.dx + (b * a.ob + d * a.od) + t0, a.L - t0, dx);
         if (t0 == 0 && a.dstate) {
@@ -309,7 +324,7 @@ void launch_taps(int K, const ConvArgs &c, dim3 grid, hipStream_t s) {
 }
 
 // The fields that both directions share; FINC_OK, or the error.
-int conv_common(const finc_conv_args *a, ConvArgs &c) {
+int conv_common(const finc_conv_args *a, bool back, ConvArgs &c) {
     c = ConvArgs{};
     c.x = a->x.p;
     c.xb = a->x.sb;
@@ -321,7 +336,7 @@ int conv_common(const finc_conv_args *a, ConvArgs &c) {
     c.B = a->B;
     c.D = a->D;
     c.L = a->L;
-    const Tiling t = tiling(a->L, 16 / type_size(a->type));
+    const Tiling t = tiling(a->L, kTileBytes(back) / type_size(a->type));
     c.txl = t.txl;
     if (t.along >= (1ll << 31))
         return FINC_EUNSUPPORTED;
@@ -357,7 +372,7 @@ int finc_causal_conv_forward(const finc_conv_args *a, hipStream_t stream) {
     if (a->B == 0)
         return FINC_OK;
     ConvArgs c;
-    const int rc = conv_common(a, c);
+    const int rc = conv_common(a, false, c);
     if (rc != FINC_OK)
         return rc;
     c.y = a->y.p;
@@ -409,7 +424,7 @@ int finc_causal_conv_backward(const finc_conv_args *a, const finc_conv_grads *g,
     if (!disjoint(in, out))
         return FINC_EINVAL;
     ConvArgs c;
-    const int rc = conv_common(a, c);
+    const int rc = conv_common(a, true, c);
     if (rc != FINC_OK)
         return rc;
     c.dy = g->dy.p;

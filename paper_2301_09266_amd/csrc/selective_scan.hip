@@ -18,7 +18,7 @@ namespace {
 
 using namespace finc_seq;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr float kLog2e = 1.44269504088896341f;
 
 struct Rows {
@@ -38,7 +38,6 @@ struct ScanArgs {
     const int *lengths;
     int B, D, L, N, G, Dg;   // Dg: channels of a group
     int softplus, parts;     // parts: that states are kept for, of the whole raster
-    int every;               // a forward's lanes between two of them
     int NP;                  // states that are kept: N with those that fill four rows
     int blocks;              // of channels, in a group
 };
@@ -101,14 +100,13 @@ __device__ inline int tile_at(int n, int j4, int lane) {
     return ((n * (T / 4) + j4) * 16 + lane) * 4;
 }
 
-// S states of a row's part: adds C h to y, and gives the states at the start of the
-// lane's run and at the part's end (in the row's last lane); `in` are the states
-// before the part.
+// S states of a row's part: adds C h to y, and gives the states at the part's end (in
+// the row's last lane); `in` are the states before the part.
 template <int T, int S>
 __device__ inline void scan_states(const float *tb, const float *tc, const int (&n)[S],
                                    const float (&A2)[S], const float (&in)[S], int lane,
                                    const float (&delta)[T], const float (&dx)[T], float sum,
-                                   float (&y)[T], float (&start)[S], float (&end)[S]) {
+                                   float (&y)[T], float (&end)[S]) {
     float a[S][T], b[S][T], m[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
@@ -131,7 +129,7 @@ __device__ inline void scan_states(const float *tb, const float *tc, const int (
 #pragma unroll
     for (int s = 0; s < S; ++s) {
         end[s] = __builtin_fmaf(m[s], in[s], end[s]);
-        float h = start[s] = neighbour<kFromLower>(in[s], end[s]);
+        float h = neighbour<kFromLower>(in[s], end[s]);
 #pragma unroll
         for (int j4 = 0; j4 < T / 4; ++j4) {
             const float4 v = *(const float4 *)(tc + tile_at<T>(n[s], j4, lane));
@@ -216,7 +214,10 @@ __device__ inline typename Vec<E, N>::type load_part(const E *p, int count) {
     return v;
 }
 // `whole`, that every lane has all of them, is the same in the whole wave: a branch of
-// some lanes would wait for the loads of the others, whose registers it fills.
+// some lanes would wait for the loads of the others, whose registers it fills.  For the
+// same reason what is loaded ahead is loaded in every round, the last one's place again
+// where nothing follows: a value that a round may leave as it was is copied, which
+// waits for it.
 template <typename E, int N>
 __device__ inline typename Vec<E, N>::type load_raw(const E *p, int count, bool whole) {
     return whole ? load_whole<E, N>(p) : load_part<E, N>(p, count);
@@ -246,153 +247,42 @@ __device__ inline void store_tile(float *tb, float *tc, int N, int u,
             make_float4((float)v[k], (float)v[k + 1], (float)v[k + 2], (float)v[k + 3]);
 }
 
-// What each forward kernel does with the states: read before the raster, kept for the
-// gradients every a.every lanes' runs, written after the row.
-__device__ inline float *kept_states(const ScanArgs &a, int b, int d, int part, int lane, int t0,
-                                     int n_pos) {
-    // a part that the row does not reach is not read either
-    if (!a.states || lane % a.every || t0 >= n_pos)
-        return nullptr;
-    return a.states + (((long long)b * a.D + d) * a.parts +
-                       (long long)part * (16 / a.every) + lane / a.every) * a.NP;
-}
-
-// Many channels: one block of 16 channels of one batch row and group, a row of lanes
-// for all the states of each.  The four rows of a wave read the same B and C.  The
-// next part's loads are under way while a part is computed.
+// The forward's tiles: two in LDS, and the loads of one more.  Up to K units a thread
+// are loaded ahead, which covers 16 states; the others are loaded as they are stored.
 template <typename E, int T>
-__global__ __launch_bounds__(kThreads, 2) void scan_channels_kernel(ScanArgs a) {
-    constexpr int CB = 16, P = 16 * T;       // P: positions of a part
-    constexpr int K = 4;                     // units of B and C loaded ahead
-    extern __shared__ __attribute__((aligned(16))) float lds[];
-    float *tb = lds, *tc = tb + a.N * P;
-    float *hs = tc + a.N * P;                // the states between parts, CB x N
-    float *As = hs + CB * a.N;               // A log2 e, CB x N
-    const int tid = threadIdx.x, lane = tid & 15, cl = tid >> 4;
-    int blk = blockIdx.x;
-    const int cb = blk % a.blocks;
-    blk /= a.blocks;
-    const int grp = blk % a.G, b = blk / a.G;
-    const bool live = cb * CB + cl < a.Dg;
-    const bool all = (cb + 1) * CB <= a.Dg;  // the block's channels are all there
-    const int d = grp * a.Dg + (live ? cb * CB + cl : 0);
-    const int n_pos = __builtin_amdgcn_readfirstlane(row_length(a.lengths, b, a.L));
-    const int units = 2 * a.N * (P / kUnit);
-    for (int i = tid; i < CB * a.N; i += kThreads) {
-        const int c = i / a.N, n = i - c * a.N, dd = cb * CB + c;
-        const bool ok = dd < a.Dg;
-        const long long at = (long long)(grp * a.Dg + (ok ? dd : 0)) * a.N + n;
-        As[i] = ok ? a.A[at] * kLog2e : 0.0f;
-        hs[i] = ok && a.state ? a.state[(long long)b * a.D * a.N + at] : 0.0f;
-    }
-    const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
-    const float skip = a.Dskip ? a.Dskip[d] : 0.0f;
-    const E *xr = a.x.row<const E>(b, d) + lane * T, *dr = a.dt.row<const E>(b, d) + lane * T;
-    const E *zr = a.z.p ? a.z.row<const E>(b, d) + lane * T : nullptr;
-    E *yr = a.y.row<E>(b, d) + lane * T;
-    const int own = live ? n_pos - lane * T : 0;
-    const int parts = (n_pos + P - 1) / P;
-    typename Vec<E, T>::type nx, nd, nz;
-    typename Vec<E, kUnit>::type nt[K];
-    if (parts > 0) {
-        nx = load_raw<E, T>(xr, own, all && P <= n_pos);
-        nd = load_raw<E, T>(dr, own, all && P <= n_pos);
+struct Tiles {
+    static constexpr int P = 16 * T, K = 2 * 16 * P / kUnit / kThreads > 0 ? 2 * 16 * P / kUnit / kThreads : 1;
+    const ScanArgs &a;
+    float *lds;
+    int b, grp, n_pos, units;
+    typename Vec<E, kUnit>::type ahead[K];
+    __device__ Tiles(const ScanArgs &a_, float *lds_, int b_, int grp_, int n_pos_)
+        : a(a_), lds(lds_), b(b_), grp(grp_), n_pos(n_pos_), units(2 * a_.N * (P / kUnit)) {}
+    __device__ float *of(int part) const { return lds + (part & 1) * 2 * a.N * P; }
+    __device__ void fetch(int part) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (tid + k * kThreads < units)
-                nt[k] = load_tile<E, T>(a, b, grp, tid + k * kThreads, 0, n_pos);
+            ahead[k] = load_tile<E, T>(a, b, grp, min((int)threadIdx.x + k * kThreads, units - 1),
+                                       part * P, n_pos);
     }
-    for (int part = 0; part < parts; ++part) {
-        const int p0 = part * P;
-        // positions past the row's length: delta 0 keeps the state, B and C are 0
+    // The part that was fetched.
+    __device__ void store(int part) {
+        float *tb = of(part), *tc = tb + a.N * P;
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (tid + k * kThreads < units)
-                store_tile<E, T>(tb, tc, a.N, tid + k * kThreads, nt[k]);
-        for (int u = tid + K * kThreads; u < units; u += kThreads)
-            store_tile<E, T>(tb, tc, a.N, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
-        float x[T], delta[T], dx[T], y[T], sum = 0.0f;
-#pragma unroll
-        for (int j = 0; j < T; ++j) {
-            x[j] = (float)nx[j];
-            float v = (float)nd[j] + bias;
-            if (a.softplus)
-                v = softplus(v);
-            delta[j] = keep_if(j < own - p0, v);
-            dx[j] = delta[j] * x[j];
-            sum += delta[j];
-            y[j] = 0.0f;
-        }
-        __syncthreads();
-        // under way until the part is done
-        if (zr)
-            nz = load_raw<E, T>(zr + p0, own - p0, all && p0 + P <= n_pos);
-        if (part + 1 < parts) {
-            const bool whole = all && p0 + 2 * P <= n_pos;
-            nx = load_raw<E, T>(xr + p0 + P, own - p0 - P, whole);
-            nd = load_raw<E, T>(dr + p0 + P, own - p0 - P, whole);
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (tid + k * kThreads < units)
-                    nt[k] = load_tile<E, T>(a, b, grp, tid + k * kThreads, p0 + P, n_pos);
-        }
-        float *kept = live ? kept_states(a, b, d, part, lane, p0 + lane * T, n_pos) : nullptr;
-        float *hr = hs + cl * a.N;
-        const float *Ar = As + cl * a.N;
-        int i = 0;
-        for (; i + 1 < a.N; i += 2) {
-            const int n[2] = {i, i + 1};
-            const float A2[2] = {Ar[i], Ar[i + 1]}, in[2] = {hr[i], hr[i + 1]};
-            float start[2], end[2];
-            scan_states<T, 2>(tb, tc, n, A2, in, lane, delta, dx, sum, y, start, end);
-            if (kept) {
-                kept[i] = start[0];
-                kept[i + 1] = start[1];
-            }
-            if (lane == 15) {
-                hr[i] = end[0];
-                hr[i + 1] = end[1];
-            }
-        }
-        if (i < a.N) {
-            const int n[1] = {i};
-            const float A2[1] = {Ar[i]}, in[1] = {hr[i]};
-            float start[1], end[1];
-            scan_states<T, 1>(tb, tc, n, A2, in, lane, delta, dx, sum, y, start, end);
-            if (kept)
-                kept[i] = start[0];
-            if (lane == 15)
-                hr[i] = end[0];
-        }
-        if (live) {
-#pragma unroll
-            for (int j = 0; j < T; ++j) {
-                float v = __builtin_fmaf(skip, x[j], y[j]);
-                if (zr)
-                    v *= silu((float)nz[j]);
-                y[j] = keep_if(j < own - p0, v);
-            }
-            store_upto<E, T>(yr + p0, a.L - p0 - lane * T, y);
-        }
-        // the next part's tile takes the place of this one's
-        __syncthreads();
+            if ((int)threadIdx.x + k * kThreads < units)
+                store_tile<E, T>(tb, tc, a.N, threadIdx.x + k * kThreads, ahead[k]);
+        for (int u = threadIdx.x + K * kThreads; u < units; u += kThreads)
+            store_tile<E, T>(tb, tc, a.N, u, load_tile<E, T>(a, b, grp, u, part * P, n_pos));
     }
-    // padding
-    for (int c = 0; c < CB; ++c) {
-        const int dd = cb * CB + c;
-        if (dd >= a.Dg)
-            break;
-        E *r = a.y.row<E>(b, grp * a.Dg + dd);
-        for (long long t = (long long)parts * P + tid; t < a.L; t += kThreads)
-            r[t] = (E)0.0f;
-    }
-    __syncthreads();
-    if (a.state_out)
-        for (int i = tid; i < CB * a.N; i += kThreads) {
-            const int c = i / a.N, n = i - c * a.N, dd = cb * CB + c;
-            if (dd < a.Dg)
-                a.state_out[((long long)b * a.D + grp * a.Dg + dd) * a.N + n] = hs[i];
-        }
+};
+
+// The states at a part's start, kept for the gradients: those of one channel, by its
+// wave, before it goes on from them.
+__device__ inline void keep_states(const ScanArgs &a, int b, int d, int part, const float *hs,
+                                   int lane64) {
+    if (lane64 < a.N)
+        a.states[(((long long)b * a.D + d) * a.parts + part) * a.NP + lane64] = hs[lane64];
 }
 
 // The sums over the four rows of T values a lane: row r gets those of positions
@@ -418,18 +308,17 @@ __device__ inline void sum_rows(const float (&v)[T], float (&out)[T / 4]) {
         out[j] = swap16(u[j], u[j + T / 4]);
 }
 
-// Few channels: a wave for a channel, whose four rows of lanes share the states (state
-// n in row n % 4) over the same positions.  Each row prepares a quarter of them and
-// hands them to the others through LDS; the sums over the states are sums over the
-// rows, and come back to the row that prepared the position.  The block's four waves
-// share the tile of B and C.
+// A wave for a channel: its four rows of lanes share the states (state n in row n % 4)
+// over the same positions.  Each row prepares a quarter of them and hands them to the
+// others through LDS; the sums over the states are sums over the rows, and come back
+// to the row that prepared the position.  The block's waves share the tiles of B and
+// C; the next part's tile is stored, and the one after it is under way, while a part
+// is computed.
 template <typename E, int T>
-__global__ __launch_bounds__(kThreads, 2) void scan_rows_kernel(ScanArgs a) {
-    constexpr int CB = 4, P = 16 * T, I = T / 4;
-    constexpr int K = 4;                     // units of B and C loaded ahead
+__global__ __launch_bounds__(kThreads, 4) void scan_forward_kernel(ScanArgs a) {
+    constexpr int CB = kThreads / 64, P = 16 * T, I = T / 4;
     extern __shared__ __attribute__((aligned(16))) float lds[];
-    float *tb = lds, *tc = tb + a.N * P;
-    float *hs = tc + a.N * P;                // the states between parts, CB x N
+    float *hs = lds + 4 * a.N * P;           // the states between parts, CB x N
     float *As = hs + CB * a.N;               // A log2 e, CB x N
     float *pre = As + CB * a.N;              // delta, delta x of every wave's channel
     const int tid = threadIdx.x, lane = tid & 15, rowi = (tid >> 4) & 3;
@@ -441,7 +330,6 @@ __global__ __launch_bounds__(kThreads, 2) void scan_rows_kernel(ScanArgs a) {
     const bool live = cb * CB + wave < a.Dg;
     const int d = grp * a.Dg + (live ? cb * CB + wave : 0);
     const int n_pos = __builtin_amdgcn_readfirstlane(row_length(a.lengths, b, a.L));
-    const int units = 2 * a.N * (P / kUnit);
     for (int i = tid; i < CB * a.N; i += kThreads) {
         const int c = i / a.N, n = i - c * a.N, dd = cb * CB + c;
         const bool ok = dd < a.Dg;
@@ -455,7 +343,7 @@ __global__ __launch_bounds__(kThreads, 2) void scan_rows_kernel(ScanArgs a) {
     float *mine = pre + wave * 2 * P;
     const int parts = (n_pos + P - 1) / P;
     typename Vec<E, I>::type nx, nd, nz;
-    typename Vec<E, kUnit>::type nt[K];
+    Tiles<E, T> tiles(a, lds, b, grp, n_pos);
     auto fetch = [&](int p0) {
         const E *xr = a.x.row<const E>(b, d) + p0, *dr = a.dt.row<const E>(b, d) + p0;
         const E *zr = a.z.p ? a.z.row<const E>(b, d) + p0 : xr;
@@ -469,22 +357,19 @@ __global__ __launch_bounds__(kThreads, 2) void scan_rows_kernel(ScanArgs a) {
             nd = load_part<E, I>(at(dr, pos), left);
             nz = load_part<E, I>(at(zr, pos), left);
         }
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (tid + k * kThreads < units)
-                nt[k] = load_tile<E, T>(a, b, grp, tid + k * kThreads, p0, n_pos);
     };
-    if (parts > 0)
+    if (parts > 0) {
         fetch(0);
+        tiles.fetch(0);
+        tiles.store(0);
+        tiles.fetch(parts > 1);
+    }
+    __syncthreads();
     for (int part = 0; part < parts; ++part) {
         const int p0 = part * P, left = n_pos - p0 - pos;
-        // positions past the row's length: delta 0 keeps the state, B and C are 0
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (tid + k * kThreads < units)
-                store_tile<E, T>(tb, tc, a.N, tid + k * kThreads, nt[k]);
-        for (int u = tid + K * kThreads; u < units; u += kThreads)
-            store_tile<E, T>(tb, tc, a.N, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
+        const float *tb = tiles.of(part), *tc = tb + a.N * P;
+        if (part + 1 < parts)
+            tiles.store(part + 1);
         float x[I], z[I], delta[T], dx[T], y[T], sum = 0.0f;
         float *q = mine + slot_at<T>(pos);   // I neighbours of one slot
 #pragma unroll
@@ -498,10 +383,10 @@ __global__ __launch_bounds__(kThreads, 2) void scan_rows_kernel(ScanArgs a) {
             q[i] = v;
             q[P + i] = v * x[i];
         }
-        __syncthreads();
         // under way until the part is done
-        if (part + 1 < parts)
-            fetch(p0 + P);
+        fetch(part + 1 < parts ? p0 + P : p0);
+        tiles.fetch(min(part + 2, parts - 1));
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int j = 0; j < T; j += 4) {
             lds_load<4>(mine + (j * 4 + lane) * 4, delta + j);
@@ -512,19 +397,17 @@ __global__ __launch_bounds__(kThreads, 2) void scan_rows_kernel(ScanArgs a) {
             sum += delta[j];
             y[j] = 0.0f;
         }
-        float *kept = live ? kept_states(a, b, d, part, lane, p0 + lane * T, n_pos) : nullptr;
+        __builtin_amdgcn_wave_barrier();
+        if (a.states && live)
+            keep_states(a, b, d, part, hs + wave * a.N, tid & 63);
         float *hr = hs + wave * a.N;
         const float *Ar = As + wave * a.N;
         int i = rowi;
         for (int k = a.N / 8; k; --k, i += 8) {
             const int n[2] = {i, i + 4};
             const float A2[2] = {Ar[i], Ar[i + 4]}, in[2] = {hr[i], hr[i + 4]};
-            float start[2], end[2];
-            scan_states<T, 2>(tb, tc, n, A2, in, lane, delta, dx, sum, y, start, end);
-            if (kept) {
-                kept[i] = start[0];
-                kept[i + 4] = start[1];
-            }
+            float end[2];
+            scan_states<T, 2>(tb, tc, n, A2, in, lane, delta, dx, sum, y, end);
             if (lane == 15) {
                 hr[i] = end[0];
                 hr[i + 4] = end[1];
@@ -535,18 +418,16 @@ __global__ __launch_bounds__(kThreads, 2) void scan_rows_kernel(ScanArgs a) {
             const bool has = i < a.N;
             const int n[1] = {has ? i : 0};
             const float A2[1] = {has ? Ar[i] : 0.0f}, in[1] = {has ? hr[i] : 0.0f};
-            float start[1], end[1], more[T], part_dx[T];
+            float end[1], more[T], part_dx[T];
 #pragma unroll
             for (int j = 0; j < T; ++j) {
                 more[j] = 0.0f;
                 part_dx[j] = keep_if(has, dx[j]);
             }
-            scan_states<T, 1>(tb, tc, n, A2, in, lane, delta, part_dx, sum, more, start, end);
+            scan_states<T, 1>(tb, tc, n, A2, in, lane, delta, part_dx, sum, more, end);
 #pragma unroll
             for (int j = 0; j < T; ++j)
                 y[j] += keep_if(has, more[j]);
-            if (kept && has)
-                kept[i] = start[0];
             if (lane == 15 && has)
                 hr[i] = end[0];
         }
@@ -566,7 +447,7 @@ __global__ __launch_bounds__(kThreads, 2) void scan_rows_kernel(ScanArgs a) {
             else
                 store_upto<E, I>(at(yr, pos), a.L - p0 - pos, v);
         }
-        // the next part's tile takes the place of this one's
+        // the next part's tile is there, and this one's place free
         __syncthreads();
     }
     // padding
@@ -706,8 +587,7 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
     if (parts > 0) {
         if (wave < count)
             fetch(wave, parts - 1);
-        if (tid < units)
-            nt = load_tile<E, T>(a, b, grp, tid, (parts - 1) * P, n_pos);
+        nt = load_tile<E, T>(a, b, grp, min(tid, units - 1), (parts - 1) * P, n_pos);
     }
     for (int part = parts - 1; part >= 0; --part) {
         const int p0 = part * P;
@@ -716,8 +596,7 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
         for (int u = tid + TH; u < units; u += TH)
             store_tile<E, T>(tb, tc, a.N, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
         __syncthreads();
-        if (part > 0 && tid < units)
-            nt = load_tile<E, T>(a, b, grp, tid, p0 - P, n_pos);
+        nt = load_tile<E, T>(a, b, grp, min(tid, units - 1), max(p0 - P, 0), n_pos);
         float dB[S][T], dC[S][T];
 #pragma unroll
         for (int s = 0; s < S; ++s)
@@ -746,13 +625,14 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
             lds_load<S>(As + c * NP + n0, A2);
             lds_load<S>(own, end);
 #pragma unroll
-            for (int s = 0; s < S; ++s)
+            for (int s = 0; s < S; ++s) {
                 in[s] = n0 + s < a.N ? nin[s] : 0.0f;
+                // before the next loads: behind them it would wait for them
+                asm volatile("" : "+v"(in[s]));
+            }
             // the next channel's, under way
-            if (c + kGradWaves < count)
-                fetch(c + kGradWaves, part);
-            else if (part > 0)
-                fetch(wave, part - 1);
+            const bool more = c + kGradWaves < count;
+            fetch(more ? c + kGradWaves : wave, more ? part : max(part - 1, 0));
             __builtin_amdgcn_wave_barrier();
             float de[T], dx[T], g[T], gB[T], sA[T], yv[T], sum = 0.0f;
 #pragma unroll
@@ -1001,11 +881,13 @@ struct StepArgs {
     int B, S, D, N, G, Dg, softplus;
 };
 
+constexpr int kStepThreads = 256;
+
 // Q lanes a channel, four states each at a time.
 template <typename E, int Q>
-__global__ __launch_bounds__(kThreads) void scan_step_kernel(StepArgs a) {
+__global__ __launch_bounds__(kStepThreads) void scan_step_kernel(StepArgs a) {
     const int q = threadIdx.x % Q;
-    const long long d0 = (long long)blockIdx.x * (kThreads / Q) + threadIdx.x / Q;
+    const long long d0 = (long long)blockIdx.x * (kStepThreads / Q) + threadIdx.x / Q;
     const bool live = d0 < a.D;
     const int d = live ? (int)d0 : 0, grp = d / a.Dg;
     for (int b = blockIdx.y; b < a.B; b += gridDim.y) {
@@ -1071,22 +953,21 @@ inline long long part_count(int L, int N) {
     return cdivll(L > 0 ? L : 1, 16 * lane_positions(L, N));
 }
 
-template <typename E, int T, bool ROWS>
+template <typename E, int T>
 int launch_forward(ScanArgs &c, hipStream_t s) {
-    constexpr int CB = ROWS ? 4 : 16;
+    constexpr int CB = kThreads / 64;
     c.blocks = (int)cdivll(c.Dg, CB);
-    c.every = lane_positions(c.L, c.N) * 16 / T;
     const long long grid = (long long)c.blocks * c.G * c.B;
     const size_t lds =
-        ((size_t)2 * c.N * 16 * T + 2 * CB * c.N + (ROWS ? 4 * 2 * 16 * T : 0)) * sizeof(float);
-    const auto kernel = ROWS ? scan_rows_kernel<E, T> : scan_channels_kernel<E, T>;
+        ((size_t)4 * c.N * 16 * T + 2 * CB * c.N + CB * 2 * 16 * T) * sizeof(float);
     if (grid >= (1ll << 31) || lds > (size_t)kLds)
         return FINC_EUNSUPPORTED;
     if (lds > 64 * 1024)
-        (void)hipFuncSetAttribute((const void *)kernel,
+        (void)hipFuncSetAttribute((const void *)scan_forward_kernel<E, T>,
                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     (void)hipGetLastError();   // the launch check decides
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), (unsigned)lds, s, c);
+    hipLaunchKernelGGL((scan_forward_kernel<E, T>), dim3((unsigned)grid), dim3(kThreads),
+                       (unsigned)lds, s, c);
     return launched();
 }
 
@@ -1200,24 +1081,10 @@ int finc_selective_scan_forward(const finc_scan_args *a, hipStream_t stream) {
     c.state = a->state;
     c.state_out = a->state_out;
     int rc = FINC_EINVAL;
-    // A wave for a channel up to 8192 of them, a row of lanes from there on, where the
-    // rows of a wave share their reads of B and C and nothing is handed over: 2048 x
-    // 4096 positions at batch 4 take 230 us by waves and 180 by rows, 6000 channels x
-    // 1531 positions 32 us by waves and 71 by rows (too few of them).  Sixteen
-    // positions a lane halve the scans over lanes and the barriers, but their
-    // registers leave two waves a SIMD: where no more are there (2048 x 4096
-    // positions: 71 us against 82 with eight; 6000 x 1531: 42 against 32).
-    const long long channels = (long long)B * D;
-    const bool sixteen = L > 128 && a->N <= 32 && channels <= 2048;
     with_type(a->type, [&](auto e) {
         typedef decltype(e) E;
-        if (channels < 8192)
-            rc = L <= 64   ? launch_forward<E, 4, true>(c, stream)
-                 : sixteen ? launch_forward<E, 16, true>(c, stream)
-                           : launch_forward<E, 8, true>(c, stream);
-        else
-            rc = L <= 64 ? launch_forward<E, 4, false>(c, stream)
-                         : launch_forward<E, 8, false>(c, stream);
+        rc = lane_positions(L, a->N) == 4 ? launch_forward<E, 4>(c, stream)
+                                          : launch_forward<E, 8>(c, stream);
     });
     return rc;
 }
@@ -1326,11 +1193,11 @@ int finc_selective_scan_step(const finc_scan_step_args *a, hipStream_t stream) {
         typedef decltype(e) E;
         const unsigned gy = (unsigned)(B < 32768 ? B : 32768);
         if (a->N <= 4)
-            hipLaunchKernelGGL((scan_step_kernel<E, 1>), dim3((unsigned)cdivll(D, kThreads), gy),
-                               dim3(kThreads), 0, stream, c);
+            hipLaunchKernelGGL((scan_step_kernel<E, 1>), dim3((unsigned)cdivll(D, kStepThreads), gy),
+                               dim3(kStepThreads), 0, stream, c);
         else
             hipLaunchKernelGGL((scan_step_kernel<E, 4>),
-                               dim3((unsigned)cdivll(D, kThreads / 4), gy), dim3(kThreads), 0,
+                               dim3((unsigned)cdivll(D, kStepThreads / 4), gy), dim3(kStepThreads), 0,
                                stream, c);
     });
     return launched();

@@ -105,18 +105,12 @@ __device__ inline float sigmoid(float v) {
     // 1 / (1 + inf) = 0 on the left, 1 / (1 + 0) = 1 on the right
     return __builtin_amdgcn_rcpf(1.0f + exp_fast(-v));
 }
-// v, at most 1e30 from 0 (NaN stays): an infinite v times a sigmoid of 0 has no value.
-__device__ inline float finite(float v) {
-    v = v < -1e30f ? -1e30f : v;
-    return v > 1e30f ? 1e30f : v;
-}
-__device__ inline float silu(float v) {
-    const float sg = sigmoid(v);
-    return (v < -1e30f ? -1e30f : v) * sg;
-}
+// An infinite v times a sigmoid of 0 has no value: v stays within 1e30 of 0.  (The
+// maximum and the median drop NaN, which the sigmoid brings back.)
+__device__ inline float silu(float v) { return __builtin_fmaxf(v, -1e30f) * sigmoid(v); }
 // d silu / dv, with sg = sigmoid(v).
 __device__ inline float silu_grad(float v, float sg) {
-    return sg * __builtin_fmaf(finite(v), 1.0f - sg, 1.0f);
+    return sg * __builtin_fmaf(__builtin_amdgcn_fmed3f(v, -1e30f, 1e30f), 1.0f - sg, 1.0f);
 }
 // v, or 0: a mask of bits, so that what v takes to compute gets no branch.
 __device__ inline float keep_if(bool ok, float v) {

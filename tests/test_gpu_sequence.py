@@ -349,6 +349,20 @@ def test_scan_rows_do_not_depend_on_the_batch():
     assert torch.equal(one[0], whole[2])
 
 
+def test_scan_bits_do_not_depend_on_the_number_of_rows():
+    """One row alone and among enough rows to fill the card, states kept or not."""
+    t, _, _ = scan_inputs(1, 520, 200, 16, 2, "gsdbp", BF16, 10)
+    g, kw = scan_kw(t, None, "gsdbp", None)
+    one = finc.selective_scan_forward(**g, **kw)
+    wide = {k: v.expand(40, *v.shape[1:]) if k in ("x", "dt", "Bm", "Cm", "z") else v
+            for k, v in g.items()}
+    many = dict(kw, state=kw["state"].expand(40, 520, 16).contiguous())
+    got = finc.selective_scan_forward(**wide, **many)
+    assert torch.equal(got, one.expand_as(got))
+    states = finc.selective_scan_states(1, 520, 200, 16, DEV)
+    assert torch.equal(finc.selective_scan_forward(**g, **kw, states=states), one)
+
+
 # ---- norm ------------------------------------------------------------------------
 
 NORM = [  # M, D, residual, type, rtype, p
