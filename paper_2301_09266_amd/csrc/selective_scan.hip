@@ -489,13 +489,13 @@ struct GradArgs {
 
 constexpr int kGradWaves = 8;
 
-// States a lane whose gradients the waves exchange at once.
-template <int T>
-constexpr int kSwap = 32 / T;
+// Floats of LDS through which the waves add their gradients of B and C: eight units of
+// four values a lane from each.
+constexpr int kSwap = kGradWaves * kGradWaves * 64 * 4;
 
 inline size_t backward_lds(int NP, int T, int set) {
     return ((size_t)2 * NP * 16 * T + kGradWaves * 3 * 16 * T + (size_t)3 * set * NP +
-            (size_t)10 * set + (size_t)2 * 32 * 64 * (kGradWaves / 2)) * 4;
+            (size_t)10 * set + kSwap) * 4;
 }
 
 // The sums over a row's lanes of four values: that of value s in lanes 4 s to 4 s + 3.
@@ -516,14 +516,14 @@ __device__ inline float row_sum4(float v0, float v1, float v2, float v3, int lan
 
 template <typename E, int T, int S>
 __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs ga) {
-    constexpr int P = 16 * T, I = T / 4, TH = 64 * kGradWaves, SW = S < kSwap<T> ? S : kSwap<T>;
+    constexpr int P = 16 * T, I = T / 4, TH = 64 * kGradWaves;
     constexpr int NP = 4 * S;                      // states with those that fill the rows
     const ScanArgs &a = ga.f;
     extern __shared__ __attribute__((aligned(16))) float lds[];
     float *tb = lds, *tc = tb + NP * P;
     float *pre = tc + NP * P;                      // delta, delta x, dy of a wave's channel
-    float *swp = pre + kGradWaves * 3 * P;         // half the waves' gradients of B and C
-    float *carry = swp + 2 * 32 * 64 * (kGradWaves / 2);   // G at the part's end, set x NP
+    float *swp = pre + kGradWaves * 3 * P;         // the waves' gradients of B and C
+    float *carry = swp + kSwap;                    // G at the part's end, set x NP
     float *As = carry + ga.set * NP;               // A log2 e
     float *dAs = As + ga.set * NP;                 // dA
     float *ps = dAs + ga.set * NP;                 // dDskip, ddt_bias by rows: set x 4 x 2
@@ -740,53 +740,43 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
             if ((lane & 3) == 0 && lane < 8)
                 ps[(c * 4 + rowi) * 2 + (lane >> 2)] += u;
         }
-        // dB and dC of the part: the upper half of the waves to the lower, by halves
+        // dB and dC of the part: four values a lane at a time, eight such units in LDS from
+        // every wave, of which each wave adds one over the waves, in their order
+        const long long rows = (long long)a.G * a.N;
 #pragma unroll
-        for (int s0 = 0; s0 < S; s0 += SW) {
+        for (int u0 = 0; u0 < S * T / 4; u0 += kGradWaves) {
+            constexpr int U = S * T / 4 < kGradWaves ? S * T / 4 : kGradWaves;
 #pragma unroll
-            for (int half = kGradWaves / 2; half; half >>= 1) {
-                float *q = swp + (wave & (half - 1)) * 2 * SW * T * 64 + (tid & 63) * 4;
-                if (wave >= half && wave < 2 * half)
+            for (int which = 0; which < 2; ++which) {
+                float4 *q = (float4 *)swp + (tid & 63);
 #pragma unroll
-                    for (int k = 0; k < SW * T / 4; ++k) {
-                        const int s = s0 + 4 * k / T, j = 4 * k % T;
-                        *(float4 *)(q + 2 * k * 256) =
-                            make_float4(dB[s][j], dB[s][j + 1], dB[s][j + 2], dB[s][j + 3]);
-                        *(float4 *)(q + (2 * k + 1) * 256) =
-                            make_float4(dC[s][j], dC[s][j + 1], dC[s][j + 2], dC[s][j + 3]);
-                    }
+                for (int u = 0; u < U; ++u) {
+                    const int s = 4 * (u0 + u) / T, j = 4 * (u0 + u) % T;
+                    const float *v = which ? &dC[s][j] : &dB[s][j];
+                    q[(wave * U + u) * 64] = make_float4(v[0], v[1], v[2], v[3]);
+                }
                 __syncthreads();
-                if (wave < half)
+                if (wave < U) {
+                    float4 sum = q[wave * 64];
 #pragma unroll
-                    for (int k = 0; k < SW * T / 4; ++k) {
-                        const int s = s0 + 4 * k / T, j = 4 * k % T;
-                        const float4 u = *(const float4 *)(q + 2 * k * 256);
-                        const float4 v = *(const float4 *)(q + (2 * k + 1) * 256);
-                        dB[s][j] += u.x;
-                        dB[s][j + 1] += u.y;
-                        dB[s][j + 2] += u.z;
-                        dB[s][j + 3] += u.w;
-                        dC[s][j] += v.x;
-                        dC[s][j + 1] += v.y;
-                        dC[s][j + 2] += v.z;
-                        dC[s][j + 3] += v.w;
+                    for (int k = 1; k < kGradWaves; ++k) {
+                        const float4 v = q[(k * U + wave) * 64];
+                        sum.x += v.x;
+                        sum.y += v.y;
+                        sum.z += v.z;
+                        sum.w += v.w;
                     }
+                    const int n = n0 + 4 * (u0 + wave) / T;
+                    const int t0 = p0 + lane * T + 4 * (u0 + wave) % T;
+                    if (n < a.N) {
+                        const long long r = (((long long)which * ga.sets + set) * a.B + b) * rows +
+                                            (long long)grp * a.N + n;
+                        const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+                        store_upto<float, 4>(ga.shared + r * a.L + t0, a.L - t0, v);
+                    }
+                }
                 __syncthreads();
             }
-        }
-        if (wave == 0) {
-            const long long rows = (long long)a.G * a.N;
-            const int t0 = p0 + lane * T;
-#pragma unroll
-            for (int s = 0; s < S; ++s)
-                if (n0 + s < a.N) {
-                    const long long r =
-                        ((long long)set * a.B + b) * rows + (long long)grp * a.N + n0 + s;
-                    store_upto<float, T>(ga.shared + r * a.L + t0, a.L - t0, dB[s]);
-                    store_upto<float, T>(ga.shared + ((long long)ga.sets * a.B * rows + r) * a.L +
-                                             t0,
-                                         a.L - t0, dC[s]);
-                }
         }
     }
     __syncthreads();
