@@ -101,11 +101,9 @@ __device__ inline unsigned all_lanes(unsigned v, unsigned *lds, int &turn_of) {
     if ((threadIdx.x & 63) == 0)
         buf[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = buf[0];
-#pragma unroll
-    for (int i = 1; i < R / 64; ++i)
-        v = Op::of(v, buf[i]);
-    return v;
+    // a wave's result in every row of lanes, 0 past the last wave
+    const int i = threadIdx.x & 15;
+    return all16<Op>(i < R / 64 ? buf[i] : 0u);
 }
 template <int R>
 __device__ inline float sum_lanes(float v, unsigned *lds, int &turn_of) {
@@ -126,12 +124,15 @@ __device__ inline double lane64(double v, int lane) {
     const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(b >> 32), lane);
     return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
 }
-template <int R>
-__device__ inline double sum_lanes64(double v, double *lds, int &turn_of) {
+__device__ inline double sum16(double v) {
     v += turn64<0x128>(v);
     v += turn64<0x124>(v);
     v += turn64<0x122>(v);
-    v += turn64<0x121>(v);
+    return v + turn64<0x121>(v);
+}
+template <int R>
+__device__ inline double sum_lanes64(double v, double *lds, int &turn_of) {
+    v = sum16(v);
     if (R == 16)
         return v;
     v = (lane64(v, 0) + lane64(v, 16)) + (lane64(v, 32) + lane64(v, 48));
@@ -142,11 +143,8 @@ __device__ inline double sum_lanes64(double v, double *lds, int &turn_of) {
     if ((threadIdx.x & 63) == 0)
         buf[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = buf[0];
-#pragma unroll
-    for (int i = 1; i < R / 64; ++i)
-        v += buf[i];
-    return v;
+    const int i = threadIdx.x & 15;
+    return sum16(i < R / 64 ? buf[i] : 0.0);
 }
 
 struct NormArgs {
@@ -279,13 +277,16 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(NormArgs a) {
     __shared__ double lds[2 * (TH / 64)];
     constexpr int GR = TH / R;   // rows at a time
     __shared__ __attribute__((aligned(16))) float sums[GR > 1 ? TH * V * 8 : 8];
+    // w and dy in registers; the widest rows read them again, which come from L2
+    constexpr bool kKeep = V == 1;
     const int lane = threadIdx.x % R;
     int turn_of = 0;
     float w[V][8], dw[V][8];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int c = (lane + v * R) * 8;
-        load_upto<float, 8>(a.w + c, a.D - c, w[v]);
+        if (kKeep)
+            load_upto<float, 8>(a.w + c, a.D - c, w[v]);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             dw[v][i] = 0.0f;
@@ -297,6 +298,8 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(NormArgs a) {
         const bool live = mm < a.M;
         const long long m = live ? mm : a.M - 1;
         float r[V][8], g[V][8];
+        const float *wr = a.w;
+        asm volatile("" : "+s"(wr));   // read in every row, not once into registers
         double ss = 0.0, sg = 0.0;
         const F *rr = (const F *)a.res + m * a.sres;
         const E *dy = (const E *)a.x + m * a.sx;
@@ -305,16 +308,23 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(NormArgs a) {
         for (int v = 0; v < V; ++v) {
             const int c = (lane + v * R) * 8;
             load_upto<F, 8>(rr + c, a.D - c, r[v]);
-            load_upto<E, 8>(dy + c, a.D - c, g[v]);
+            if (kKeep)
+                load_upto<E, 8>(dy + c, a.D - c, g[v]);
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+        for (int v = 0; v < V; ++v) {
+            const int c = (lane + v * R) * 8;
+            if (!kKeep) {
+                load_upto<float, 8>(wr + c, a.D - c, w[v]);
+                load_upto<E, 8>(dy + c, a.D - c, g[v]);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const double rd = r[v][i];
                 ss = __builtin_fma(rd, rd, ss);
                 sg = __builtin_fma((double)w[v][i] * (double)g[v][i], rd, sg);
             }
+        }
         ss = sum_lanes64<R>(ss, lds, turn_of);
         sg = sum_lanes64<R>(sg, lds, turn_of);
         const double var = __builtin_fma(ss, mean, a.eps);
@@ -326,8 +336,15 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(NormArgs a) {
             float o[8];
             if (dr)
                 load_upto<F, 8>(dr + c, a.D - c, o);
+            if (!kKeep) {
+                load_upto<float, 8>(wr + c, a.D - c, w[v]);
+                load_upto<E, 8>(dy + c, a.D - c, g[v]);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+                // converted again: the fp64 values of both passes at once would take
+                // twice the registers
+                asm volatile("" : "+v"(r[v][i]), "+v"(g[v][i]));
                 if (live)
                     dw[v][i] = __builtin_fmaf(g[v][i] * inv, r[v][i], dw[v][i]);
                 const float t =
@@ -373,8 +390,15 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float *partial, in
     const int l = threadIdx.x & 31, g = threadIdx.x >> 5, c = blockIdx.x * 32 + l;
     float s = 0.0f;
     if (c < D)
-        for (int p = g; p < parts; p += 32)
-            s += partial[(long long)p * D + c];
+        for (int p = g; p < parts; p += 256) {
+            float v[8];   // in flight together
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                v[k] = partial[(long long)min(p + 32 * k, parts - 1) * D + c];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                s += p + 32 * k < parts ? v[k] : 0.0f;
+        }
     red[g][l] = s;
     __syncthreads();
     if (g == 0 && c < D) {
@@ -424,10 +448,6 @@ inline bool make_drop(double p, unsigned long long seed, unsigned long long offs
     return true;
 }
 
-// Workgroups that walk the rows: two of 256 threads a compute unit keep the
-// partial sums few.
-constexpr int kGradBlocks = 512;
-
 inline bool norm_shape(int type, int rtype, int M, int D) {
     return type_size(type) && (rtype == type || rtype == FINC_F32) && M >= 0 && D >= 1 &&
            (long long)M * per_row(D) < (1ll << 31);
@@ -441,8 +461,11 @@ inline bool same(const Region &a, const Region &b) {
     return a.p == b.p && a.so == b.so && a.size == b.size;
 }
 
-// Calls f<E, F, R, V, TH>: lanes a row, vectors a lane and threads, by the width.
-template <typename E, typename F, typename Fn>
+// Calls f<E, F, R, V, TH>: lanes a row, vectors a lane and threads, by the width.  The
+// gradients hold three values an element and w, and their sums in fp64: one vector a
+// lane, up to a whole workgroup a row (32768 x 2048 in bf16: 134 us; 276 with four
+// vectors in each lane of a wave a row, whose registers leave a wave a SIMD).
+template <typename E, typename F, bool BACK, typename Fn>
 void with_width(int D, Fn fn) {
 #define FINC_WIDTH(r, v, th)                                                              \
     return fn(E(), F(), std::integral_constant<int, r>(), std::integral_constant<int, v>(), \
@@ -451,27 +474,44 @@ void with_width(int D, Fn fn) {
         FINC_WIDTH(16, 1, 256);
     if (D <= 512)
         FINC_WIDTH(64, 1, 256);
-    if (D <= 1024)
-        FINC_WIDTH(64, 2, 256);
-    if (D <= 2048)
-        FINC_WIDTH(64, 4, 256);
-    if (D <= 4096)
-        FINC_WIDTH(256, 2, 256);
-    if (D <= 8192)
-        FINC_WIDTH(512, 2, 512);
+    if constexpr (BACK) {
+        if (D <= 2048)
+            FINC_WIDTH(256, 1, 256);
+        if (D <= 4096)
+            FINC_WIDTH(512, 1, 512);
+        if (D <= 8192)
+            FINC_WIDTH(1024, 1, 1024);
+    } else {
+        if (D <= 1024)
+            FINC_WIDTH(64, 2, 256);
+        if (D <= 2048)
+            FINC_WIDTH(64, 4, 256);
+        if (D <= 4096)
+            FINC_WIDTH(256, 2, 256);
+        if (D <= 8192)
+            FINC_WIDTH(512, 2, 512);
+    }
     FINC_WIDTH(1024, 2, 1024);
 #undef FINC_WIDTH
 }
-inline int rows_at_a_time(int D) { return D <= 128 ? 16 : D <= 2048 ? 4 : 1; }
 
-template <typename Fn>
+// Workgroups that walk the rows of a gradient, a partial sum of dw each: four waves a
+// SIMD, which the registers allow (32768 x 2048: 134 us, and 192 with half of them; 8192
+// x 8192, whose workgroups are 16 waves: 134 us with 512 and 157 with 2048).
+inline int grad_blocks(int M, int D) {
+    const long long blocks = cdivll(M > 0 ? M : 1, D <= 128 ? 16 : D <= 512 ? 4 : 1);
+    const long long most = D <= 2048 ? 1024 : 512;
+    return (int)(blocks < most ? blocks : most);
+}
+
+template <bool BACK, typename Fn>
 void with_types(int type, int rtype, int D, Fn fn) {
     with_type(type, [&](auto e) {
         typedef decltype(e) E;
         if (rtype == type)
-            with_width<E, E>(D, fn);
+            with_width<E, E, BACK>(D, fn);
         else
-            with_width<E, float>(D, fn);
+            with_width<E, float, BACK>(D, fn);
     });
 }
 
@@ -545,7 +585,7 @@ int finc_add_norm_forward(const finc_norm_args *a, hipStream_t stream) {
     c.D = D;
     c.per = per_row(D);
     c.eps = a->eps;
-    with_types(a->type, a->rtype, D, [&](auto e, auto f, auto R, auto V, auto TH) {
+    with_types<false>(a->type, a->rtype, D, [&](auto e, auto f, auto R, auto V, auto TH) {
         const long long blocks = cdivll(M, TH / R);
         const long long most = 8 * 256 * 256 / TH;   // eight waves a SIMD
         hipLaunchKernelGGL((norm_forward_kernel<decltype(e), decltype(f), R, V, TH>),
@@ -557,8 +597,7 @@ int finc_add_norm_forward(const finc_norm_args *a, hipStream_t stream) {
 size_t finc_add_norm_workspace_bytes(int M, int D) {
     if (!norm_shape(FINC_F32, FINC_F32, M, D) || D > FINC_MAX_ROW)
         return 0;
-    const long long blocks = cdivll(M > 0 ? M : 1, rows_at_a_time(D));
-    return ((size_t)(blocks < kGradBlocks ? blocks : kGradBlocks) * D * 4 + 255) / 256 * 256;
+    return ((size_t)grad_blocks(M, D) * D * 4 + 255) / 256 * 256;
 }
 
 int finc_add_norm_backward(const finc_norm_grad_args *a, hipStream_t stream) {
@@ -608,9 +647,8 @@ int finc_add_norm_backward(const finc_norm_grad_args *a, hipStream_t stream) {
     c.eps = a->eps;
     int parts = 0;
     if (M > 0) {
-        const long long blocks = cdivll(M, rows_at_a_time(D));
-        parts = (int)(blocks < kGradBlocks ? blocks : kGradBlocks);
-        with_types(a->type, a->rtype, D, [&](auto e, auto f, auto R, auto V, auto TH) {
+        parts = grad_blocks(M, D);
+        with_types<true>(a->type, a->rtype, D, [&](auto e, auto f, auto R, auto V, auto TH) {
             hipLaunchKernelGGL((norm_backward_kernel<decltype(e), decltype(f), R, V, TH>),
                                dim3((unsigned)parts), dim3(TH), 0, stream, c);
         });

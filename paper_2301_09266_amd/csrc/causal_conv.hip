@@ -219,8 +219,15 @@ __global__ __launch_bounds__(256) void conv_sum_kernel(const float *partial, int
     const long long e = blockIdx.x * 32ll + l;
     float s = 0.0f;
     if (e < n)
-        for (int p = grp; p < parts; p += 8)
-            s += partial[p * n + e];
+        for (int p = grp; p < parts; p += 64) {
+            float v[8];   // in flight together
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                v[k] = partial[min(p + 8 * k, parts - 1) * n + e];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                s += p + 8 * k < parts ? v[k] : 0.0f;
+        }
     red[grp][l] = s;
     __syncthreads();
     if (grp == 0 && e < n) {

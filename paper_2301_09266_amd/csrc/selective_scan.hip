@@ -204,12 +204,13 @@ __device__ inline typename Vec<E, N>::type load_part(const E *p, int count) {
     for (int i = 0; i < N; ++i)
         v[i] = (E)0.0f;
     if (count > 0) {
+        const int n = afresh(count);
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            v[i] = p[min(i, count - 1)];
+            v[i] = p[min(i, n - 1)];
 #pragma unroll
         for (int i = 1; i < N; ++i)
-            v[i] = i < count ? v[i] : (E)0.0f;
+            v[i] = i < n ? v[i] : (E)0.0f;
     }
     return v;
 }
@@ -840,8 +841,15 @@ __global__ __launch_bounds__(256) void param_sum_kernel(GradArgs ga, float *dA, 
     const long long i = blockIdx.x * 32ll + l;
     float s = 0.0f;
     if (i < n)
-        for (int b = g; b < a.B; b += 8)
-            s += ga.params[b * n + i];
+        for (int b = g; b < a.B; b += 64) {
+            float v[8];   // in flight together
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                v[k] = ga.params[min(b + 8 * k, a.B - 1) * n + i];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                s += b + 8 * k < a.B ? v[k] : 0.0f;
+        }
     red[g][l] = s;
     __syncthreads();
     if (g || i >= n)

@@ -48,6 +48,14 @@ __device__ inline void load_vec(const E *p, float *v) {
     }
 }
 
+// The value, of which the compiler knows nothing: what follows from it is formed here
+// and not ahead of a loop, where the addresses and masks of a vector's elements would
+// take its registers for a path that few lanes take.
+__device__ inline int afresh(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // The first `count` (any int) of N elements; the others are 0.  A part of a vector
 // takes its elements one by one, the last one again in place of those past it: no
 // branch an element.
@@ -61,12 +69,13 @@ __device__ inline void load_upto(const E *p, int count, float *v) {
     for (int i = 0; i < N; ++i)
         v[i] = 0.0f;
     if (count > 0) {
+        const int n = afresh(count);
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            v[i] = (float)p[min(i, count - 1)];
+            v[i] = (float)p[min(i, n - 1)];
 #pragma unroll
         for (int i = 1; i < N; ++i)
-            v[i] = i < count ? v[i] : 0.0f;
+            v[i] = i < n ? v[i] : 0.0f;
     }
 }
 
@@ -89,9 +98,10 @@ __device__ inline void store_upto(E *p, int count, const float *v) {
         store_vec<E, N>(p, v);
         return;
     }
+    const int n = afresh(count);
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        if (i < count)
+        if (i < n)
             p[i] = (E)v[i];
 }
 
