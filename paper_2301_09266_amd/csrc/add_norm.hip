@@ -463,7 +463,7 @@ inline bool same(const Region &a, const Region &b) {
 
 // Calls f<E, F, R, V, TH>: lanes a row, vectors a lane and threads, by the width.  The
 // gradients hold three values an element and w, and their sums in fp64: one vector a
-// lane, up to a whole workgroup a row (32768 x 2048 in bf16: 134 us; 276 with four
+// lane, up to a whole workgroup a row (32768 x 2048 in bf16: 131 us; 276 with four
 // vectors in each lane of a wave a row, whose registers leave a wave a SIMD).
 template <typename E, typename F, bool BACK, typename Fn>
 void with_width(int D, Fn fn) {
@@ -496,8 +496,8 @@ void with_width(int D, Fn fn) {
 }
 
 // Workgroups that walk the rows of a gradient, a partial sum of dw each: four waves a
-// SIMD, which the registers allow (32768 x 2048: 134 us, and 192 with half of them; 8192
-// x 8192, whose workgroups are 16 waves: 134 us with 512 and 157 with 2048).
+// SIMD, which the registers allow (32768 x 2048: 131 us, and 192 with half of them; 8192
+// x 8192, whose workgroups are 16 waves: 133 us with 512 and 157 with 2048).
 inline int grad_blocks(int M, int D) {
     const long long blocks = cdivll(M > 0 ? M : 1, D <= 128 ? 16 : D <= 512 ? 4 : 1);
     const long long most = D <= 2048 ? 1024 : 512;

@@ -939,7 +939,8 @@ constexpr int kLds = 160 * 1024;
 
 inline bool scan_shape(int type, int B, int D, int L, int N, int G) {
     return type_size(type) && B >= 0 && D >= 1 && L >= 0 && L < (1 << 30) && N >= 1 &&
-           N <= FINC_MAX_STATE && G >= 1 && D % G == 0 && (long long)B * D < (1ll << 31) - 256;
+           N <= FINC_MAX_STATE && G >= 1 && D % G == 0 && (long long)B * D < (1ll << 31) - 256 &&
+           (long long)B * G * N < (1ll << 31) && (long long)G * N < (1ll << 31);
 }
 
 // Positions a lane: the gradients' parts and the states' layout depend on it.
@@ -1000,7 +1001,7 @@ inline int set_channels(int B, int D, int G) {
     long long c = cdivll(cdivll((long long)B * D, 256), kGradWaves) * kGradWaves;
     const long long most = cdivll(D / G, kGradWaves) * kGradWaves;
     c = c < most ? c : most;
-    return (int)(c > 64 ? 64 : c);
+    return (int)(c < kGradWaves ? kGradWaves : c > 64 ? 64 : c);
 }
 
 template <typename E, int T, int S>
@@ -1031,9 +1032,18 @@ int dispatch_backward(GradArgs &c, hipStream_t s) {
                     : launch_backward<E, 8, 4>(c, s);
 }
 
-inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+// A buffer of a * b * c * d floats, whole 256-byte lines; 0 for one of more bytes than
+// an address space has.
+inline size_t floats(long long a, long long b, long long c, long long d) {
+    const unsigned __int128 n = (unsigned __int128)a * b * c * d;
+    return n >> 48 ? 0 : ((size_t)n * 4 + 255) / 256 * 256;
+}
 inline size_t shared_bytes(int B, int D, int L, int N, int G) {
-    return up256((size_t)2 * cdivll(D / G, set_channels(B, D, G)) * B * G * N * L * 4);
+    return floats(2 * cdivll(D / G, set_channels(B, D, G)), B, (long long)G * N, L);
+}
+// Whether both of the gradients' buffers have a size.
+inline bool grad_sizes(int B, int D, int L, int N, int G) {
+    return B == 0 || L == 0 || (shared_bytes(B, D, L, N, G) && floats(B, D, N + 2, 1));
 }
 
 }  // namespace
@@ -1043,13 +1053,15 @@ extern "C" {
 size_t finc_selective_scan_states_bytes(int B, int D, int L, int N) {
     if (!scan_shape(FINC_F32, B, D, L, N, 1))
         return 0;
-    return ((size_t)B * D * part_count(L, N) * 4 * row_states(N) * 4 + 255) / 256 * 256;
+    return floats(B, D, part_count(L, N), 4 * row_states(N));
 }
 
 int finc_selective_scan_forward(const finc_scan_args *a, hipStream_t stream) {
     if (!a || !scan_shape(a->type, a->B, a->D, a->L, a->N, a->G) || ((uintptr_t)a->states & 255u))
         return FINC_EINVAL;
     const int sz = type_size(a->type), B = a->B, D = a->D, L = a->L;
+    if (a->states && B > 0 && !finc_selective_scan_states_bytes(B, D, L, a->N))
+        return FINC_EUNSUPPORTED;
     const long long st = (long long)B * D * a->N, GN = (long long)a->G * a->N;
     const Region in[] = {raster(a->x, B, D, L, sz), raster(a->dt, B, D, L, sz),
                          a->z.p ? raster(a->z, B, D, L, sz) : flat(nullptr, 0, sz),
@@ -1088,9 +1100,9 @@ int finc_selective_scan_forward(const finc_scan_args *a, hipStream_t stream) {
 }
 
 size_t finc_selective_scan_workspace_bytes(int B, int D, int L, int N, int G) {
-    if (!scan_shape(FINC_F32, B, D, L, N, G))
+    if (!scan_shape(FINC_F32, B, D, L, N, G) || !grad_sizes(B, D, L, N, G))
         return 0;
-    return shared_bytes(B, D, L, N, G) + up256((size_t)B * D * (N + 2) * 4);
+    return shared_bytes(B, D, L, N, G) + floats(B, D, N + 2, 1);
 }
 
 int finc_selective_scan_backward(const finc_scan_args *a, const finc_scan_grads *g,
@@ -1099,6 +1111,8 @@ int finc_selective_scan_backward(const finc_scan_args *a, const finc_scan_grads 
         ((uintptr_t)a->states & 255u) || ((uintptr_t)g->workspace & 255u))
         return FINC_EINVAL;
     const int sz = type_size(a->type), B = a->B, D = a->D, L = a->L, N = a->N, G = a->G;
+    if (!grad_sizes(B, D, L, N, G) || (B > 0 && !finc_selective_scan_states_bytes(B, D, L, N)))
+        return FINC_EUNSUPPORTED;
     const long long st = (long long)B * D * N;
     const int GN = G * N;
     const Region none = flat(nullptr, 0, 4);

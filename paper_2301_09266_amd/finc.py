@@ -955,7 +955,7 @@ def _raster(t: torch.Tensor | None):
     if len(st) == 3:
         return t.data_ptr(), st[0], st[1]
     G, N = t.shape[1], t.shape[2]
-    if G > 1 and N > 1 and st[1] != N * st[2]:
+    if G > 1 and N > 1 and st[1] != N * st[2] and t.numel():
         raise ValueError("the groups of a (B, G, N, L) tensor must follow each other")
     return t.data_ptr(), st[0], st[2] if N > 1 else st[1]
 
@@ -1186,7 +1186,7 @@ def selective_scan_step(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, Bm: 
         zp, zs = _act(z, "z", dev, T, shape).data_ptr(), z.stride(0)
     for t, name in ((Bm, "Bm"), (Cm, "Cm")):
         _act(t, name, dev, T, (B, G, N))
-        if G > 1 and t.stride(1) != N:
+        if B > 0 and G > 1 and t.stride(1) != N:
             raise ValueError(f"the groups of {name} must follow each other")
     y = _out(out, x, "out", dev)
     a = SCAN_STEP_ARGS.pack(kind, B, S, C, N, G, bool(softplus), x.data_ptr(), dt.data_ptr(), zp,

@@ -593,6 +593,105 @@ def test_graphs_replay_the_calls():
         assert same_bits(want, call()), "eager work between replays"
 
 
+def test_outputs_beside_their_inputs():
+    """A projection's two halves: the output of one in the other's place, and two
+    gradients side by side."""
+    t, _, r = scan_inputs(3, 10, 70, 16, 1, "gdbp", BF16, 31)
+    g, kw = scan_kw(t, None, "gdbp", None)
+    w = r.normal(10, 4).to(DEV)
+    both = torch.full((3, 20, 70), NAN, dtype=BF16, device=DEV)
+    both[:, :10] = g["x"]
+    y = finc.causal_conv_forward(both[:, :10], w, out=both[:, 10:])
+    assert torch.equal(both[:, 10:], finc.causal_conv_forward(g["x"], w))
+    assert torch.equal(both[:, :10], g["x"]) and y.data_ptr() == both[:, 10:].data_ptr()
+    with pytest.raises(finc.FincError):
+        finc.causal_conv_forward(both[:, :10], w, out=both[:, 5:15])
+    states = finc.selective_scan_states(3, 10, 70, 16, DEV)
+    kw.pop("state")
+    finc.selective_scan_forward(**g, **kw, states=states)
+    dy = r.normal(3, 10, 70, kind=BF16).to(DEV)
+    args = {k: v for k, v in g.items()}
+    apart = finc.selective_scan_backward(**args, **kw, dy=dy, states=states)
+    pair = torch.full((3, 20, 70), NAN, dtype=BF16, device=DEV)
+    finc.selective_scan_backward(**args, **kw, dy=dy, states=states, dx=pair[:, :10],
+                                 dz=pair[:, 10:])
+    assert torch.equal(pair, torch.cat([apart["dx"], apart["dz"]], dim=1))
+
+
+def test_empty_batches():
+    x = torch.empty(0, 6, 40, device=DEV)
+    w, bias = torch.ones(6, 4, device=DEV), torch.ones(6, device=DEV)
+    assert finc.causal_conv_forward(x, w, bias).shape == x.shape
+    dx, dw, db, _ = finc.causal_conv_backward(x, w, x, bias)
+    assert dx.shape == x.shape and not dw.any() and not db.any()
+    A, Bm = -torch.ones(6, 16, device=DEV), torch.empty(0, 2, 16, 40, device=DEV)
+    states = finc.selective_scan_states(0, 6, 40, 16, DEV)
+    assert finc.selective_scan_forward(x, x, A, Bm, Bm, bias, x, bias,
+                                       states=states).shape == x.shape
+    grads = finc.selective_scan_backward(x, x, A, Bm, Bm, x, states, bias, x, bias)
+    assert not grads["dA"].any() and not grads["dD"].any() and not grads["ddt_bias"].any()
+    assert finc.causal_conv_step(x[:, :, 0], w, torch.ones(2, 6, 3, device=DEV)).shape == (0, 6)
+    assert finc.selective_scan_step(x[:, :, 0], x[:, :, 0], A, Bm[..., 0], Bm[..., 0],
+                                    torch.ones(2, 6, 16, device=DEV)).shape == (0, 6)
+    q, scale, _ = finc.add_norm_forward(x, torch.ones(40, device=DEV), fp8=True)
+    assert q.shape == x.shape and scale.shape == (0, 6)
+
+
+def test_the_binding_refuses():
+    t, _, r = scan_inputs(2, 6, 40, 16, 2, "gsdbp", F32, 41)
+    g, kw = scan_kw(t, None, "gsdbp", None)
+    w = r.normal(6, 4).to(DEV)
+    x = g["x"]
+
+    def refused(text, call, *args, **more):
+        with pytest.raises(ValueError, match=text):
+            call(*args, **more)
+
+    conv, scan = finc.causal_conv_forward, finc.selective_scan_forward
+    refused("x must be float32, bfloat16 or float16", conv, x.double(), w)
+    refused("x must be contiguous in its last", conv, x.transpose(1, 2), r.normal(40, 4).to(DEV))
+    refused("w has shape", conv, x, w[:5])
+    refused("w must be torch.float32", conv, x, w.bfloat16())
+    refused("w must be on the device", conv, x, w.cpu())
+    refused("w must be contiguous", conv, x, w.t().contiguous().t())
+    refused("state has shape", conv, x, w, state=torch.zeros(2, 6, 4, device=DEV))
+    refused("state must be", conv, x, w, state=torch.zeros(2, 6, 3, device=DEV, dtype=BF16))
+    refused("lengths must be torch.int32", conv, x, w, lengths=torch.zeros(2, device=DEV))
+    refused("out has shape", conv, x, w, out=x[:, :, 1:])
+    refused("dy has shape", finc.causal_conv_backward, x, w, x[:1])
+    refused("workspace holds", finc.causal_conv_backward, x, w, x,
+            workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+    refused("state has 1 entries for 2", finc.causal_conv_step, x[:, :, 0].contiguous(), w,
+            torch.zeros(1, 6, 3, device=DEV))
+    refused("dt must be", scan, **dict(g, dt=g["dt"].bfloat16()), **kw)
+    refused("Cm has shape", scan, **dict(g, Cm=g["Cm"][:, :1]), **kw)
+    refused("groups of a", scan, **dict(g, Bm=torch.zeros(2, 3, 16, 40, device=DEV)[:, ::2]), **kw)
+    refused("D has shape", scan, **dict(g, D=w[0]), **kw)
+    refused("state must be", scan, **g, **dict(kw, state=kw["state"].bfloat16()))
+    refused("states holds", scan, **g, **kw, states=torch.empty(8, device=DEV))
+    refused("slots must be", finc.selective_scan_step, x[:, :, 0].contiguous(),
+            x[:, :, 0].contiguous(), g["A"], g["Bm"][..., 0].contiguous(),
+            g["Cm"][..., 0].contiguous(), kw["state"], slots=torch.zeros(2, device=DEV))
+    rows, nw = r.normal(8, 40).to(DEV), torch.ones(40, device=DEV)
+    refused("expected 0 <= p", finc.dropout, rows, 1.0, 0)
+    refused("expected 0 <= p", finc.dropout, rows, -0.5, 0)
+    refused("seed must be", finc.dropout, rows, 0.5, -1)
+    refused("offset must be", finc.dropout, rows, 0.5, 0, 1 << 64)
+    refused("must lie evenly", finc.dropout, torch.zeros(4, 6, 5, 40, device=DEV)[:, :2, :3], 0.5, 0)
+    refused("residual must be", finc.add_norm_forward, rows, nw, rows.bfloat16())
+    refused("residual_out must be", finc.add_norm_forward, rows.bfloat16(), nw, rows.bfloat16(),
+            residual_out=rows)
+    refused("scale goes with fp8", finc.add_norm_forward, rows, nw,
+            scale=torch.zeros(8, device=DEV))
+    refused("out must be", finc.add_norm_forward, rows, nw, fp8=True, out=rows.bfloat16())
+    refused("r must be", finc.add_norm_backward, rows, rows.half(), nw)
+    refused("dr must be", finc.add_norm_backward, rows, rows, nw, rows.bfloat16())
+    wide = torch.zeros(2, 16385, device=DEV)
+    with pytest.raises(finc.FincError) as e:
+        finc.add_norm_forward(wide, torch.zeros(16385, device=DEV))
+    assert e.value.code == finc.EUNSUPPORTED
+
+
 def test_offsets_past_31_bits():
     """Rows of one tensor of more than 2^31 elements."""
     D, L = 3, (1 << 30) - 8
