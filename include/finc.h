@@ -664,9 +664,10 @@ int finc_dropout(int type, const void *x, long long sx, const void *residual, lo
  *   y = r (mean_d r^2 + eps)^(-1/2) w,
  * from r in fp32.  x, y: type; residual, r: rtype (type itself or FINC_F32),
  * residual NULL for 0, r NULL where it is not wanted; w: D.  With scale (M
- * floats) y is instead 8 bits wide, OCP e4m3: scale[m] = max(max_d |y| / 448,
- * 2^-126), and y / scale rounded to nearest even.  A NaN in a row makes its
- * outputs and its scale NaN.  r may be residual itself and y may be x itself,
+ * floats) y is instead 8 bits wide, OCP e4m3: s = max(max_d |y| / 448, 2^-126)
+ * and y / s in fp64, from the sum before r rounds it; y / s is rounded to fp32
+ * and then to 8 bits, each to nearest even, and scale[m] is s in fp32.  A NaN in
+ * a row makes its outputs and its scale NaN.  r may be residual itself and y may be x itself,
  * with their rows' steps. */
 typedef struct {
     int type, rtype, M, D;

@@ -44,6 +44,15 @@ __device__ inline void drop_bits(const Drop &d, unsigned long long at, unsigned 
     w[2] = c2;
     w[3] = c3;
 }
+// Which of eight elements are kept.
+__device__ inline unsigned kept_bits(const Drop &d, unsigned long long at) {
+    unsigned w[4], kept = 0;
+    drop_bits(d, at, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        kept |= (unsigned)((i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu) >= d.cut) << i;
+    return kept;
+}
 __device__ inline void drop(const Drop &d, unsigned long long at, float (&v)[8]) {
     unsigned w[4];
     drop_bits(d, at, w);
@@ -66,11 +75,6 @@ struct Sum {
                                   __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
     }
 };
-// The largest of magnitudes by their bits: NaN is above infinity and stays.
-struct Max {
-    static __device__ unsigned of(unsigned a, unsigned b) { return a > b ? a : b; }
-};
-
 template <typename Op>
 __device__ inline unsigned all16(unsigned v) {
     v = Op::of(v, turn<0x128>(v));   // row_ror:8, 4, 2, 1
@@ -111,7 +115,7 @@ __device__ inline float sum_lanes(float v, unsigned *lds, int &turn_of) {
                               all_lanes<Sum, R>(__builtin_bit_cast(unsigned, v), lds, turn_of));
 }
 
-// Sums in 64 bits, the result in all lanes.
+// Sums and largest magnitudes in 64 bits, the result in all lanes.
 template <int CTRL>
 __device__ inline double turn64(double v) {
     const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
@@ -124,18 +128,30 @@ __device__ inline double lane64(double v, int lane) {
     const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(b >> 32), lane);
     return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
 }
-__device__ inline double sum16(double v) {
-    v += turn64<0x128>(v);
-    v += turn64<0x124>(v);
-    v += turn64<0x122>(v);
-    return v + turn64<0x121>(v);
+struct Sum64 {
+    static __device__ double of(double a, double b) { return a + b; }
+};
+// By the bits without the sign: NaN is above infinity and stays.
+struct Max64 {
+    static __device__ double of(double a, double b) {
+        const unsigned long long u = __builtin_bit_cast(unsigned long long, a) << 1;
+        const unsigned long long v = __builtin_bit_cast(unsigned long long, b) << 1;
+        return u > v ? a : b;
+    }
+};
+template <typename Op>
+__device__ inline double all16_64(double v) {
+    v = Op::of(v, turn64<0x128>(v));
+    v = Op::of(v, turn64<0x124>(v));
+    v = Op::of(v, turn64<0x122>(v));
+    return Op::of(v, turn64<0x121>(v));
 }
-template <int R>
-__device__ inline double sum_lanes64(double v, double *lds, int &turn_of) {
-    v = sum16(v);
+template <typename Op, int R>
+__device__ inline double all_lanes64(double v, double *lds, int &turn_of) {
+    v = all16_64<Op>(v);
     if (R == 16)
         return v;
-    v = (lane64(v, 0) + lane64(v, 16)) + (lane64(v, 32) + lane64(v, 48));
+    v = Op::of(Op::of(lane64(v, 0), lane64(v, 16)), Op::of(lane64(v, 32), lane64(v, 48)));
     if (R == 64)
         return v;
     double *buf = lds + (turn_of & 1) * (R / 64);
@@ -144,7 +160,32 @@ __device__ inline double sum_lanes64(double v, double *lds, int &turn_of) {
         buf[threadIdx.x >> 6] = v;
     __syncthreads();
     const int i = threadIdx.x & 15;
-    return sum16(i < R / 64 ? buf[i] : 0.0);
+    return all16_64<Op>(i < R / 64 ? buf[i] : 0.0);
+}
+
+// 1 / sqrt(v) and 1 / v, from the hardware's first 24 bits by two steps of Newton's,
+// without the scaling that the correctly rounded ones do near the range's ends.  At 0
+// and infinity, where a step is NaN, the first value is the result.
+__device__ inline double rsqrt64(double v) {
+    const double first = __builtin_amdgcn_rsq(v);
+    double y = first;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        y = __builtin_fma(0.5 * y, __builtin_fma(-v * y, y, 1.0), y);
+    return y == y ? y : first;
+}
+__device__ inline double rcp64(double v) {
+    const double first = __builtin_amdgcn_rcp(v);
+    double y = first;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        y = __builtin_fma(y, __builtin_fma(-v, y, 1.0), y);
+    return y == y ? y : first;
+}
+
+// y of the 8-bit norm, from r and what its rounding dropped.
+__device__ inline double row_value(float r, float low, double inv, float w) {
+    return ((double)r + (double)low) * inv * (double)w;
 }
 
 struct NormArgs {
@@ -157,8 +198,6 @@ struct NormArgs {
     double eps;
     Drop drop;
 };
-
-constexpr float kE4m3Max = 448.0f, kLeastScale = 0x1p-126f;
 
 // R lanes a row, V vectors of 8 a lane: vector v of a lane is lane + v R.
 template <typename E, typename F, int R, int V, int TH>
@@ -214,55 +253,121 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(NormArgs a) {
         }
         ss = sum_lanes<R>(ss, lds, turn_of);
         const float inv = rsqrtf(__builtin_fmaf(ss, mean, eps));
-        unsigned top = 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                r[v][i] = r[v][i] * inv * w[v][i];
-                // the padding's lanes hold 0 * inv, which is NaN in a row of NaN
-                const unsigned bits = __builtin_bit_cast(unsigned, r[v][i]) & 0x7fffffffu;
-                top = bits > top ? bits : top;
-            }
-        if (!a.scale) {
-            if (live) {
-                E *out = (E *)a.y + m * a.sy;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const int c = (lane + v * R) * 8;
-                    store_upto<E, 8>(out + c, a.D - c, r[v]);
-                }
-            }
-            continue;
-        }
-        const float most = __builtin_bit_cast(float, all_lanes<Max, R>(top, lds, turn_of));
-        float s = most / kE4m3Max;
-        s = s < kLeastScale ? kLeastScale : s;
-        const float to = 1.0f / s;
         if (live) {
-            if (lane == 0)
-                a.scale[m] = s;
-            unsigned char *out = (unsigned char *)a.y + m * a.sy;
+            E *out = (E *)a.y + m * a.sy;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int c = (lane + v * R) * 8;
-                int q[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    q[h] = __builtin_amdgcn_cvt_pk_fp8_f32(r[v][4 * h] * to, r[v][4 * h + 1] * to,
-                                                           0, false);
-                    q[h] = __builtin_amdgcn_cvt_pk_fp8_f32(r[v][4 * h + 2] * to,
-                                                           r[v][4 * h + 3] * to, q[h], true);
-                }
-                if (c + 8 <= a.D) {
-                    typedef int int2u __attribute__((ext_vector_type(2), aligned(1)));
-                    *(int2u *)(out + c) = int2u{q[0], q[1]};
-                } else {
+                for (int i = 0; i < 8; ++i)
+                    r[v][i] = r[v][i] * inv * w[v][i];
+                store_upto<E, 8>(out + c, a.D - c, r[v]);
+            }
+        }
+    }
+}
+
+// The same with the output in 8 bits.  An element takes another step of e4m3 than the
+// definition's where its error crosses the middle of two: in fp32 a few in ten
+// million.  So the sum (kept as an fp32 value and what that rounds off), the mean, the
+// scale and the quotient are in fp64, and r keeps its low part: 32768 x 2048 in bf16 with
+// the sum stored takes 137 us (bytes: 98), 93 in fp32; 64 x 1000 takes 5.6 (4.8).
+template <typename E, typename F, int R, int V, int TH>
+__global__ __launch_bounds__(TH) void norm_fp8_kernel(NormArgs a) {
+    __shared__ double lds[2 * (TH / 64)];
+    constexpr bool kKeep = V == 1;   // w in registers; the widest rows read it again
+    const int lane = threadIdx.x % R;
+    int turn_of = 0;
+    const double mean = 1.0 / (double)a.D;
+    const double factor = 65536.0 / (65536.0 - (double)a.drop.cut);
+    float w[8];
+    if (kKeep)
+        load_upto<float, 8>(a.w + lane * 8, a.D - lane * 8, w);
+    const long long step = (long long)gridDim.x * (TH / R);
+    for (long long m0 = (long long)blockIdx.x * (TH / R); m0 < a.M; m0 += step) {
+        const long long mm = m0 + threadIdx.x / R;
+        const bool live = mm < a.M;
+        const long long m = live ? mm : a.M - 1;
+        float r[V][8], low[V][8];
+        double ss = 0.0;
+        const E *x = (const E *)a.x + m * a.sx;
+        const F *res = a.res ? (const F *)a.res + m * a.sres : nullptr;
+        const float *wr = a.w;
+        asm volatile("" : "+s"(wr));   // read in every row, not once into registers
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (c + i < a.D)
-                            out[c + i] = (unsigned char)(q[i >> 2] >> (8 * (i & 3)));
-                }
+        for (int v = 0; v < V; ++v) {
+            const int c = (lane + v * R) * 8;
+            float t[8];
+            load_upto<E, 8>(x + c, a.D - c, r[v]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                t[i] = 0.0f;
+            if (res)
+                load_upto<F, 8>(res + c, a.D - c, t);
+            unsigned kept = 0xffu;
+            if (a.drop.cut && c < a.D)
+                kept = kept_bits(a.drop, (unsigned long long)m * a.per + (lane + v * R));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double d = __builtin_fma((double)(kept >> i & 1 ? r[v][i] : 0.0f), factor,
+                                               (double)t[i]);
+                r[v][i] = (float)d;
+                low[v][i] = (float)(d - (double)r[v][i]);
+                ss = __builtin_fma(d, d, ss);
+            }
+        }
+        if (a.r && live) {
+            F *out = (F *)a.r + m * a.sr;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int c = (lane + v * R) * 8;
+                store_upto<F, 8>(out + c, a.D - c, r[v]);
+            }
+        }
+        ss = all_lanes64<Sum64, R>(ss, lds, turn_of);
+        const double inv = rsqrt64(__builtin_fma(ss, mean, a.eps));
+        double top = 0.0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = (lane + v * R) * 8;
+            if (!kKeep)
+                load_upto<float, 8>(wr + c, a.D - c, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                top = Max64::of(top, row_value(r[v][i], low[v][i], inv, w[i]));
+        }
+        top = all_lanes64<Max64, R>(top, lds, turn_of);
+        double s = __builtin_fabs(top) * (1.0 / 448.0);
+        s = s < 0x1p-126 ? 0x1p-126 : s;
+        const double to = rcp64(s);
+        if (!live)
+            continue;
+        if (lane == 0)
+            a.scale[m] = (float)s;
+        unsigned char *out = (unsigned char *)a.y + m * a.sy;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = (lane + v * R) * 8;
+            float y[8];
+            if (!kKeep)
+                load_upto<float, 8>(wr + c, a.D - c, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                y[i] = (float)(row_value(r[v][i], low[v][i], inv, w[i]) * to);
+            int q[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                q[h] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h], y[4 * h + 1], 0, false);
+                q[h] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h + 2], y[4 * h + 3], q[h], true);
+            }
+            if (c + 8 <= a.D) {
+                typedef int int2u __attribute__((ext_vector_type(2), aligned(1)));
+                *(int2u *)(out + c) = int2u{q[0], q[1]};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c + i < a.D)
+                        out[c + i] = (unsigned char)(q[i >> 2] >> (8 * (i & 3)));
             }
         }
     }
@@ -325,11 +430,11 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(NormArgs a) {
                 sg = __builtin_fma((double)w[v][i] * (double)g[v][i], rd, sg);
             }
         }
-        ss = sum_lanes64<R>(ss, lds, turn_of);
-        sg = sum_lanes64<R>(sg, lds, turn_of);
+        ss = all_lanes64<Sum64, R>(ss, lds, turn_of);
+        sg = all_lanes64<Sum64, R>(sg, lds, turn_of);
         const double var = __builtin_fma(ss, mean, a.eps);
-        const double k = -(sg * mean) / var;
-        const float inv = (float)(1.0 / __builtin_sqrt(var));
+        const double root = rsqrt64(var), k = -(sg * mean) * (root * root);
+        const float inv = (float)root;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = (lane + v * R) * 8;
@@ -461,11 +566,17 @@ inline bool same(const Region &a, const Region &b) {
     return a.p == b.p && a.so == b.so && a.size == b.size;
 }
 
+enum { kForward, kFp8, kBackward };
+
 // Calls f<E, F, R, V, TH>: lanes a row, vectors a lane and threads, by the width.  The
-// gradients hold three values an element and w, and their sums in fp64: one vector a
-// lane, up to a whole workgroup a row (32768 x 2048 in bf16: 131 us; 276 with four
-// vectors in each lane of a wave a row, whose registers leave a wave a SIMD).
-template <typename E, typename F, bool BACK, typename Fn>
+// forward holds little an element, so more vectors a lane spare it barriers.  The
+// gradients hold three values an element and w and their sums in fp64, and the 8-bit
+// output fp64 values: above 1024 one vector a lane, up to a whole workgroup a row
+// (gradients of 32768 x 2048 in bf16: 126 us; 276 with four vectors in each lane of a
+// wave a row, whose registers leave a wave a SIMD.  8 bits: 137 us and 185).  Up to
+// 1024 a wave a row, two vectors a lane: with four waves a row a width just below fills
+// two of them (32768 x 1000 in bf16: gradients 63 us and 103, 8 bits 56 and 130).
+template <typename E, typename F, int KIND, typename Fn>
 void with_width(int D, Fn fn) {
 #define FINC_WIDTH(r, v, th)                                                              \
     return fn(E(), F(), std::integral_constant<int, r>(), std::integral_constant<int, v>(), \
@@ -474,7 +585,9 @@ void with_width(int D, Fn fn) {
         FINC_WIDTH(16, 1, 256);
     if (D <= 512)
         FINC_WIDTH(64, 1, 256);
-    if constexpr (BACK) {
+    if (D <= 1024)
+        FINC_WIDTH(64, 2, 256);
+    if constexpr (KIND != kForward) {
         if (D <= 2048)
             FINC_WIDTH(256, 1, 256);
         if (D <= 4096)
@@ -482,8 +595,6 @@ void with_width(int D, Fn fn) {
         if (D <= 8192)
             FINC_WIDTH(1024, 1, 1024);
     } else {
-        if (D <= 1024)
-            FINC_WIDTH(64, 2, 256);
         if (D <= 2048)
             FINC_WIDTH(64, 4, 256);
         if (D <= 4096)
@@ -496,22 +607,22 @@ void with_width(int D, Fn fn) {
 }
 
 // Workgroups that walk the rows of a gradient, a partial sum of dw each: four waves a
-// SIMD, which the registers allow (32768 x 2048: 131 us, and 192 with half of them; 8192
-// x 8192, whose workgroups are 16 waves: 133 us with 512 and 157 with 2048).
+// SIMD, which the registers allow (32768 x 2048: 126 us, and 192 with half of them; 8192
+// x 8192, whose workgroups are 16 waves: 127 us with 512 and 157 with 2048).
 inline int grad_blocks(int M, int D) {
-    const long long blocks = cdivll(M > 0 ? M : 1, D <= 128 ? 16 : D <= 512 ? 4 : 1);
+    const long long blocks = cdivll(M > 0 ? M : 1, D <= 128 ? 16 : D <= 1024 ? 4 : 1);
     const long long most = D <= 2048 ? 1024 : 512;
     return (int)(blocks < most ? blocks : most);
 }
 
-template <bool BACK, typename Fn>
+template <int KIND, typename Fn>
 void with_types(int type, int rtype, int D, Fn fn) {
     with_type(type, [&](auto e) {
         typedef decltype(e) E;
         if (rtype == type)
-            with_width<E, E, BACK>(D, fn);
+            with_width<E, E, KIND>(D, fn);
         else
-            with_width<E, float, BACK>(D, fn);
+            with_width<E, float, KIND>(D, fn);
     });
 }
 
@@ -585,7 +696,16 @@ int finc_add_norm_forward(const finc_norm_args *a, hipStream_t stream) {
     c.D = D;
     c.per = per_row(D);
     c.eps = a->eps;
-    with_types<false>(a->type, a->rtype, D, [&](auto e, auto f, auto R, auto V, auto TH) {
+    if (a->scale) {
+        with_types<kFp8>(a->type, a->rtype, D, [&](auto e, auto f, auto R, auto V, auto TH) {
+            const long long blocks = cdivll(M, TH / R), most = 8 * 256 * 256 / TH;
+            hipLaunchKernelGGL((norm_fp8_kernel<decltype(e), decltype(f), R, V, TH>),
+                               dim3((unsigned)(blocks < most ? blocks : most)), dim3(TH), 0,
+                               stream, c);
+        });
+        return launched();
+    }
+    with_types<kForward>(a->type, a->rtype, D, [&](auto e, auto f, auto R, auto V, auto TH) {
         const long long blocks = cdivll(M, TH / R);
         const long long most = 8 * 256 * 256 / TH;   // eight waves a SIMD
         hipLaunchKernelGGL((norm_forward_kernel<decltype(e), decltype(f), R, V, TH>),
@@ -648,7 +768,7 @@ int finc_add_norm_backward(const finc_norm_grad_args *a, hipStream_t stream) {
     int parts = 0;
     if (M > 0) {
         parts = grad_blocks(M, D);
-        with_types<true>(a->type, a->rtype, D, [&](auto e, auto f, auto R, auto V, auto TH) {
+        with_types<kBackward>(a->type, a->rtype, D, [&](auto e, auto f, auto R, auto V, auto TH) {
             hipLaunchKernelGGL((norm_backward_kernel<decltype(e), decltype(f), R, V, TH>),
                                dim3((unsigned)parts), dim3(TH), 0, stream, c);
         });
