@@ -802,7 +802,8 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
     }
 }
 
-// dB and dC: the sets' sums in order.
+// dB and dC: the sets' sums in order, eight loads in flight a thread: bound by memory (64
+// sets' sums of 4 x 16 x 4096, 134 MB: 22 us, and 39 with one load at a time).
 template <typename E>
 __global__ __launch_bounds__(256) void shared_sum_kernel(GradArgs ga, Rows dB, Rows dC) {
     const ScanArgs &a = ga.f;
@@ -821,12 +822,16 @@ __global__ __launch_bounds__(256) void shared_sum_kernel(GradArgs ga, Rows dB, R
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     const long long step = (long long)a.B * rows * a.L;
     const float *p = ga.shared + which * ga.sets * step + ((long long)b * rows + r) * a.L + t0;
-    for (int k = 0; k < ga.sets; ++k) {
-        float v[4];
-        load_upto<float, 4>(p + k * step, n_pos - t0, v);
+    for (int k0 = 0; k0 < ga.sets; k0 += 8) {
+        float v[8][4];   // in flight together
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            s[i] += v[i];
+        for (int k = 0; k < 8; ++k)
+            load_upto<float, 4>(p + min(k0 + k, ga.sets - 1) * step, n_pos - t0, v[k]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                s[i] += k0 + k < ga.sets ? v[k][i] : 0.0f;
     }
     store_upto<E, 4>((which ? dC : dB).row<E>(b, r) + t0, a.L - t0, s);
 }
