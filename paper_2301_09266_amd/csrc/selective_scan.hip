@@ -224,28 +224,73 @@ __device__ inline typename Vec<E, N>::type load_raw(const E *p, int count, bool 
     return whole ? load_whole<E, N>(p) : load_part<E, N>(p, count);
 }
 
+// Where N elements from `pos` of a row of L are loaded, or its last N where they would
+// pass its end: bytes from the row's start.  One load in every lane, which is waited for
+// only where settle() uses it.
+template <typename E, int N>
+__device__ inline unsigned back(int pos, int L) {
+    unsigned o = (unsigned)min(pos, L - N) * (unsigned)sizeof(E);
+    asm volatile("" : "+v"(o));   // formed where it is used (see at())
+    return o;
+}
+template <typename E, int N>
+__device__ inline typename Vec<E, N>::type load_back(const E *row, unsigned o) {
+    return load_whole<E, N>((const E *)((const char *)row + o));
+}
+// Those of load_back at their places, 0 from n_pos on.
+template <typename E, int N>
+__device__ inline void settle(typename Vec<E, N>::type v, int pos, int L, int n_pos,
+                              float (&out)[N]) {
+    static_assert(N <= 2, "one element to move");
+    out[N - 1] = keep_if(pos + N - 1 < n_pos, (float)v[N - 1]);
+    if (N == 2)
+        out[0] = keep_if(pos < n_pos, (float)(pos + N > L ? v[N - 1] : v[0]));
+}
+template <typename E, int N>
+__device__ inline void convert(typename Vec<E, N>::type v, float (&out)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        out[i] = (float)v[i];
+}
+
 constexpr int kUnit = 8;   // elements of B and C that a thread moves at once
 
-// What a thread loads of B and C for one part: unit u of 2 N P / 8.
+// What a thread loads of B and C for one part: unit u of 2 N P / 8, the row's last
+// elements where the unit passes its end.
+__device__ inline int unit_at(int pos, int L) { return L < kUnit ? pos : min(pos, L - kUnit); }
 template <typename E, int T>
 __device__ inline typename Vec<E, kUnit>::type load_tile(const ScanArgs &a, int b, int grp, int u,
                                                          int p0, int n_pos) {
     constexpr int Q = 16 * T / kUnit;
-    const int r = u / Q, q = (u % Q) * kUnit;
+    const int r = u / Q, pos = p0 + (u % Q) * kUnit;
     const E *row = (r >= a.N ? a.Cm : a.Bm)
                        .row<const E>(b, (long long)grp * a.N + (r >= a.N ? r - a.N : r));
-    return load_raw<E, kUnit>(row + p0 + q, n_pos - p0 - q, p0 + 16 * T <= n_pos);
+    // parts of eight positions a lane are those of longer rasters
+    return load_raw<E, kUnit>(row + unit_at(pos, a.L), n_pos - pos, T == 8 || a.L >= kUnit);
 }
 template <typename E, int T>
-__device__ inline void store_tile(float *tb, float *tc, int N, int u,
+__device__ inline void store_tile(const ScanArgs &a, float *tb, float *tc, int u, int p0, int n_pos,
                                   typename Vec<E, kUnit>::type v) {
     constexpr int Q = 16 * T / kUnit;
-    const int r = u / Q, q = (u % Q) * kUnit;
-    float *to = r >= N ? tc + (r - N) * 16 * T : tb + r * 16 * T;
+    const int r = u / Q;
+    float *to = r >= a.N ? tc + (r - a.N) * 16 * T : tb + r * 16 * T;
+    int q = (u % Q) * kUnit;
+    if (p0 + 16 * T <= n_pos) {
+#pragma unroll
+        for (int k = 0; k < kUnit; k += 4)
+            *(float4 *)(to + slot_at<T>(q + k)) =
+                make_float4((float)v[k], (float)v[k + 1], (float)v[k + 2], (float)v[k + 3]);
+        return;
+    }
+    q = afresh(q);
 #pragma unroll
     for (int k = 0; k < kUnit; k += 4)
-        *(float4 *)(to + slot_at<T>(q + k)) =
-            make_float4((float)v[k], (float)v[k + 1], (float)v[k + 2], (float)v[k + 3]);
+        *(float4 *)(to + slot_at<T>(q + k)) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const int first = unit_at(p0 + q, a.L) - p0;   // in the part, or before it
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k)
+        if (first + k >= q && first + k < n_pos - p0)
+            to[slot_at<T>(first + k)] = (float)v[k];
 }
 
 // The forward's tiles: two in LDS, and the loads of one more.  Up to K units a thread
@@ -262,9 +307,11 @@ struct Tiles {
     __device__ float *of(int part) const { return lds + (part & 1) * 2 * a.N * P; }
     __device__ void fetch(int part) {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            ahead[k] = load_tile<E, T>(a, b, grp, min((int)threadIdx.x + k * kThreads, units - 1),
-                                       part * P, n_pos);
+        for (int k = 0; k < K; ++k) {
+            // fp32's tile leaves no registers for the unit's address (bf16: 3% more time)
+            const int u = min((int)threadIdx.x + k * kThreads, units - 1);
+            ahead[k] = load_tile<E, T>(a, b, grp, sizeof(E) == 4 ? afresh(u) : u, part * P, n_pos);
+        }
     }
     // The part that was fetched.
     __device__ void store(int part) {
@@ -272,9 +319,10 @@ struct Tiles {
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if ((int)threadIdx.x + k * kThreads < units)
-                store_tile<E, T>(tb, tc, a.N, threadIdx.x + k * kThreads, ahead[k]);
+                store_tile<E, T>(a, tb, tc, threadIdx.x + k * kThreads, part * P, n_pos, ahead[k]);
         for (int u = threadIdx.x + K * kThreads; u < units; u += kThreads)
-            store_tile<E, T>(tb, tc, a.N, u, load_tile<E, T>(a, b, grp, u, part * P, n_pos));
+            store_tile<E, T>(a, tb, tc, u, part * P, n_pos,
+                             load_tile<E, T>(a, b, grp, u, part * P, n_pos));
     }
 };
 
@@ -346,18 +394,12 @@ __global__ __launch_bounds__(kThreads, 4) void scan_forward_kernel(ScanArgs a) {
     typename Vec<E, I>::type nx, nd, nz;
     Tiles<E, T> tiles(a, lds, b, grp, n_pos);
     auto fetch = [&](int p0) {
-        const E *xr = a.x.row<const E>(b, d) + p0, *dr = a.dt.row<const E>(b, d) + p0;
-        const E *zr = a.z.p ? a.z.row<const E>(b, d) + p0 : xr;
-        if (p0 + P <= n_pos) {
-            nx = load_whole<E, I>(at(xr, pos));
-            nd = load_whole<E, I>(at(dr, pos));
-            nz = load_whole<E, I>(at(zr, pos));
-        } else {
-            const int left = n_pos - p0 - pos;
-            nx = load_part<E, I>(at(xr, pos), left);
-            nd = load_part<E, I>(at(dr, pos), left);
-            nz = load_part<E, I>(at(zr, pos), left);
-        }
+        const E *xr = a.x.row<const E>(b, d), *dr = a.dt.row<const E>(b, d);
+        const E *zr = a.z.p ? a.z.row<const E>(b, d) : xr;
+        const unsigned o = back<E, I>(p0 + pos, a.L);
+        nx = load_back<E, I>(xr, o);
+        nd = load_back<E, I>(dr, o);
+        nz = load_back<E, I>(zr, o);
     };
     if (parts > 0) {
         fetch(0);
@@ -371,13 +413,20 @@ __global__ __launch_bounds__(kThreads, 4) void scan_forward_kernel(ScanArgs a) {
         const float *tb = tiles.of(part), *tc = tb + a.N * P;
         if (part + 1 < parts)
             tiles.store(part + 1);
-        float x[I], z[I], delta[T], dx[T], y[T], sum = 0.0f;
+        float x[I], z[I], dt[I], delta[T], dx[T], y[T], sum = 0.0f;
         float *q = mine + slot_at<T>(pos);   // I neighbours of one slot
+        if (p0 + P <= n_pos) {
+            convert<E, I>(nx, x);
+            convert<E, I>(nz, z);
+            convert<E, I>(nd, dt);
+        } else {
+            settle<E, I>(nx, p0 + pos, a.L, n_pos, x);
+            settle<E, I>(nz, p0 + pos, a.L, n_pos, z);
+            settle<E, I>(nd, p0 + pos, a.L, n_pos, dt);
+        }
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            x[i] = (float)nx[i];
-            z[i] = (float)nz[i];
-            float v = (float)nd[i] + bias;
+            float v = dt[i] + bias;
             if (a.softplus)
                 v = softplus(v);
             v = keep_if(i < left, v);
@@ -464,6 +513,170 @@ __global__ __launch_bounds__(kThreads, 4) void scan_forward_kernel(ScanArgs a) {
             if (dd < a.Dg)
                 a.state_out[((long long)b * a.D + grp * a.Dg + dd) * a.N + n] = hs[i];
         }
+}
+
+// ---- short rasters -------------------------------------------------------------------
+// A scan over lanes would leave most of them past the raster's end.  Four lanes a
+// channel, a quarter of the states each, go through the positions in order: each lane
+// prepares every fourth four of them, which the others take from it by DPP, and adds up
+// its states' share of y, which the four sum.  A position then takes, a lane, the
+// exponential, 2 multiplies and 2 multiply-adds of each of its S states: 64 x 2048
+// channels of 16 positions, N = 16, bf16, 15 us (their bytes 7; the scan over lanes 168).
+template <int K>
+__device__ inline float from_quad(float v) {   // lane K of each four
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
+                                         0, __builtin_bit_cast(int, v), K * 0x55, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ inline float add_quad(float v) {
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
+                                             0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+
+// Positions 4 K to 4 K + 3 of the 16 that the lanes prepared.
+template <int S, int K, bool ALL>
+__device__ inline void short_four(const float *tb, const float *tc, const float (&delta)[4],
+                                  const float (&dx)[4], const float (&A2)[S], int states,
+                                  float (&h)[S], bool own, float (&y)[4]) {
+    // as many positions side by side as the registers hold
+    constexpr int W = S <= 4 ? 4 : S == 8 ? 2 : 1;
+#pragma unroll
+    for (int j0 = 0; j0 < 4; j0 += W) {
+        float Bv[W][S], Cv[W][S], av[W][S], v[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            lds_load<S>(tb + (4 * K + j0 + j) * 4 * S, Bv[j]);
+            lds_load<S>(tc + (4 * K + j0 + j) * 4 * S, Cv[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const float de = from_quad<K>(delta[j0 + j]), u = from_quad<K>(dx[j0 + j]);
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                av[j][s] = __builtin_amdgcn_exp2f(A2[s] * de);
+                Bv[j][s] *= u;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            v[j] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                h[s] = __builtin_fmaf(av[j][s], h[s], Bv[j][s]);
+                if (!ALL)
+                    h[s] = keep_if(s < states, h[s]);   // 0 times an infinite input is NaN
+                v[j] = __builtin_fmaf(Cv[j][s], h[s], v[j]);
+            }
+        }
+        // over the four lanes
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            v[j] = add_quad<0xb1>(v[j]);
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            v[j] = add_quad<0x4e>(v[j]);
+            y[j0 + j] = own ? v[j] : y[j0 + j];
+        }
+    }
+}
+
+constexpr int kShortThreads = 256;
+
+// 2^keep positions are a part of the gradients', at whose start the states are kept.
+// ALL: N = 4 S.
+template <typename E, int S, bool ALL>
+__global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a, int keep) {
+    constexpr int NP = 4 * S;
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    const int tid = threadIdx.x, q = tid & 3, n0 = q * S, CB = blockDim.x / 4;
+    int blk = blockIdx.x;
+    const int cb = blk % a.blocks;
+    blk /= a.blocks;
+    const int grp = blk % a.G, b = blk / a.G;
+    const bool live = cb * CB + tid / 4 < a.Dg;
+    const int d = grp * a.Dg + (live ? cb * CB + tid / 4 : 0);
+    const int n_pos = __builtin_amdgcn_readfirstlane(row_length(a.lengths, b, a.L));
+    const int rounds = (n_pos + 15) / 16;
+    float *tb = lds, *tc = lds + rounds * 16 * NP;
+    const E *xr = a.x.row<const E>(b, d) + 4 * q, *dr = a.dt.row<const E>(b, d) + 4 * q;
+    const E *zr = a.z.p ? a.z.row<const E>(b, d) + 4 * q : xr;
+    typename Vec<E, 4>::type nx, nd, nz;
+    auto fetch = [&](int p0) {
+        const int left = n_pos - p0 - 4 * q;
+        const bool whole = p0 + 16 <= n_pos;
+        nx = load_raw<E, 4>(xr + p0, left, whole);
+        nd = load_raw<E, 4>(dr + p0, left, whole);
+        nz = load_raw<E, 4>(zr + p0, left, whole);
+    };
+    if (rounds > 0)
+        fetch(0);
+    float h[S], A2[S];
+    const long long at0 = ((long long)b * a.D + d) * a.N + n0;
+    load_upto<float, S>(a.A + (long long)d * a.N + n0, a.N - n0, A2);
+    load_upto<float, S>(a.state + at0, a.state ? a.N - n0 : 0, h);
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+        A2[s] *= kLog2e;
+    const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
+    const float skip = a.Dskip ? a.Dskip[d] : 0.0f;
+    // B and C of all positions, position by position; 0 past the raster and the states
+    for (int u = tid; u < 2 * rounds * 4 * NP; u += blockDim.x) {
+        const int n = u % NP, t = u / NP % (rounds * 4) * 4;
+        const bool isC = u >= rounds * 4 * NP;
+        const E *row = (isC ? a.Cm : a.Bm).row<const E>(b, (long long)grp * a.N + n);
+        float v[4];
+        load_upto<E, 4>(row + t, n < a.N ? n_pos - t : 0, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            (isC ? tc : tb)[(t + i) * NP + n] = v[i];
+    }
+    __syncthreads();
+    for (int k = 0; k < rounds; ++k) {
+        const int p0 = 16 * k, left = n_pos - p0 - 4 * q;
+        float x[4], z[4], delta[4], dx[4], y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = (float)nx[i];
+            z[i] = (float)nz[i];
+            float v = (float)nd[i] + bias;
+            if (a.softplus)
+                v = softplus(v);
+            delta[i] = keep_if(i < left, v);
+            dx[i] = delta[i] * x[i];
+            y[i] = 0.0f;
+            asm volatile("" : "+v"(x[i]), "+v"(z[i]));   // before the next loads
+        }
+        if (k + 1 < rounds)
+            fetch(p0 + 16);
+        if (a.states && live && (p0 >> keep << keep) == p0)
+            store_upto<float, S>(
+                a.states + (((long long)b * a.D + d) * a.parts + (p0 >> keep)) * NP + n0, S, h);
+        const float *bp = tb + p0 * NP + n0, *cp = tc + p0 * NP + n0;
+        short_four<S, 0, ALL>(bp, cp, delta, dx, A2, a.N - n0, h, q == 0, y);
+        if (p0 + 4 < n_pos)
+            short_four<S, 1, ALL>(bp, cp, delta, dx, A2, a.N - n0, h, q == 1, y);
+        if (p0 + 8 < n_pos)
+            short_four<S, 2, ALL>(bp, cp, delta, dx, A2, a.N - n0, h, q == 2, y);
+        if (p0 + 12 < n_pos)
+            short_four<S, 3, ALL>(bp, cp, delta, dx, A2, a.N - n0, h, q == 3, y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            y[i] = __builtin_fmaf(skip, x[i], y[i]);
+            if (a.z.p)
+                y[i] *= silu(z[i]);
+            y[i] = keep_if(i < left, y[i]);
+        }
+        if (live)
+            store_upto<E, 4>(a.y.row<E>(b, d) + p0 + 4 * q, a.L - p0 - 4 * q, y);
+    }
+    if (!live)
+        return;
+    // padding
+    const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t = rounds * 16 + 4 * q; t < a.L; t += 16)
+        store_upto<E, 4>(a.y.row<E>(b, d) + t, a.L - t, none);
+    if (a.state_out)
+        store_upto<float, S>(a.state_out + at0, a.N - n0, h);
 }
 
 // ---- gradients ----------------------------------------------------------------------
@@ -566,21 +779,13 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
     Raw nx, nd, ng, nz;
     float nin[S];
     auto fetch = [&](int c, int part) {
-        const int d = (int)first + c, p0 = part * P, left = n_pos - p0 - pos;
-        const E *xr = a.x.row<const E>(b, d) + p0, *dr = a.dt.row<const E>(b, d) + p0;
-        const E *gr = ga.dy.row<const E>(b, d) + p0;
-        const E *zr = a.z.p ? a.z.row<const E>(b, d) + p0 : gr;
-        if (p0 + P <= n_pos) {
-            nx = load_whole<E, I>(at(xr, pos));
-            nd = load_whole<E, I>(at(dr, pos));
-            ng = load_whole<E, I>(at(gr, pos));
-            nz = load_whole<E, I>(at(zr, pos));
-        } else {
-            nx = load_part<E, I>(at(xr, pos), left);
-            nd = load_part<E, I>(at(dr, pos), left);
-            ng = load_part<E, I>(at(gr, pos), left);
-            nz = load_part<E, I>(at(zr, pos), left);
-        }
+        const int d = (int)first + c;
+        const unsigned o = back<E, I>(part * P + pos, a.L);
+        const E *gr = ga.dy.row<const E>(b, d), *zr = a.z.p ? a.z.row<const E>(b, d) : gr;
+        nx = load_back<E, I>(a.x.row<const E>(b, d), o);
+        nd = load_back<E, I>(a.dt.row<const E>(b, d), o);
+        ng = load_back<E, I>(gr, o);
+        nz = load_back<E, I>(zr, o);
         load_vec<float, S>(at(a.states + (((long long)b * a.D + d) * a.parts + part) * NP, n0), nin);
     };
     const int units = 2 * a.N * (P / kUnit);
@@ -593,9 +798,10 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
     for (int part = parts - 1; part >= 0; --part) {
         const int p0 = part * P;
         if (tid < units)
-            store_tile<E, T>(tb, tc, a.N, tid, nt);
+            store_tile<E, T>(a, tb, tc, tid, p0, n_pos, nt);
         for (int u = tid + TH; u < units; u += TH)
-            store_tile<E, T>(tb, tc, a.N, u, load_tile<E, T>(a, b, grp, u, p0, n_pos));
+            store_tile<E, T>(a, tb, tc, u, p0, n_pos,
+                             load_tile<E, T>(a, b, grp, u, p0, n_pos));
         __syncthreads();
         nt = load_tile<E, T>(a, b, grp, min(tid, units - 1), max(p0 - P, 0), n_pos);
         float dB[S][T], dC[S][T];
@@ -606,16 +812,25 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
                 dB[s][j] = dC[s][j] = 0.0f;
         for (int c = wave; c < count; c += kGradWaves) {
             const int d = (int)first + c, left = n_pos - p0 - pos;
-            float x[I], delta[I], slope[I], z[I], dout[I], dy[I], in[S], A2[S], end[S], dA[S];
+            float x[I], dt[I], delta[I], slope[I], z[I], dout[I], dy[I], in[S], A2[S], end[S], dA[S];
             const float bias = vec[2 * c], skip = vec[2 * c + 1];
+            if (p0 + P <= n_pos) {
+                convert<E, I>(nx, x);
+                convert<E, I>(nd, dt);
+                convert<E, I>(ng, dout);
+                convert<E, I>(nz, z);
+            } else {
+                settle<E, I>(nx, p0 + pos, a.L, n_pos, x);
+                settle<E, I>(nd, p0 + pos, a.L, n_pos, dt);
+                settle<E, I>(ng, p0 + pos, a.L, n_pos, dout);
+                settle<E, I>(nz, p0 + pos, a.L, n_pos, z);
+            }
 #pragma unroll
             for (int i = 0; i < I; ++i) {
-                const float v = (float)nd[i] + bias;
-                x[i] = (float)nx[i];
-                dout[i] = (float)ng[i];
+                const float v = dt[i] + bias;
                 slope[i] = a.softplus ? sigmoid(v) : 1.0f;
                 delta[i] = keep_if(i < left, a.softplus ? softplus(v) : v);
-                z[i] = a.z.p ? (float)nz[i] : 0.0f;
+                z[i] = a.z.p ? z[i] : 0.0f;
                 dy[i] = a.z.p ? dout[i] * silu(z[i]) : dout[i];
                 float *q = mine + slot_at<T>(pos + i);
                 q[0] = delta[i];
@@ -975,6 +1190,42 @@ int launch_forward(ScanArgs &c, hipStream_t s) {
     return launched();
 }
 
+// Positions of a raster that the short form takes, however many rows there are: the bits
+// do not depend on them.  In us, here and by the scan over lanes: 64 positions of 64 x
+// 2048 channels 47 and 137, of 4 x 1024 12 and 7; 32 of those 7.2 and 8.2; but 128 of
+// them 20 and 8.
+constexpr int kShort = 64;
+
+template <typename E, int S, bool ALL>
+int launch_short(ScanArgs &c, hipStream_t s) {
+    // a wave a workgroup where whole ones would leave compute units without work
+    const int threads =
+        (long long)c.B * c.D >= 1024ll * kShortThreads / 4 ? kShortThreads : 64;
+    c.blocks = (int)cdivll(c.Dg, threads / 4);
+    const long long grid = (long long)c.blocks * c.G * c.B;
+    static_assert(2 * 4 * 16 * kShort * sizeof(float) <= 64 * 1024, "B and C in LDS");
+    const size_t lds = (size_t)2 * 4 * S * cdivll(c.L, 16) * 16 * sizeof(float);
+    if (grid >= (1ll << 31))
+        return FINC_EUNSUPPORTED;
+    (void)hipGetLastError();   // the launch check decides
+    hipLaunchKernelGGL((scan_short_kernel<E, S, ALL>), dim3((unsigned)grid), dim3(threads),
+                       (unsigned)lds, s, c, lane_positions(c.L, c.N) == 4 ? 6 : 7);
+    return launched();
+}
+template <typename E, int S>
+int launch_short(ScanArgs &c, hipStream_t s) {
+    return c.N == 4 * S ? launch_short<E, S, true>(c, s) : launch_short<E, S, false>(c, s);
+}
+template <typename E>
+int dispatch_short(ScanArgs &c, hipStream_t s) {
+    const int S = row_states(c.N);
+    return S == 1   ? launch_short<E, 1>(c, s)
+           : S == 2 ? launch_short<E, 2>(c, s)
+           : S == 4 ? launch_short<E, 4>(c, s)
+           : S == 8 ? launch_short<E, 8>(c, s)
+                    : launch_short<E, 16>(c, s);
+}
+
 // The parts of the arguments that both directions check and use.
 bool scan_common(const finc_scan_args *a, ScanArgs &c) {
     c = ScanArgs{};
@@ -1098,8 +1349,9 @@ int finc_selective_scan_forward(const finc_scan_args *a, hipStream_t stream) {
     int rc = FINC_EINVAL;
     with_type(a->type, [&](auto e) {
         typedef decltype(e) E;
-        rc = lane_positions(L, a->N) == 4 ? launch_forward<E, 4>(c, stream)
-                                          : launch_forward<E, 8>(c, stream);
+        rc = L <= kShort                    ? dispatch_short<E>(c, stream)
+             : lane_positions(L, a->N) == 4 ? launch_forward<E, 4>(c, stream)
+                                            : launch_forward<E, 8>(c, stream);
     });
     return rc;
 }

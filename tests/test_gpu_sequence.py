@@ -263,6 +263,60 @@ def test_scan_forward_and_gradients(B, D, L, N, G, opt, kind, view):
             assert grads[key[k]] is None
 
 
+SHORT = [  # short rasters and last parts of every length, rows that end before them
+    (3, 37, 3, 16, 1, "gsldbp", BF16, None),
+    (2, 70, 4, 1, 1, "gsdbp", F32, "odd"),
+    (4, 20, 8, 5, 2, "gsldbp", F16, "half"),
+    (2, 66, 15, 64, 1, "gsdbp", F32, None),
+    (3, 18, 16, 2, 1, "sldp", BF16, "odd"),
+    (5, 33, 17, 16, 3, "gsldbp", F32, None),
+    (2, 64, 31, 33, 1, "gdbp", F16, None),
+    (6, 24, 49, 7, 2, "gsldbp", BF16, "half"),
+    (130, 505, 20, 8, 1, "gsldbp", BF16, None),   # whole workgroups
+    (5, 10, 66, 16, 1, "gsldbp", F32, "odd"),
+    (5, 10, 71, 16, 2, "gsldbp", BF16, "odd"),
+    (4, 9, 133, 40, 1, "gsldbp", F16, "half"),
+    (6, 9, 135, 16, 1, "gsldbp", F32, None),
+    (5, 8, 257, 9, 2, "sldbp", BF16, "odd"),
+]
+
+
+@pytest.mark.parametrize("B,D,L,N,G,opt,kind,view", SHORT)
+def test_scan_short_rasters_and_ends(B, D, L, N, G, opt, kind, view):
+    test_scan_forward_and_gradients(B, D, L, N, G, opt, kind, view)
+
+
+@pytest.mark.parametrize("L,N", [(1, 3), (20, 5), (20, 16), (40, 33)])
+def test_scan_infinite_inputs_stay_infinite(L, N):
+    """An infinite input's row, N filling its lanes or not: the formula's values in a
+    short raster (in a longer one the lanes' maps may multiply it by 0)."""
+    t, _, _ = scan_inputs(2, 6, L, N, 1, "sdbp", F32, L + N)
+    t["Bm"], t["Cm"] = t["Bm"].abs() + 0.1, t["Cm"].abs() + 0.1
+    t["x"][0, 2, L // 2] = float("inf")
+    t["x"][1, 3, L - 1] = -float("inf")
+    t["D"] = t["D"].abs() + 0.1
+    g, kw = scan_kw(t, None, "sdbp", None)
+    end = torch.empty(2, 6, N, device=DEV)
+    y = finc.selective_scan_forward(**g, **kw, state_out=end)
+    yr, er = ref.scan(**{k: d64(v) if v is not None else None for k, v in t.items()},
+                      softplus=True, lengths=None)
+    assert bool(torch.isinf(yr).any()) and bool(torch.isinf(er).any())
+    ref.close(y, yr, "y", 64 + 2 * L ** 0.5)
+    ref.close(end, er, "state after", 64 + 2 * L ** 0.5)
+
+
+def test_scan_bits_of_short_rasters_do_not_depend_on_the_number_of_rows():
+    t, _, _ = scan_inputs(1, 520, 40, 16, 2, "gsdbp", BF16, 11)
+    g, kw = scan_kw(t, None, "gsdbp", None)
+    one = finc.selective_scan_forward(**g, **kw)
+    wide = {k: v.expand(130, *v.shape[1:]) if k in ("x", "dt", "Bm", "Cm", "z") else v
+            for k, v in g.items()}
+    many = dict(kw, state=kw["state"].expand(130, 520, 16).contiguous())
+    assert torch.equal(finc.selective_scan_forward(**wide, **many), one.expand(130, 520, 40))
+    states = finc.selective_scan_states(1, 520, 40, 16, DEV)
+    assert torch.equal(finc.selective_scan_forward(**g, **kw, states=states), one)
+
+
 def test_scan_gradients_are_the_differences():
     """The change of the fp32 forward along a direction, against the gradients."""
     t, n, r = scan_inputs(2, 12, 90, 16, 2, "gsdbp", F32, 5)
