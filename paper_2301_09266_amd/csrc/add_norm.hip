@@ -199,19 +199,61 @@ struct NormArgs {
     Drop drop;
 };
 
+// Eight elements of a row from c on as they lie in memory, or its last eight where they
+// would pass its end: all of a row's loads are under way before settle8() waits for the
+// first, and the row's end is one load, not eight.  16384 x 2063 in bf16: 56 us forward and
+// 103 the gradients, 73 and 126 with elements one by one and each vector waited for.
+// TINY: rows of fewer than eight.
+constexpr int kTinyThreads = 128;   // of a workgroup for them, and for no other rows
+template <typename E>
+using Raw8 = typename Vec<E, 8>::type;
+template <bool TINY, typename E>
+__device__ inline Raw8<E> load8(const E *row, int c, int D) {
+    Raw8<E> t = {};
+    if (!TINY) {
+        if (c < D)   // lanes past the end would only load again what others do
+            t = *(const Raw8<E> *)(row + min(c, D - 8));
+        return t;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        t[i] = row[min(i, D - 1)];
+    return t;
+}
+// Those of load8 at their places, 0 past the row's end.
+template <bool TINY, typename E>
+__device__ inline void settle8(Raw8<E> t, int c, int D, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = (float)t[i];
+    if (TINY) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = keep_if(c + i < D, v[i]);
+    } else if (c + 8 > D) {
+        const int by = afresh(min(c + 8 - D, 8));
+#pragma unroll
+        for (int h = 8; h; h >>= 1)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                v[i] = by & h ? (i + h < 8 ? v[i + h < 8 ? i + h : 0] : 0.0f) : v[i];
+    }
+}
+
 // R lanes a row, V vectors of 8 a lane: vector v of a lane is lane + v R.  Bound by
 // memory: 32768 x 2048 in bf16 with an fp32 residual and dropout 150 us, 805 MB at 5.4
 // TB/s (the last-level cache holds some of them; a copy of 2 GiB reaches 4.8).
 template <typename E, typename F, int R, int V, int TH>
 __global__ __launch_bounds__(TH) void norm_forward_kernel(NormArgs a) {
     __shared__ unsigned lds[2 * (TH / 64)];
+    constexpr bool kTiny = TH == kTinyThreads;
     const int lane = threadIdx.x % R;
     int turn_of = 0;
     float w[V][8];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int c = (lane + v * R) * 8;
-        load_upto<float, 8>(a.w + c, a.D - c, w[v]);
+        settle8<kTiny, float>(load8<kTiny>(a.w, c, a.D), c, a.D, w[v]);
     }
     const float mean = 1.0f / (float)a.D, eps = (float)a.eps;
     const long long step = (long long)gridDim.x * (TH / R);
@@ -224,19 +266,24 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(NormArgs a) {
         float r[V][8], ss = 0.0f;
         const E *x = (const E *)a.x + m * a.sx;
         const F *res = a.res ? (const F *)a.res + m * a.sres : nullptr;
+        Raw8<E> tx[V];
+        Raw8<F> tr[V] = {};
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            tx[v] = load8<kTiny>(x, (lane + v * R) * 8, a.D);
+        if (res)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                tr[v] = load8<kTiny>(res, (lane + v * R) * 8, a.D);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = (lane + v * R) * 8;
-            load_upto<E, 8>(x + c, a.D - c, r[v]);
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = (lane + v * R) * 8;
+            settle8<kTiny, E>(tx[v], c, a.D, r[v]);
             if (a.drop.cut && c < a.D)
                 drop(a.drop, (unsigned long long)m * a.per + (lane + v * R), r[v]);
             if (res) {
                 float t[8];
-                load_upto<F, 8>(res + c, a.D - c, t);
+                settle8<kTiny, F>(tr[v], c, a.D, t);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     r[v][i] += t[i];
@@ -385,7 +432,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(NormArgs a) {
     constexpr int GR = TH / R;   // rows at a time
     __shared__ __attribute__((aligned(16))) float sums[GR > 1 ? TH * V * 8 : 8];
     // w and dy in registers; the widest rows read them again, which come from L2
-    constexpr bool kKeep = V == 1;
+    constexpr bool kKeep = V == 1, kTiny = TH == kTinyThreads;
     const int lane = threadIdx.x % R;
     int turn_of = 0;
     float w[V][8], dw[V][8];
@@ -411,12 +458,22 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(NormArgs a) {
         const F *rr = (const F *)a.res + m * a.sres;
         const E *dy = (const E *)a.x + m * a.sx;
         const F *dr = a.dr ? (const F *)a.dr + m * a.sdr : nullptr;
+        // with two vectors a lane its registers are better left to a fourth wave a SIMD
+        // (32768 x 1000 in bf16: 59 us, and 88 with the loads ahead)
+        Raw8<F> td = {};
+        if constexpr (kKeep) {
+            const Raw8<F> tr = load8<kTiny>(rr, lane * 8, a.D);
+            const Raw8<E> tg = load8<kTiny>(dy, lane * 8, a.D);
+            if (dr)
+                td = load8<kTiny>(dr, lane * 8, a.D);
+            settle8<kTiny, F>(tr, lane * 8, a.D, r[0]);
+            settle8<kTiny, E>(tg, lane * 8, a.D, g[0]);
+        } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = (lane + v * R) * 8;
-            load_upto<F, 8>(rr + c, a.D - c, r[v]);
-            if (kKeep)
-                load_upto<E, 8>(dy + c, a.D - c, g[v]);
+            for (int v = 0; v < V; ++v) {
+                const int c = (lane + v * R) * 8;
+                load_upto<F, 8>(rr + c, a.D - c, r[v]);
+            }
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -441,7 +498,9 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(NormArgs a) {
         for (int v = 0; v < V; ++v) {
             const int c = (lane + v * R) * 8;
             float o[8];
-            if (dr)
+            if (kKeep && dr)
+                settle8<kTiny, F>(td, c, a.D, o);
+            else if (dr)
                 load_upto<F, 8>(dr + c, a.D - c, o);
             if (!kKeep) {
                 load_upto<float, 8>(wr + c, a.D - c, w[v]);
@@ -578,7 +637,7 @@ enum { kForward, kFp8, kBackward };
 // forward holds little an element, so more vectors a lane spare it barriers.  The
 // gradients hold three values an element and w and their sums in fp64, and the 8-bit
 // output fp64 values: above 1024 one vector a lane, up to a whole workgroup a row
-// (gradients of 32768 x 2048 in bf16: 126 us; 276 with four vectors in each lane of a
+// (gradients of 32768 x 2048 in bf16: 115 us; 276 with four vectors in each lane of a
 // wave a row, whose registers leave a wave a SIMD.  8 bits: 137 us and 185).  Up to
 // 1024 a wave a row, two vectors a lane: with four waves a row a width just below fills
 // two of them (32768 x 1000 in bf16: gradients 63 us and 103, 8 bits 56 and 130).
@@ -587,6 +646,8 @@ void with_width(int D, Fn fn) {
 #define FINC_WIDTH(r, v, th)                                                              \
     return fn(E(), F(), std::integral_constant<int, r>(), std::integral_constant<int, v>(), \
               std::integral_constant<int, th>())
+    if (D < 8)
+        FINC_WIDTH(16, 1, kTinyThreads);
     if (D <= 128)
         FINC_WIDTH(16, 1, 256);
     if (D <= 512)
@@ -614,7 +675,8 @@ void with_width(int D, Fn fn) {
 
 // Workgroups that walk the rows of a gradient, a partial sum of dw each: four waves a
 // SIMD, which the registers allow (32768 x 2048: 126 us, and 192 with half of them; 8192
-// x 8192, whose workgroups are 16 waves: 127 us with 512 and 157 with 2048).
+// x 8192, whose workgroups are 16 waves: 127 us with 512 and 157 with 2048; 115 and 114
+// since a row's loads are under way together).
 inline int grad_blocks(int M, int D) {
     const long long blocks = cdivll(M > 0 ? M : 1, D <= 128 ? 16 : D <= 1024 ? 4 : 1);
     const long long most = D <= 2048 ? 1024 : 512;

@@ -92,17 +92,35 @@ __device__ inline void store_vec(E *p, const float *v) {
     }
 }
 
+// The first n < N of N elements, N a power of two.
+template <typename E, int N>
+__device__ inline void store_bits(E *p, int n, const float *v) {
+    if constexpr (N > 1) {
+        constexpr int H = N / 2;
+        float u[H];
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+            u[i] = v[i];
+        if (n & H) {
+            store_vec<E, H>(p, v);
+            p += H;
+#pragma unroll
+            for (int i = 0; i < H; ++i)
+                u[i] = v[i + H];
+        }
+        store_bits<E, H>(p, n, u);
+    }
+}
 template <typename E, int N>
 __device__ inline void store_upto(E *p, int count, const float *v) {
     if (count >= N) {
         store_vec<E, N>(p, v);
         return;
     }
+    // a half, a quarter and so on, each where the count has it
     const int n = afresh(count);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (i < n)
-            p[i] = (E)v[i];
+    if (n > 0)
+        store_bits<E, N>(p, n, v);
 }
 
 // ---- activations ----------------------------------------------------------------
