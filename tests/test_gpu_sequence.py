@@ -504,6 +504,28 @@ def test_norm_in_place():
     assert a is not b and torch.equal(a, want) and torch.equal(b, want)
 
 
+@pytest.mark.parametrize("D", [9, 131, 515, 1030, 2063, 4099, 8201])
+def test_norm_in_place_over_rows_of_many_waves(D):
+    """The last elements of a row are loaded with some of the neighbouring wave's."""
+    r = Rand(D)
+    x, res, dr = (r.normal(70, D, kind=BF16).to(DEV) for _ in range(3))
+    w = 1 + r.normal(D, scale=0.1).to(DEV)
+    y, s = finc.add_norm_forward(x, w, res)
+    dx, dres, dw = finc.add_norm_backward(x, s, w, dr, p=0.1, seed=4)
+    y8, scale, _ = finc.add_norm_forward(x, w, res, fp8=True)
+    for _ in range(3):
+        x2, res2 = x.clone(), res.clone()
+        finc.add_norm_forward(x2, w, res2, out=x2, residual_out=res2)
+        assert torch.equal(x2, y) and torch.equal(res2, s)
+        x2, dr2 = x.clone(), dr.clone()
+        dw2 = finc.add_norm_backward(x2, s, w, dr2, p=0.1, seed=4, dx=x2, dresidual=dr2)[2]
+        assert torch.equal(x2, dx) and torch.equal(dr2, dres) and torch.equal(dw2, dw)
+        res2 = res.clone()
+        got8, scale2, _ = finc.add_norm_forward(x, w, res2, fp8=True, residual_out=res2)
+        assert torch.equal(got8.view(torch.uint8), y8.view(torch.uint8))
+        assert torch.equal(scale2, scale) and torch.equal(res2, s)
+
+
 @pytest.mark.parametrize("M,D,kind", [(1, 5, F32), (40, 64, BF16), (9, 1000, BF16), (7, 2048, F16),
                                       (3, 5000, F32), (2, 16384, BF16)])
 def test_norm_in_eight_bits(M, D, kind):
