@@ -21,8 +21,9 @@ template <int K>
 constexpr int kHalo = K <= 1 ? 1 : K <= 2 ? 1 : K <= 3 ? 2 : K <= 5 ? 4 : 8;
 
 // Elements a thread takes: 16 bytes forward; twice that for the gradients, which
-// recompute K - 1 gradients beside them (8 x 2048 x 4096 in bf16, K 4: 106 us, and 132
-// with 16 bytes; 300 x 9000, where few threads are left, 11.2 and 9.4).
+// recompute K - 1 gradients beside them (8 x 2048 x 4096 in bf16, K 4: 113 us, and 132
+// with 16 bytes; 300 x 9000, where few threads are left, 11.2 and 9.4; with the loads
+// together 94 and 12.0).
 constexpr int kTileBytes(bool back) { return back ? 32 : 16; }
 template <typename E, bool BACK>
 constexpr int kTile = kTileBytes(BACK) / (int)sizeof(E);
@@ -44,13 +45,25 @@ __device__ inline int row_length(const int *lengths, int b, int L) {
     return lengths ? min(max(lengths[b], 0), L) : L;
 }
 
-// H elements before t0 of one row: of x, of the state (K - 1 elements) or 0.
+// N elements as they lie in memory, 0 in lanes where `ok` is false.  The loads of a tile
+// are all under way before the first is converted.
+template <typename E, int N>
+__device__ inline typename Vec<E, N>::type load_raw(const E *p, bool ok) {
+    typename Vec<E, N>::type v = {};
+    if (ok)
+        v = *(const typename Vec<E, N>::type *)p;
+    return v;
+}
+template <typename E, int N>
+__device__ inline void convert(typename Vec<E, N>::type t, float *v) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        v[i] = (float)t[i];
+}
+
+// The H elements before t0 < H: of x, of the state (K - 1 elements) or 0.
 template <typename E, int K, int H>
-__device__ inline void load_before(const E *x, const E *state, int t0, float *v) {
-    if (t0 >= H) {
-        load_vec<E, H>(x + (t0 - H), v);
-        return;
-    }
+__device__ inline void load_first(const E *x, const E *state, int t0, float *v) {
 #pragma unroll
     for (int i = 0; i < H; ++i) {
         const int t = t0 - H + i;
@@ -77,13 +90,20 @@ __global__ __launch_bounds__(kThreads) void conv_forward_kernel(ConvArgs a) {
         return;
     const int t0 = (int)t0l;
     float v[H + V], y[V];
-    load_before<E, K, H>(x, state, t0, v);
-    load_upto<E, V>(x + t0, a.L - t0, v + H);
+    const bool whole = t0 + V <= a.L;
+    const auto before = load_raw<E, H>(x + (t0 - H), t0 >= H);
+    const auto tile = load_raw<E, V>(x + t0, whole);
     const float bias = a.bias ? a.bias[d] : 0.0f;
     float w[K];
 #pragma unroll
     for (int j = 0; j < K; ++j)
         w[j] = a.w[(long long)d * K + j];
+    convert<E, H>(before, v);
+    convert<E, V>(tile, v + H);
+    if (t0 < H)
+        load_first<E, K, H>(x, state, t0, v);
+    if (!whole)
+        load_upto<E, V>(x + t0, a.L - t0, v + H);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         float p = bias;
@@ -105,7 +125,8 @@ __global__ __launch_bounds__(kThreads) void conv_forward_kernel(ConvArgs a) {
 
 // One channel and a part of its (row, tile) pairs: dx of the part, and the part's
 // sums for dw and dbias, which stay in registers until the part ends.  Bound by memory:
-// 8 x 2048 x 4096 in bf16, K 4, in 106 us, 3.8 TB/s.
+// 8 x 2048 x 4096 in bf16, K 4, in 94 us, 4.3 TB/s (111 with each load waited for by
+// itself).
 template <typename E, int K, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
     constexpr int V = kTile<E, true>, H = kHalo<K>, Q = K - 1;
@@ -134,11 +155,26 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
         const E *state = a.state ? (const E *)a.state + row * Q : nullptr;
         const E *dso = a.dstate_out ? (const E *)a.dstate_out + row * Q : nullptr;
         float v[H + V + H], g[V + H];
-        load_before<E, K, H>(x, state, t0, v);
-        load_upto<E, V>(x + t0, a.L - t0, v + H);
-        load_upto<E, H>(x + t0 + V, a.L - t0 - V, v + H + V);
-        load_upto<E, V>(dy + t0, a.L - t0, g);
-        load_upto<E, H>(dy + t0 + V, a.L - t0 - V, g + V);
+        {
+            const bool whole = t0 + V <= a.L, more = t0 + V + H <= a.L;
+            const auto before = load_raw<E, H>(x + (t0 - H), t0 >= H);
+            const auto xt = load_raw<E, V>(x + t0, whole), gt = load_raw<E, V>(dy + t0, whole);
+            const auto xa = load_raw<E, H>(x + t0 + V, more), ga = load_raw<E, H>(dy + t0 + V, more);
+            convert<E, H>(before, v);
+            convert<E, V>(xt, v + H);
+            convert<E, H>(xa, v + H + V);
+            convert<E, V>(gt, g);
+            convert<E, H>(ga, g + V);
+            if (t0 < H)
+                load_first<E, K, H>(x, state, t0, v);
+            if (!whole) {
+                load_upto<E, V>(x + t0, a.L - t0, v + H);
+                load_upto<E, V>(dy + t0, a.L - t0, g);
+            } else if (!more && t0 + V < a.L) {
+                load_upto<E, H>(x + t0 + V, a.L - t0 - V, v + H + V);
+                load_upto<E, H>(dy + t0 + V, a.L - t0 - V, g + V);
+            }
+        }
         // padding may hold anything, also to the left of a tile that lies in it
         if (t0 + V + H > n) {
 #pragma unroll
