@@ -175,15 +175,6 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
                 load_upto<E, H>(dy + t0 + V, a.L - t0 - V, g + V);
             }
         }
-        // padding may hold anything, also to the left of a tile that lies in it
-        if (t0 + V + H > n) {
-#pragma unroll
-            for (int i = 0; i < H + V + H; ++i)
-                v[i] = keep_if(t0 - H + i < n, v[i]);
-#pragma unroll
-            for (int i = 0; i < V + H; ++i)
-                g[i] = keep_if(t0 + i < n, g[i]);
-        }
         if (SILU) {
 #pragma unroll
             for (int i = 0; i < V + Q; ++i) {
@@ -193,10 +184,11 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
                     p = __builtin_fmaf(w[j], v[H - Q + i + j], p);
                 g[i] *= silu_grad(p, sigmoid(p));
             }
-            if (t0 + V + H > n)   // 0 times a gradient that has no value
+        }
+        if (t0 + V + H > n) {   // padding may hold anything
 #pragma unroll
-                for (int i = 0; i < V + Q; ++i)
-                    g[i] = keep_if(t0 + i < n, g[i]);
+            for (int i = 0; i < V + H; ++i)
+                g[i] = keep_if(t0 + i < n, g[i]);
         }
         float dx[V];
 #pragma unroll
@@ -206,10 +198,27 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
             for (int j = 0; j < K; ++j)
                 s = __builtin_fmaf(w[j], g[i + Q - j], s);
             dx[i] = s;
-            db += g[i];
+        }
+        // Padding adds nothing, not even 0 times the inputs before it, which may be infinite
+        // or NaN: an empty row's state, the row's last inputs, padding itself.
+        if (t0 + V <= n) {
 #pragma unroll
-            for (int j = 0; j < K; ++j)
-                dw[j] = __builtin_fmaf(g[i], v[H - Q + i + j], dw[j]);
+            for (int i = 0; i < V; ++i) {
+                db += g[i];
+#pragma unroll
+                for (int j = 0; j < K; ++j)
+                    dw[j] = __builtin_fmaf(g[i], v[H - Q + i + j], dw[j]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                db += g[i];
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    const float s = __builtin_fmaf(g[i], v[H - Q + i + j], dw[j]);
+                    dw[j] = t0 + i < n ? s : dw[j];
+                }
+            }
         }
         if (t0 + V + Q > n) {
 #pragma unroll

@@ -1,0 +1,63 @@
+"""The sequence operators where inputs, sizes and layouts are at their ends: empty
+rows beside others, infinities, magnitudes, the 8-bit norm code for code, outputs in
+other orders, streams, launches and offsets past 32 bits."""
+import pytest
+import torch
+
+import seq_ref as ref
+from gpu_util import DEV
+from paper_2301_09266_amd import finc
+from test_gpu_sequence import BF16, F16, F32, NAN, Rand, d64, dev
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+def grads(loss, leaves):
+    """Gradients of float64 leaves, 0 where the loss does not depend on one."""
+    got = torch.autograd.grad(loss, leaves, allow_unused=True)
+    return [torch.zeros_like(t) if g is None else g for g, t in zip(got, leaves)]
+
+
+# ---- causal convolution ----------------------------------------------------------
+
+
+@pytest.mark.parametrize("K,silu,kind", [(2, False, F32), (4, True, BF16), (8, True, F16)])
+@pytest.mark.parametrize("what", [NAN, INF])
+def test_conv_gradients_take_nothing_from_an_empty_rows_state(K, silu, kind, what):
+    """A row of length 0 hands its state on and adds nothing to dw and dbias."""
+    r = Rand(K)
+    B, D, L = 4, 5, 40
+    n = torch.tensor([L, 0, 3, 0], dtype=torch.int32)
+    x, dy = (r.normal(B, D, L, kind=kind) for _ in range(2))
+    w, bias = r.normal(D, K, scale=K ** -0.5), r.normal(D, scale=0.1)
+    st, dso = (r.normal(B, D, K - 1, kind=kind) for _ in range(2))
+    st[1], st[3, :, 0] = what, what
+    leaves = [d64(t, True) for t in (x, w, bias, st)]
+    y, after = ref.conv(leaves[0], leaves[1], leaves[2], silu, leaves[3], n)
+    want = grads((y * d64(dy)).sum() + (after * d64(dso)).sum(), leaves)
+    got = finc.causal_conv_backward(dev(x), dev(w), dev(dy), dev(bias), silu=silu, state=dev(st),
+                                    lengths=dev(n), dstate_out=dev(dso))
+    # sums over the positions: fp32 roundings in quadrature, of sqrt(B L) terms' size
+    chain = 64 + 4 * (B * L) ** 0.5
+    for g, v, name in zip(got, want, ("dx", "dw", "dbias", "dstate")):
+        assert torch.isfinite(g).all(), name
+        ref.close(g, v, name, chain if name in ("dw", "dbias") else 64)
+
+
+@pytest.mark.parametrize("n", [1, 8, 37, 40])
+def test_conv_gradients_of_an_infinite_last_input(n):
+    """The taps that no position has over it stay finite."""
+    r = Rand(n)
+    B, D, L, K = 2, 3, 40, 4
+    x, dy = r.normal(B, D, L), r.normal(B, D, L)
+    x[0, 1, n - 1] = INF
+    w, lens = r.normal(D, K), torch.tensor([n, L], dtype=torch.int32)
+    leaves = [d64(t, True) for t in (x, w)]
+    y, _ = ref.conv(leaves[0], leaves[1], None, False, None, lens)
+    used = (torch.arange(L) < lens[:, None]).double()[:, None]
+    want = grads((torch.where(used > 0, y, 0.0) * d64(dy)).sum(), leaves)
+    assert torch.isinf(want[1][1, K - 1]) and torch.isfinite(want[1][1, :K - 1]).all()
+    got = finc.causal_conv_backward(dev(x), dev(w), dev(dy), lengths=dev(lens))
+    ref.close(got[0], want[0], "dx")
+    ref.close(got[1], want[1], "dw", 64 + 4 * (B * L) ** 0.5)
