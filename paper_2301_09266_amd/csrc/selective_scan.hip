@@ -21,6 +21,14 @@ using namespace finc_seq;
 constexpr int kThreads = 512;
 constexpr float kLog2e = 1.44269504088896341f;
 
+// A log2 e, finite: an infinite decay times padding's step of 0 has no value, which the
+// next state would take over.  Steps above 1e-36 still take its exponential to 0 or
+// infinity.
+__device__ inline float decay(float a) {
+    const float v = a * kLog2e;
+    return __builtin_fabsf(v) > 3e38f ? __builtin_copysignf(3e38f, v) : v;
+}
+
 struct Rows {
     void *p;
     long long sb, sd;
@@ -386,7 +394,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_forward_kernel(ScanArgs a) {
         const int c = i / a.N, n = i - c * a.N, dd = cb * CB + c;
         const bool ok = dd < a.Dg;
         const long long at = (long long)(grp * a.Dg + (ok ? dd : 0)) * a.N + n;
-        As[i] = ok ? a.A[at] * kLog2e : 0.0f;
+        As[i] = ok ? decay(a.A[at]) : 0.0f;
         hs[i] = ok && a.state ? a.state[(long long)b * a.D * a.N + at] : 0.0f;
     }
     const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
@@ -619,7 +627,7 @@ __global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a, i
     load_upto<float, S>(a.state + at0, a.state ? a.N - n0 : 0, h);
 #pragma unroll
     for (int s = 0; s < S; ++s)
-        A2[s] *= kLog2e;
+        A2[s] = decay(A2[s]);
     const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
     const float skip = a.Dskip ? a.Dskip[d] : 0.0f;
     // B and C of all positions, position by position; 0 past the raster and the states
@@ -767,7 +775,7 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
         const int c = i / NP, n = i % NP;
         const bool ok = c < count && n < a.N;
         const long long at = (first + (ok ? c : 0)) * a.N + (ok ? n : 0);
-        As[i] = ok ? a.A[at] * kLog2e : 0.0f;
+        As[i] = ok ? decay(a.A[at]) : 0.0f;
         carry[i] = ok && ga.dstate_out ? ga.dstate_out[(long long)b * a.D * a.N + at] : 0.0f;
         dAs[i] = 0.0f;
     }

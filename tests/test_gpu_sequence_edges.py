@@ -7,7 +7,7 @@ import torch
 import seq_ref as ref
 from gpu_util import DEV
 from paper_2301_09266_amd import finc
-from test_gpu_sequence import BF16, F16, F32, NAN, Rand, d64, dev
+from test_gpu_sequence import BF16, F16, F32, NAN, Rand, d64, dev, scan_inputs, scan_kw
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -61,3 +61,40 @@ def test_conv_gradients_of_an_infinite_last_input(n):
     got = finc.causal_conv_backward(dev(x), dev(w), dev(dy), lengths=dev(lens))
     ref.close(got[0], want[0], "dx")
     ref.close(got[1], want[1], "dw", 64 + 4 * (B * L) ** 0.5)
+
+
+# ---- selective scan --------------------------------------------------------------
+
+
+@pytest.mark.parametrize("L,n", [(40, 5), (64, 50), (200, 130), (300, 7)])
+@pytest.mark.parametrize("N", [3, 16, 40])
+def test_scan_of_states_without_memory_takes_nothing_from_padding(L, n, N):
+    """A decay of minus infinity keeps nothing from one position to the next, and the
+    step of 0 that stands for padding does not meet it."""
+    B, D = 2, 6
+    t, _, r = scan_inputs(B, D, L, N, 1, "gsldbp", F32, L + N)
+    t["A"][2], t["A"][4, N // 2] = -INF, -INF
+    lens = torch.tensor([n, L], dtype=torch.int32)
+    for k in ("x", "dt", "Bm", "Cm", "z"):
+        t[k] = r.normal(*t[k].shape)
+    g, kw = scan_kw(t, lens, "gsldbp", None)
+    states, end = finc.selective_scan_states(B, D, L, N, DEV), torch.empty(B, D, N, device=DEV)
+    y = finc.selective_scan_forward(**g, **kw, state_out=end, states=states)
+    leaf = {k: d64(v, True) for k, v in t.items()}
+    yr, er = ref.scan(**leaf, softplus=True, lengths=lens)
+    chain = 64 + 2 * L ** 0.5
+    ref.close(y, yr, "y", chain)
+    ref.close(end, er, "state after", chain)
+    dy, dend = r.normal(B, D, L), r.normal(B, D, N)
+    kw.pop("state")
+    got = finc.selective_scan_backward(**g, **kw, dy=dev(dy), states=states, dstate_out=dev(dend))
+    names = [k for k in leaf if k != "dt_bias"]
+    want = dict(zip(names, grads((yr * d64(dy)).sum() + (er * d64(dend)).sum(),
+                                 [leaf[k] for k in names])))
+    key = dict(x="dx", dt="ddt", A="dA", Bm="dB", Cm="dC", D="dD", z="dz", state="dstate")
+    for k in names:
+        a, b = got[key[k]], want[k]
+        if k == "dt":   # -inf exp(-inf) has no value: of the other channels
+            a, b = a[:, [0, 1, 3, 5]], b[:, [0, 1, 3, 5]]
+        ref.close(a, b, key[k], 2 * chain + (4 * (B * L * D) ** 0.5
+                                             if k in ("A", "D", "Bm", "Cm") else 0))
