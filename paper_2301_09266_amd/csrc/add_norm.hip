@@ -240,15 +240,33 @@ __device__ inline void settle8(Raw8<E> t, int c, int D, float (&v)[8]) {
     }
 }
 
-// R lanes a row, V vectors of 8 a lane: vector v of a lane is lane + v R.  Bound by
-// memory: 32768 x 2048 in bf16 with an fp32 residual and dropout 150 us, 805 MB at 5.4
-// TB/s (the last-level cache holds some of them; a copy of 2 GiB reaches 4.8).
+// (mean r^2 + eps)^(-1/2) of a row whose squares leave fp32's range.
+template <int R, int V>
+__device__ inline float inv_wide(const float (&r)[V][8], int D, double eps, double *lds,
+                                 int &turn_of) {
+    double ss = 0.0;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            ss = __builtin_fma((double)r[v][i], (double)r[v][i], ss);
+    ss = all_lanes64<Sum64, R>(ss, lds, turn_of);
+    return (float)rsqrt64(__builtin_fma(ss, 1.0 / (double)afresh(D), eps));
+}
+
+// R lanes a row, V vectors of 8 a lane: vector v of a lane is lane + v R.  The mean square
+// is in fp32, and again in fp64 for a row where it overflows or, below 2^-80, may have lost
+// squares to underflow.  That costs narrow rows some percent (32768 x 333 in bf16 19.7 us,
+// 18.6 without; in fp64 throughout 20.4) and wide ones nothing.  Bound by memory: 32768 x
+// 2048 in bf16 with an fp32 residual and dropout 150 us, 805 MB at 5.4 TB/s (the last-level
+// cache holds some of them; a copy of 2 GiB reaches 4.8).
 template <typename E, typename F, int R, int V, int TH>
 __global__ __launch_bounds__(TH) void norm_forward_kernel(NormArgs a) {
     __shared__ unsigned lds[2 * (TH / 64)];
+    __shared__ double lds64[2 * (TH / 64)];
     constexpr bool kTiny = TH == kTinyThreads;
     const int lane = threadIdx.x % R;
-    int turn_of = 0;
+    int turn_of = 0, turn_of64 = 0;
     float w[V][8];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -301,7 +319,11 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(NormArgs a) {
             }
         }
         ss = sum_lanes<R>(ss, lds, turn_of);
-        const float inv = rsqrtf(__builtin_fmaf(ss, mean, eps));
+        const float var = __builtin_fmaf(ss, mean, eps);
+        float inv = rsqrtf(var);
+        // the same in all of the row's lanes
+        if (__builtin_expect(!(var >= 0x1p-80f && var < __builtin_inff()), 0))
+            inv = inv_wide<R, V>(r, a.D, a.eps, lds64, turn_of64);
         if (live) {
             E *out = (E *)a.y + m * a.sy;
 #pragma unroll

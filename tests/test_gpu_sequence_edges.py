@@ -98,3 +98,17 @@ def test_scan_of_states_without_memory_takes_nothing_from_padding(L, n, N):
             a, b = a[:, [0, 1, 3, 5]], b[:, [0, 1, 3, 5]]
         ref.close(a, b, key[k], 2 * chain + (4 * (B * L * D) ** 0.5
                                              if k in ("A", "D", "Bm", "Cm") else 0))
+
+
+# ---- norm ------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("D", [3, 100, 333, 1000, 2063, 4096, 8200])
+@pytest.mark.parametrize("kind,size", [(F32, 1e22), (BF16, 3e36), (F32, 1e-25), (BF16, 1e-30)])
+def test_norm_of_large_and_small_rows(D, kind, size):
+    """Rows whose squares leave fp32's range."""
+    r = Rand(D)
+    x, w = r.normal(9, D, kind=kind, scale=size), 1 + r.normal(D, scale=0.1)
+    y, s = finc.add_norm_forward(dev(x), dev(w), eps=0.0)
+    assert torch.equal(s.cpu(), x)
+    ref.close(y, ref.norm(d64(x), d64(w), 0.0), "y", 64 + 2 * D ** 0.5)
