@@ -77,7 +77,7 @@ template <typename E, int K, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_forward_kernel(ConvArgs a) {
     constexpr int V = kTile<E, false>, H = kHalo<K>;
     const int tx = 1 << a.txl;
-    const int rt = fdiv(blockIdx.x, a.div_t), tt = blockIdx.x - rt * a.tiles_t;
+    const int blk = block_of(), rt = fdiv(blk, a.div_t), tt = blk - rt * a.tiles_t;
     const long long row = (long long)rt * (kThreads >> a.txl) + (threadIdx.x >> a.txl);
     if (row >= (long long)a.B * a.D)
         return;
@@ -132,7 +132,10 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
     constexpr int V = kTile<E, true>, H = kHalo<K>, Q = K - 1;
     __shared__ float red[K + 1][kThreads / 64];
     const int tx = 1 << a.txl, ty = kThreads >> a.txl;
-    const int d = blockIdx.x, lx = threadIdx.x & (tx - 1), ly = threadIdx.x >> a.txl;
+    const int blk = block_of(), part = fdiv(blk, a.div_d), d = blk - part * a.D;
+    const int lx = threadIdx.x & (tx - 1), ly = threadIdx.x >> a.txl;
+    if (part >= a.parts)
+        return;
     float w[K], dw[K], db = 0.0f;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
         dw[j] = 0.0f;
     }
     const float bias = a.bias ? a.bias[d] : 0.0f;
-    for (int u = blockIdx.y; u < a.tiles_r * a.tiles_t; u += a.parts) {
+    for (int u = part; u < a.tiles_r * a.tiles_t; u += a.parts) {
         const int rt = fdiv(u, a.div_t), tt = u - rt * a.tiles_t;
         const int b = rt * ty + ly;
         const long long t0l = ((long long)tt * tx + lx) * V;
@@ -252,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
     __syncthreads();
     if (threadIdx.x <= K) {
         const float *r = red[threadIdx.x];
-        a.partial[((long long)blockIdx.y * a.D + d) * (K + 1) + threadIdx.x] =
+        a.partial[((long long)part * a.D + d) * (K + 1) + threadIdx.x] =
             (r[0] + r[1]) + (r[2] + r[3]);
     }
 }
@@ -264,7 +267,7 @@ __global__ __launch_bounds__(256) void conv_sum_kernel(const float *partial, int
     __shared__ float red[8][33];
     const long long n = (long long)D * (K + 1);
     const int l = threadIdx.x & 31, grp = threadIdx.x >> 5;
-    const long long e = blockIdx.x * 32ll + l;
+    const long long e = block_of() * 32ll + l;
     float s = 0.0f;
     if (e < n)
         for (int p = grp; p < parts; p += 64) {
@@ -441,7 +444,7 @@ int finc_causal_conv_forward(const finc_conv_args *a, hipStream_t stream) {
         return FINC_EUNSUPPORTED;
     with_type(a->type, [&](auto e) {
         typedef decltype(e) E;
-        const dim3 grid((unsigned)(rows * c.tiles_t));
+        const dim3 grid = grid_of(rows * c.tiles_t);
         if (a->silu)
             launch_taps<E, true, false>(a->K, c, grid, stream);
         else
@@ -502,7 +505,7 @@ int finc_causal_conv_backward(const finc_conv_args *a, const finc_conv_grads *g,
     if (c.parts > 0) {
         with_type(a->type, [&](auto e) {
             typedef decltype(e) E;
-            const dim3 grid((unsigned)D, (unsigned)c.parts);
+            const dim3 grid = grid_of((long long)D * c.parts);
             if (a->silu)
                 launch_taps<E, true, true>(K, c, grid, stream);
             else
@@ -512,8 +515,7 @@ int finc_causal_conv_backward(const finc_conv_args *a, const finc_conv_grads *g,
         if (r2 != FINC_OK)
             return r2;
     }
-    hipLaunchKernelGGL(conv_sum_kernel, dim3((unsigned)cdivll((long long)D * (K + 1), 32)),
-                       dim3(256), 0, stream, c.partial, c.parts, g->dw, g->dbias, D, K);
+    hipLaunchKernelGGL(conv_sum_kernel, grid_of(cdivll((long long)D * (K + 1), 32)), dim3(256), 0, stream, c.partial, c.parts, g->dw, g->dbias, D, K);
     return launched();
 }
 

@@ -383,10 +383,12 @@ __global__ __launch_bounds__(kThreads, 4) void scan_forward_kernel(ScanArgs a) {
     float *pre = As + CB * a.N;              // delta, delta x of every wave's channel
     const int tid = threadIdx.x, lane = tid & 15, rowi = (tid >> 4) & 3;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int blk = blockIdx.x;
+    int blk = block_of();
     const int cb = blk % a.blocks;
     blk /= a.blocks;
     const int grp = blk % a.G, b = blk / a.G;
+    if (b >= a.B)
+        return;
     const bool live = cb * CB + wave < a.Dg;
     const int d = grp * a.Dg + (live ? cb * CB + wave : 0);
     const int n_pos = __builtin_amdgcn_readfirstlane(row_length(a.lengths, b, a.L));
@@ -600,10 +602,12 @@ __global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a, i
     constexpr int NP = 4 * S;
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const int tid = threadIdx.x, q = tid & 3, n0 = q * S, CB = blockDim.x / 4;
-    int blk = blockIdx.x;
+    int blk = block_of();
     const int cb = blk % a.blocks;
     blk /= a.blocks;
     const int grp = blk % a.G, b = blk / a.G;
+    if (b >= a.B)
+        return;
     const bool live = cb * CB + tid / 4 < a.Dg;
     const int d = grp * a.Dg + (live ? cb * CB + tid / 4 : 0);
     const int n_pos = __builtin_amdgcn_readfirstlane(row_length(a.lengths, b, a.L));
@@ -762,10 +766,12 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
     // uniform: a wave's rows of activations have their addresses in scalar registers
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n0 = rowi * S;
-    int blk = blockIdx.x;
+    int blk = block_of();
     const int set = blk % ga.sets;
     blk /= ga.sets;
     const int grp = blk % a.G, b = blk / a.G;
+    if (b >= a.B)
+        return;
     const int c0 = set * ga.set;                   // the set's first channel in the group
     const int count = min(ga.set, a.Dg - c0);
     const long long first = (long long)grp * a.Dg + c0;
@@ -1039,32 +1045,31 @@ template <typename E>
 __global__ __launch_bounds__(256) void shared_sum_kernel(GradArgs ga, Rows dB, Rows dC) {
     const ScanArgs &a = ga.f;
     const int rows = a.G * a.N;
-    const long long tiles = (a.L + 1023) / 1024;
-    long long blk = blockIdx.x;
-    const long long tile = blk % tiles;
-    blk /= tiles;
-    const int r = (int)(blk % rows);
-    blk /= rows;
-    const int b = (int)(blk % a.B), which = (int)(blk / a.B);
-    const int t0 = (int)(tile * 1024 + threadIdx.x * 4);
-    if (t0 >= a.L)
-        return;
-    const int n_pos = row_length(a.lengths, b, a.L);
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const long long tiles = (a.L + 1023) / 1024, all = 2 * tiles * rows * a.B;
     const long long step = (long long)a.B * rows * a.L;
-    const float *p = ga.shared + which * ga.sets * step + ((long long)b * rows + r) * a.L + t0;
-    for (int k0 = 0; k0 < ga.sets; k0 += 8) {
-        float v[8][4];   // in flight together
+    for (long long unit = blockIdx.x; unit < all; unit += gridDim.x) {
+        const long long tile = unit % tiles, row = unit / tiles;
+        const int r = (int)(row % rows), b = (int)(row / rows % a.B);
+        const int which = (int)(row / rows / a.B);
+        const int t0 = (int)(tile * 1024 + threadIdx.x * 4);
+        if (t0 >= a.L)
+            continue;
+        const int n_pos = row_length(a.lengths, b, a.L);
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float *p = ga.shared + which * ga.sets * step + ((long long)b * rows + r) * a.L + t0;
+        for (int k0 = 0; k0 < ga.sets; k0 += 8) {
+            float v[8][4];   // in flight together
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            load_upto<float, 4>(p + min(k0 + k, ga.sets - 1) * step, n_pos - t0, v[k]);
+            for (int k = 0; k < 8; ++k)
+                load_upto<float, 4>(p + min(k0 + k, ga.sets - 1) * step, n_pos - t0, v[k]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+            for (int k = 0; k < 8; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                s[i] += k0 + k < ga.sets ? v[k][i] : 0.0f;
+                for (int i = 0; i < 4; ++i)
+                    s[i] += k0 + k < ga.sets ? v[k][i] : 0.0f;
+        }
+        store_upto<E, 4>((which ? dC : dB).row<E>(b, r) + t0, a.L - t0, s);
     }
-    store_upto<E, 4>((which ? dC : dB).row<E>(b, r) + t0, a.L - t0, s);
 }
 
 // dA, dDskip, ddt_bias: the batch rows' sums, eight groups in turn, then in order (5 us
@@ -1075,7 +1080,7 @@ __global__ __launch_bounds__(256) void param_sum_kernel(GradArgs ga, float *dA, 
     const ScanArgs &a = ga.f;
     const long long n = (long long)a.D * (a.N + 2);
     const int l = threadIdx.x & 31, g = threadIdx.x >> 5;
-    const long long i = blockIdx.x * 32ll + l;
+    const long long i = block_of() * 32ll + l;
     float s = 0.0f;
     if (i < n)
         for (int b = g; b < a.B; b += 64) {
@@ -1124,10 +1129,10 @@ constexpr int kStepThreads = 256;
 template <typename E, int Q>
 __global__ __launch_bounds__(kStepThreads) void scan_step_kernel(StepArgs a) {
     const int q = threadIdx.x % Q;
-    const long long d0 = (long long)blockIdx.x * (kStepThreads / Q) + threadIdx.x / Q;
+    const long long d0 = block_of() * (long long)(kStepThreads / Q) + threadIdx.x / Q;
     const bool live = d0 < a.D;
     const int d = live ? (int)d0 : 0, grp = d / a.Dg;
-    for (int b = blockIdx.y; b < a.B; b += gridDim.y) {
+    for (int b = blockIdx.z; b < a.B; b += gridDim.z) {
         const int slot = a.slots ? a.slots[b] : b;
         E *y = (E *)a.y + b * a.sy + d;
         if (slot < 0 || slot >= a.S) {
@@ -1204,7 +1209,7 @@ int launch_forward(ScanArgs &c, hipStream_t s) {
         (void)hipFuncSetAttribute((const void *)scan_forward_kernel<E, T>,
                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     (void)hipGetLastError();   // the launch check decides
-    hipLaunchKernelGGL((scan_forward_kernel<E, T>), dim3((unsigned)grid), dim3(kThreads),
+    hipLaunchKernelGGL((scan_forward_kernel<E, T>), grid_of(grid), dim3(kThreads),
                        (unsigned)lds, s, c);
     return launched();
 }
@@ -1227,7 +1232,7 @@ int launch_short(ScanArgs &c, hipStream_t s) {
     if (grid >= (1ll << 31))
         return FINC_EUNSUPPORTED;
     (void)hipGetLastError();   // the launch check decides
-    hipLaunchKernelGGL((scan_short_kernel<E, S, ALL>), dim3((unsigned)grid), dim3(threads),
+    hipLaunchKernelGGL((scan_short_kernel<E, S, ALL>), grid_of(grid), dim3(threads),
                        (unsigned)lds, s, c, lane_positions(c.L, c.N) == 4 ? 6 : 7);
     return launched();
 }
@@ -1288,8 +1293,8 @@ int launch_backward(GradArgs &c, hipStream_t s) {
     (void)hipFuncSetAttribute((const void *)scan_backward_kernel<E, T, S>,
                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     (void)hipGetLastError();   // the launch check decides
-    hipLaunchKernelGGL((scan_backward_kernel<E, T, S>), dim3((unsigned)grid),
-                       dim3(64 * kGradWaves), (unsigned)lds, s, c);
+    hipLaunchKernelGGL((scan_backward_kernel<E, T, S>), grid_of(grid), dim3(64 * kGradWaves),
+                       (unsigned)lds, s, c);
     return launched();
 }
 
@@ -1429,7 +1434,8 @@ int finc_selective_scan_backward(const finc_scan_args *a, const finc_scan_grads 
     c.sets = (int)cdivll(c.f.Dg, c.set);
     int rc = FINC_OK;
     const long long sums = 2ll * B * GN * cdivll(L, 1024);
-    if (sums >= (1ll << 31))
+    const long long params = cdivll((long long)D * (N + 2), 32);
+    if (params > (1ll << 31))
         return FINC_EUNSUPPORTED;
     if (B > 0) {
         with_type(a->type, [&](auto e) { rc = dispatch_backward<decltype(e)>(c, stream); });
@@ -1438,15 +1444,16 @@ int finc_selective_scan_backward(const finc_scan_args *a, const finc_scan_grads 
     }
     if (sums > 0) {
         with_type(a->type, [&](auto e) {
-            hipLaunchKernelGGL(shared_sum_kernel<decltype(e)>, dim3((unsigned)sums), dim3(256), 0,
-                               stream, c, rows_of(g->dBm), rows_of(g->dCm));
+            const unsigned blocks = sums < (1 << kRowBits) ? (unsigned)sums : 1u << kRowBits;
+            hipLaunchKernelGGL(shared_sum_kernel<decltype(e)>, dim3(blocks), dim3(256), 0, stream,
+                               c, rows_of(g->dBm), rows_of(g->dCm));
         });
         rc = launched();
         if (rc != FINC_OK)
             return rc;
     }
-    hipLaunchKernelGGL(param_sum_kernel, dim3((unsigned)cdivll((long long)D * (N + 2), 32)),
-                       dim3(256), 0, stream, c, g->dA, g->dDskip, g->ddt_bias);
+    hipLaunchKernelGGL(param_sum_kernel, grid_of(params), dim3(256), 0, stream, c, g->dA,
+                       g->dDskip, g->ddt_bias);
     return launched();
 }
 
@@ -1479,14 +1486,12 @@ int finc_selective_scan_step(const finc_scan_step_args *a, hipStream_t stream) {
                         B, a->S, D, a->N, a->G, D / a->G, a->softplus};
     with_type(a->type, [&](auto e) {
         typedef decltype(e) E;
-        const unsigned gy = (unsigned)(B < 32768 ? B : 32768);
+        dim3 grid = grid_of(cdivll(D, a->N <= 4 ? kStepThreads : kStepThreads / 4));
+        grid.z = (unsigned)(B < 32768 ? B : 32768);
         if (a->N <= 4)
-            hipLaunchKernelGGL((scan_step_kernel<E, 1>), dim3((unsigned)cdivll(D, kStepThreads), gy),
-                               dim3(kStepThreads), 0, stream, c);
+            hipLaunchKernelGGL((scan_step_kernel<E, 1>), grid, dim3(kStepThreads), 0, stream, c);
         else
-            hipLaunchKernelGGL((scan_step_kernel<E, 4>),
-                               dim3((unsigned)cdivll(D, kStepThreads / 4), gy), dim3(kStepThreads), 0,
-                               stream, c);
+            hipLaunchKernelGGL((scan_step_kernel<E, 4>), grid, dim3(kStepThreads), 0, stream, c);
     });
     return launched();
 }

@@ -184,6 +184,18 @@ __device__ inline float wave_sum(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
+// ---- grids -------------------------------------------------------------------------
+// A launch holds fewer than 2^32 threads in x: more workgroups than 2^21 lie in rows of
+// y, the last of which may hold some without work.
+
+constexpr int kRowBits = 21;
+inline dim3 grid_of(long long blocks) {   // up to 2^31
+    const long long row = 1ll << kRowBits;
+    return blocks <= row ? dim3((unsigned)blocks)
+                         : dim3((unsigned)row, (unsigned)((blocks + row - 1) / row));
+}
+__device__ inline int block_of() { return (int)(blockIdx.y << kRowBits | blockIdx.x); }
+
 // ---- the host's checks -------------------------------------------------------------
 
 inline int launched() { return hipGetLastError() == hipSuccess ? FINC_OK : FINC_EHIP; }

@@ -112,3 +112,100 @@ def test_norm_of_large_and_small_rows(D, kind, size):
     y, s = finc.add_norm_forward(dev(x), dev(w), eps=0.0)
     assert torch.equal(s.cpu(), x)
     ref.close(y, ref.norm(d64(x), d64(w), 0.0), "y", 64 + 2 * D ** 0.5)
+
+
+# ---- launches of many workgroups -------------------------------------------------
+
+
+def repeated(t, B):
+    """B batch rows at one address."""
+    return None if t is None else t.to(DEV).expand(B, *t.shape[1:])
+
+
+def all_rows_equal(t, one):
+    for part in t.split(max(1, (1 << 28) // max(1, one.numel()))):
+        assert torch.equal(part, one.expand_as(part))
+
+
+def test_conv_of_many_workgroups():
+    """2^24 of them: 2^30 rows of 17 positions."""
+    r = Rand(1)
+    B, D, L = 1 << 15, 1 << 15, 17
+    x, w = r.normal(1, D, L, kind=BF16), r.normal(D, 4).to(DEV)
+    all_rows_equal(finc.causal_conv_forward(repeated(x, B), w, silu=True),
+                   finc.causal_conv_forward(x.to(DEV), w, silu=True))
+
+
+def test_conv_gradients_of_many_channels():
+    """2^24 and some, a workgroup each."""
+    D, L = (1 << 24) + 7, 3
+    x, dy = (torch.empty(1, D, L, dtype=BF16, device=DEV).normal_() for _ in range(2))
+    w = torch.empty(D, 2, device=DEV).normal_()
+    dx, dw, _, _ = finc.causal_conv_backward(x, w, dy, silu=True)
+    for at in (slice(0, 1000), slice((1 << 21) - 500, (1 << 21) + 500), slice(D - 1000, D)):
+        one = finc.causal_conv_backward(x[:, at], w[at], dy[:, at], silu=True)
+        assert torch.equal(dx[:, at], one[0]) and torch.equal(dw[at], one[1])
+
+
+@pytest.mark.parametrize("L,B", [(65, 1 << 13), (1, 1 << 14)])
+def test_scan_of_many_workgroups(L, B):
+    """2^23 and 2^24 of them: a group a channel."""
+    D = 1 << 10
+    t, _, _ = scan_inputs(1, D, L, 1, D, "gsdbp", BF16, L)
+    g, kw = scan_kw(t, None, "gsdbp", None)
+    one_end, end = torch.empty(1, D, 1, device=DEV), torch.empty(B, D, 1, device=DEV)
+    one = finc.selective_scan_forward(**g, **kw, state_out=one_end)
+    for k in ("x", "dt", "z", "Bm", "Cm"):
+        g[k] = repeated(g[k], B)
+    kw["state"] = kw["state"].expand(B, D, 1).contiguous()
+    y = finc.selective_scan_forward(**g, **kw, state_out=end)
+    all_rows_equal(y, one)
+    all_rows_equal(end, one_end)
+
+
+def back(t, B, L, D, N, dy):
+    g, kw = scan_kw(t, None, "gdbp", None)
+    kw.pop("state")
+    for k in ("x", "dt", "z", "Bm", "Cm"):
+        g[k] = repeated(g[k], B)
+    states = finc.selective_scan_states(B, D, L, N, DEV)
+    finc.selective_scan_forward(**g, **kw, states=states)
+    return finc.selective_scan_backward(**g, **kw, dy=repeated(dy, B), states=states)
+
+
+@pytest.mark.parametrize("B,D,G,N,L", [(1 << 14, 16, 16, 32, 64), (1 << 13, 1 << 10, 1 << 10, 1, 65),
+                                       (1 << 17, 64, 64, 64, 1)])
+def test_scan_gradients_of_many_rows(B, D, G, N, L):
+    """2^24 workgroups' worth of sums of dB and dC, 2^23 workgroups, and 2^30 of sums."""
+    t, _, r = scan_inputs(1, D, L, N, G, "gdbp", BF16, N)
+    dy = r.normal(1, D, L, kind=BF16)
+    one, many = back(t, 1, L, D, N, dy), back(t, B, L, D, N, dy)
+    for k in ("dx", "ddt", "dz", "dB", "dC", "dstate"):
+        all_rows_equal(many[k], one[k])
+    for k in ("dA", "dD", "ddt_bias"):   # B equal terms, each sum of them one rounding
+        bar = B * 2.0 ** -24 * B * one[k].abs()
+        assert ((many[k] - B * one[k]).abs() <= bar).all(), k
+
+
+def test_scan_gradients_of_many_channels():
+    """2^24 workgroups' worth of sums of the parameters."""
+    D, N = 1 << 23, 62
+    mk = lambda *s, kind=BF16: torch.empty(*s, dtype=kind, device=DEV).normal_()  # noqa: E731
+    x, dt, dy = (mk(1, D, 1) for _ in range(3))
+    Bm, Cm, A = mk(1, 1, N, 1), mk(1, 1, N, 1), mk(D, N, kind=F32).abs_().neg_()
+    skip = mk(D, kind=F32)
+
+    def run(at):
+        c = slice(at.start, at.stop)
+        v = dict(x=x[:, c], dt=dt[:, c], A=A[c], Bm=Bm, Cm=Cm, D=skip[c])
+        states = finc.selective_scan_states(1, at.stop - at.start, 1, N, DEV)
+        finc.selective_scan_forward(**v, states=states)
+        return finc.selective_scan_backward(**v, dy=dy[:, c], states=states)
+
+    whole = run(slice(0, D))
+    for at in (slice(0, 64), slice(1 << 22, (1 << 22) + 128), slice(D - 64, D)):
+        part = run(at)
+        for k in ("dA", "dD"):
+            assert torch.equal(whole[k][at], part[k]), (k, at)
+        for k in ("dx", "ddt"):
+            assert torch.equal(whole[k][:, at], part[k]), (k, at)
