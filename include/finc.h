@@ -526,7 +526,8 @@ int finc_conv1x1_inverse(const float *y, float *x, const float *Wm, int B, int C
  *  - Inner tensors are (B, D, L) with the L positions of a row contiguous (an
  *    image's H*W), given with their steps: a finc_raster, so that a
  *    projection's halves need no copy.  Inputs may repeat rows (steps of 0);
- *    an output's elements must lie at different addresses.  Any alignment of
+ *    an output's elements must lie at different addresses, its batch rows one
+ *    after another or its channels (no interleaved ones).  Any alignment of
  *    the element's size.  L < 2^30, B*D < 2^31 - 256, B*G*N < 2^31; of (M, D) rows
  *    M ceil(D / 8) < 2^31 (FINC_EINVAL past them).  Offsets are 64-bit.
  *  - lengths: device ints, B, or NULL (all L); clamped to [0, L].  Positions at

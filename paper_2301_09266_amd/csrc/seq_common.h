@@ -236,14 +236,16 @@ inline bool readable(const Region &r) {
     const long long e = extent(r);
     return e == 0 || (e > 0 && r.p && (uintptr_t)r.p % r.size == 0);
 }
-// An output: no two of its elements share an address.
+// An output: no two of its elements share an address, as one of its steps passes the
+// rows that the other one spans.
 inline bool writable(const Region &r) {
     if (!readable(r))
         return false;
     if (extent(r) == 0)
         return true;
-    const long long inner = (r.inner - 1) * r.si + r.n;
-    return (r.inner == 1 || r.si >= r.n) && (r.outer == 1 || r.so >= inner);
+    const long long inner = (r.inner - 1) * r.si + r.n, outer = (r.outer - 1) * r.so + r.n;
+    return ((r.inner == 1 || r.si >= r.n) && (r.outer == 1 || r.so >= inner)) ||
+           (r.so >= r.n && r.si >= outer);
 }
 
 // Whether two regions share memory.  Regions of the same steps whose blocks lie

@@ -114,6 +114,48 @@ def test_norm_of_large_and_small_rows(D, kind, size):
     ref.close(y, ref.norm(d64(x), d64(w), 0.0), "y", 64 + 2 * D ** 0.5)
 
 
+# ---- layouts of outputs ----------------------------------------------------------
+
+
+def channels_first(t):
+    """The (B, D, L) view of a (D, B, L) tensor that is NaN."""
+    B, D, L = t.shape
+    return torch.full((D, B, L), NAN, dtype=t.dtype, device=DEV).transpose(0, 1)
+
+
+@pytest.mark.parametrize("L,kind", [(40, F32), (150, BF16)])
+def test_outputs_with_the_channels_outside(L, kind):
+    """(D, B, L) in memory, as a channel-major projection writes it."""
+    B, D, N = 3, 10, 16
+    t, _, r = scan_inputs(B, D, L, N, 1, "gdbp", kind, L)
+    g, kw = scan_kw(t, None, "gdbp", None)
+    kw.pop("state")
+    w, dy = r.normal(D, 4).to(DEV), r.normal(B, D, L, kind=kind).to(DEV)
+    swapped = {k: channels_first(v).copy_(v) if k in ("x", "dt", "z") else v for k, v in g.items()}
+    new = lambda: channels_first(dy)  # noqa: E731
+    want = finc.causal_conv_forward(g["x"], w, silu=True)
+    assert torch.equal(finc.causal_conv_forward(swapped["x"], w, silu=True, out=new()), want)
+    want = finc.causal_conv_backward(g["x"], w, dy, silu=True)
+    got = finc.causal_conv_backward(swapped["x"], w, dy, silu=True, dx=new())
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    states = finc.selective_scan_states(B, D, L, N, DEV)
+    want = finc.selective_scan_forward(**g, **kw, states=states)
+    assert torch.equal(finc.selective_scan_forward(**swapped, **kw, out=new()), want)
+    want = finc.selective_scan_backward(**g, **kw, dy=dy, states=states)
+    got = finc.selective_scan_backward(**swapped, **kw, dy=dy, states=states, dx=new(), ddt=new(),
+                                       dz=new())
+    assert all(torch.equal(got[k], want[k]) for k in want if want[k] is not None)
+
+
+def test_outputs_that_share_elements_are_refused():
+    x, w = torch.zeros(3, 10, 40, device=DEV), torch.zeros(10, 4, device=DEV)
+    space = torch.zeros(10 * 3 * 40, device=DEV)
+    for steps in ((40, 119), (39, 120), (0, 120), (399, 40), (400, 39), (40, 40)):
+        with pytest.raises(finc.FincError) as e:
+            finc.causal_conv_forward(x, w, out=space.as_strided(x.shape, (*steps, 1)))
+        assert e.value.code == finc.EINVAL, steps
+
+
 # ---- launches of many workgroups -------------------------------------------------
 
 
