@@ -525,7 +525,7 @@ int finc_causal_conv_step(int type, const void *x, long long sx, void *y, long l
     if (!conv_shape(type, B, D, 1, K) || S < 0 || (!slots && S < B))
         return FINC_EINVAL;
     const int sz = type_size(type);
-    const long long st = (long long)S * D * (K - 1);
+    const long long st = elements(S, D, K - 1);
     const Region in[] = {{x, B, sx, 1, 0, D, sz}, flat(w, (long long)D * K, 4),
                          flat(bias, bias ? D : 0, 4), flat(slots, slots ? B : 0, 4)};
     const Region out[] = {{y, B, sy, 1, 0, D, sz}, flat(state, st, sz)};

@@ -1470,7 +1470,7 @@ int finc_selective_scan_step(const finc_scan_step_args *a, hipStream_t stream) {
                          flat(a->dt_bias, a->dt_bias ? D : 0, 4),
                          flat(a->slots, a->slots ? B : 0, 4)};
     const Region out[] = {{a->y, B, a->sy, 1, 0, D, sz},
-                          flat(a->state, (long long)a->S * D * a->N, 4)};
+                          flat(a->state, elements(a->S, D, a->N), 4)};
     for (const Region &r : in)
         if (!readable(r))
             return FINC_EINVAL;

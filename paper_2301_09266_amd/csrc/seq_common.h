@@ -212,6 +212,11 @@ struct Region {
     long long outer, so, inner, si, n;
     int size;
 };
+// a b c, or a length that no region has.
+inline long long elements(long long a, long long b, long long c) {
+    long long n;
+    return __builtin_mul_overflow(a, b, &n) || __builtin_mul_overflow(n, c, &n) ? INT64_MAX : n;
+}
 inline Region flat(const void *p, long long n, int size) { return {p, 1, 0, 1, 0, n, size}; }
 inline Region raster(const finc_raster &r, int B, int D, int L, int size) {
     return {r.p, B, r.sb, D, r.sd, L, size};

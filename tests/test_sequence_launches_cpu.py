@@ -101,6 +101,17 @@ def test_ordinary_calls_take_one_row_of_workgroups(drive):
     for (call, want), (rc, ls) in zip(calls, drive([c for c, _ in calls])):
         assert rc == finc.OK and ls[0][1] == want, (call, ls)
     # dB and dC: a workgroup for 1024 positions of a row; the parameters: for 32 of them
-    assert drive([calls[4][0]])[0][1][1:] == [
-        (n, b, 256, 0) for n, b in zip((k for k, *_ in drive([calls[4][0]])[0][1][1:]),
-                                       (2 * 4 * 16 * 4, 2048 * 18 // 32))]
+    (_, ls), = drive([calls[4][0]])
+    assert [blocks for _, blocks, _, _ in ls[1:]] == [2 * 4 * 16 * 4, 2048 * 18 // 32]
+
+
+@pytest.mark.parametrize("S,D,N", [(1 << 30, 1 << 30, 16), (1 << 30, 1 << 30, 64),
+                                   ((1 << 31) - 1, 1 << 30, 9), (1 << 28, 1 << 30, 64)])
+def test_states_past_the_address_space_are_refused(S, D, N):
+    """Entries whose number would wrap to a small one."""
+    at = [1 << (40 + i) for i in range(10)]
+    a = finc.SCAN_STEP_ARGS.pack(BF16, 1, S, D, N, 1, 1, at[0], at[1], 0, at[2], at[3], D, D, D, N, N,
+                                 D, at[4], at[5], 0, 0, 0, 0)
+    assert finc.lib().finc_selective_scan_step(a, None) == finc.EINVAL
+    assert finc.lib().finc_causal_conv_step(BF16, at[0], D, at[1], D, at[2], None, None, None, 1, S, D,
+                                            8, 1, None) == finc.EINVAL
