@@ -449,7 +449,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_forward_kernel(ScanArgs a) {
         // under way until the part is done
         fetch(part + 1 < parts ? p0 + P : p0);
         tiles.fetch(min(part + 2, parts - 1));
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
 #pragma unroll
         for (int j = 0; j < T; j += 4) {
             lds_load<4>(mine + (j * 4 + lane) * 4, delta + j);
@@ -460,9 +460,9 @@ __global__ __launch_bounds__(kThreads, 4) void scan_forward_kernel(ScanArgs a) {
             sum += delta[j];
             y[j] = 0.0f;
         }
-        __builtin_amdgcn_wave_barrier();
         if (a.states && live)
             keep_states(a, b, d, part, hs + wave * a.N, tid & 63);
+        wave_exchange();
         float *hr = hs + wave * a.N;
         const float *Ar = As + wave * a.N;
         int i = rowi;
@@ -871,7 +871,7 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
             // the next channel's, under way
             const bool more = c + kGradWaves < count;
             fetch(more ? c + kGradWaves : wave, more ? part : max(part - 1, 0));
-            __builtin_amdgcn_wave_barrier();
+            wave_exchange();
             float de[T], dx[T], g[T], gB[T], sA[T], yv[T], sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < T; j += 4) {
@@ -880,7 +880,7 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
                 lds_load<4>(q + P, dx + j);
                 lds_load<4>(q + 2 * P, g + j);
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_exchange();
 #pragma unroll
             for (int j = 0; j < T; ++j) {
                 sum += de[j];

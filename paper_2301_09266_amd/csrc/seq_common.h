@@ -159,6 +159,15 @@ __device__ inline float softplus(float v) {
     return __builtin_fmaf(2.0f * s, p, __builtin_fmaxf(v, 0.0f));
 }
 
+// Between what a wave's lanes write to LDS and what others of them read of it, and before
+// they write there again.  The LDS takes a wave's accesses in order: what is needed is that
+// the compiler keeps that order, which the barrier alone does not ask of it.
+__device__ inline void wave_exchange() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // ---- reductions over lanes -------------------------------------------------------
 
 template <int CTRL>
