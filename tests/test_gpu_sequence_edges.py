@@ -114,6 +114,72 @@ def test_norm_of_large_and_small_rows(D, kind, size):
     ref.close(y, ref.norm(d64(x), d64(w), 0.0), "y", 64 + 2 * D ** 0.5)
 
 
+# ---- norm in 8 bits --------------------------------------------------------------
+
+
+def codes(y):
+    """The 8-bit values and scales of float64 rows, by their definition."""
+    s = (y.abs().amax(-1, keepdim=True) / 448).clamp(min=2.0 ** -126)
+    return (y / s).float().to(torch.float8_e4m3fn), s[..., 0]
+
+
+def same_codes(got, want):
+    a, b = got.view(torch.uint8), want.view(torch.uint8)
+    n = int((a != b).sum())
+    assert n == 0, f"{n} of {a.numel()} 8-bit values are other ones"
+
+
+EIGHT = [(20000, 5), (9000, 100), (8000, 128), (3000, 333), (2000, 512), (1100, 1000), (1000, 1024),
+         (500, 2048), (500, 2063), (250, 4096), (200, 5000), (130, 8192), (130, 8200), (64, 16384)]
+
+
+@pytest.mark.parametrize("M,D", EIGHT)
+@pytest.mark.parametrize("kind,rkind,p", [(BF16, BF16, 0.0), (BF16, F32, 0.1), (F16, F32, 0.3),
+                                          (F32, F32, 0.5)])
+def test_norm_in_eight_bits_code_for_code(M, D, kind, rkind, p):
+    r = Rand(M + D)
+    x, res = r.normal(M, D, kind=kind), r.normal(M, D, kind=rkind)
+    w = 1 + r.normal(D, scale=0.1)
+    drop = dict(p=p, seed=D << 40, offset=M << 35)
+    q, scale, s = finc.add_norm_forward(dev(x), dev(w), dev(res), fp8=True, **drop)
+    f = ref.dropout_factor(M, D, p, drop["seed"], drop["offset"]).to(DEV)
+    rr = dev(x).double() * f + dev(res).double()
+    ref.close(s, rr, "r")
+    want, ws = codes(ref.norm(rr, dev(w).double(), 1e-5))
+    same_codes(q, want)
+    assert torch.equal(scale, ws.float())
+
+
+def beside_the_middles(M, D, kind, r):
+    """(x, residual or None, w) whose sums are a few fp32 steps from the middle of two 8-bit
+    values of their row."""
+    w = (1 + r.normal(D, scale=0.1)).abs() + 0.25
+    w[0] = w.max() * 1.01
+    every = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
+    mid = ((every[1:] + every[:-1]) / 2)[torch.randint(0, 126, (M, D), generator=r.g)]
+    top = torch.rand(M, 1, generator=r.g, dtype=torch.float64) * 7 + 1
+    sign = torch.randint(0, 2, (M, D), generator=r.g) * 2 - 1
+    s = (sign * mid * top * d64(w)[0] / (448 * d64(w))).float()
+    s = (s.view(torch.int32) + torch.randint(-3, 4, (M, D), generator=r.g, dtype=torch.int32)) \
+        .view(F32)
+    s[:, 0] = top[:, 0].float()
+    if kind == F32:
+        return s, None, w
+    x = r.normal(M, D, kind=kind, scale=0.01)
+    return x, (s.double() - d64(x)).float(), w
+
+
+@pytest.mark.parametrize("D", [7, 128, 500, 1000, 2063, 4096, 8000, 16384])
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_norm_in_eight_bits_beside_the_middles(D, kind):
+    x, res, w = beside_the_middles(40000 // D + 2, D, kind, Rand(D))
+    q, scale, _ = finc.add_norm_forward(dev(x), dev(w), dev(res), fp8=True)
+    rr = d64(x) if res is None else d64(x) + d64(res)
+    want, ws = codes(ref.norm(rr, d64(w), 1e-5))
+    same_codes(q.cpu(), want)
+    assert torch.equal(scale.cpu(), ws.float())
+
+
 # ---- layouts of outputs ----------------------------------------------------------
 
 
