@@ -7,7 +7,7 @@ import torch
 import seq_ref as ref
 from gpu_util import DEV
 from paper_2301_09266_amd import finc
-from test_gpu_sequence import BF16, F16, F32, NAN, Rand, d64, dev, scan_inputs, scan_kw
+from test_gpu_sequence import BF16, F16, F32, NAN, Rand, d64, dev, same_bits, scan_inputs, scan_kw
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -317,3 +317,106 @@ def test_scan_gradients_of_many_channels():
             assert torch.equal(whole[k][at], part[k]), (k, at)
         for k in ("dx", "ddt"):
             assert torch.equal(whole[k][:, at], part[k]), (k, at)
+
+
+# ---- streams and offsets ---------------------------------------------------------
+
+
+def test_calls_read_what_their_own_stream_writes_last():
+    """Inputs that are NaN until a stream's copies, behind some milliseconds of its other
+    work, have filled them: a call on any other stream would read them before."""
+    r = Rand(77)
+    B, D, L, N = 3, 24, 150, 16
+    t, _, _ = scan_inputs(B, D, L, N, 1, "gdbp", BF16, 77)
+    g, _ = scan_kw(t, None, "gdbp", None)
+    rows = {k: r.normal(B, D, kind=BF16).to(DEV) for k in ("x", "dt")}
+    Bm, Cm = (r.normal(B, 1, N, kind=BF16).to(DEV) for _ in range(2))
+    wide = {k: r.normal(50, 333, kind=BF16).to(DEV) for k in ("x", "res", "dy")}
+    w, nw, A = r.normal(D, 4).to(DEV), r.normal(333).to(DEV), g.pop("A")
+    skip, bias = g.pop("D"), g.pop("dt_bias")
+    inputs = dict(**{"s" + k: v for k, v in g.items()}, **{"r" + k: v for k, v in rows.items()},
+                  **{"w" + k: v for k, v in wide.items()}, Bm=Bm, Cm=Cm)
+    states = finc.selective_scan_states(B, D, L, N, DEV)
+
+    def call(i):
+        x, dt, z, sB, sC = (i["s" + k] for k in ("x", "dt", "z", "Bm", "Cm"))
+        out = [finc.causal_conv_forward(x, w, silu=True),
+               *finc.causal_conv_backward(x, w, z, silu=True)[:2],
+               finc.causal_conv_step(i["rx"], w, torch.zeros(B, D, 3, dtype=BF16, device=DEV)),
+               finc.selective_scan_forward(x, dt, A, sB, sC, skip, z, bias, states=states)]
+        back = finc.selective_scan_backward(x, dt, A, sB, sC, z, states, skip, z, bias)
+        out += [v for v in back.values() if v is not None]
+        out.append(finc.selective_scan_step(i["rx"], i["rdt"], A, i["Bm"], i["Cm"],
+                                            torch.zeros(B, D, N, device=DEV)))
+        out += finc.add_norm_forward(i["wx"], nw, i["wres"], p=0.1, seed=3)
+        out += finc.add_norm_forward(i["wx"], nw, i["wres"], fp8=True)
+        out += finc.add_norm_backward(i["wdy"], i["wx"], nw, i["wres"], p=0.1, seed=3)
+        out.append(finc.dropout(i["wx"], 0.2, 9, residual=i["wres"]))
+        return out
+
+    want = [v.clone() for v in call(inputs)]
+    late = {k: torch.full_like(v, NAN) for k, v in inputs.items()}
+    work = torch.zeros(2, 1 << 29, device=DEV)   # 2 GiB each
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(30):
+            work[0].copy_(work[1])
+        for k, v in late.items():
+            v.copy_(inputs[k])
+        got = call(late)
+    side.synchronize()
+    assert same_bits(want, got)
+
+
+def far(shape, kind, space, at):
+    """A view whose channels lie 2^31 elements and more apart."""
+    B, D, L = shape
+    return space.view(kind).as_strided(shape, ((1 << 31) + 8 * L, (1 << 31) + 4096, 1)
+                                       if D > 1 else ((1 << 31) + 4096, L, 1), at)
+
+
+@pytest.mark.parametrize("L", [40, 200])
+@pytest.mark.parametrize("B,D", [(1, 2), (2, 1)])
+def test_scan_offsets_past_31_bits(L, B, D):
+    """Channels, batch rows and states' rows 2^31 elements apart, in inputs and outputs."""
+    N = 2
+    t, _, r = scan_inputs(B, D, L, N, 1, "gdbp", BF16, L)
+    g, kw = scan_kw(t, None, "gdbp", None)
+    kw.pop("state")
+    dy = r.normal(B, D, L, kind=BF16).to(DEV)
+    space = [torch.empty((1 << 31) + (1 << 20), dtype=BF16, device=DEV) for _ in range(4)]
+    wide = dict(g)
+    for i, k in enumerate(("x", "dt", "z")):
+        wide[k] = far((B, D, L), BF16, space[0], 1000 * i + 1).copy_(g[k])
+    for i, k in enumerate(("Bm", "Cm")):
+        wide[k] = space[0].as_strided((B, 1, N, L), ((1 << 30) + 4096 if B > 1 else 0, 0,
+                                                     (1 << 31) - 4096 if B == 1 else L, 1),
+                                      5000 + 1000 * i).copy_(g[k])
+    states = finc.selective_scan_states(B, D, L, N, DEV)
+    want = finc.selective_scan_forward(**g, **kw, states=states)
+    y = finc.selective_scan_forward(**wide, **kw, out=far((B, D, L), BF16, space[1], 0))
+    assert torch.equal(y, want)
+    want = finc.selective_scan_backward(**g, **kw, dy=dy, states=states)
+    got = finc.selective_scan_backward(
+        **wide, **kw, dy=far((B, D, L), BF16, space[0], 8001).copy_(dy), states=states,
+        dx=far((B, D, L), BF16, space[1], 0), ddt=far((B, D, L), BF16, space[2], 0),
+        dz=far((B, D, L), BF16, space[3], 0))
+    assert all(torch.equal(got[k], want[k]) for k in want)
+
+
+@pytest.mark.parametrize("L,B,D", [(64, 33000, 1024), (129, 16400, 1024)])
+def test_scan_of_more_than_2_31_elements(L, B, D):
+    """The last rows of a tensor of more than 2^31 elements."""
+    N, r = 4, Rand(L)
+    x, dt = (torch.empty(B, D, L, dtype=BF16, device=DEV) for _ in range(2))
+    x.normal_()
+    dt.normal_(-2.0)
+    Bm, Cm = (torch.empty(B, 1, N, L, dtype=BF16, device=DEV).normal_() for _ in range(2))
+    A, end = -torch.exp(r.normal(D, N)).to(DEV), torch.empty(B, D, N, device=DEV)
+    y = finc.selective_scan_forward(x, dt, A, Bm, Cm, state_out=end)
+    for at in (slice(0, 2), slice(B // 2, B // 2 + 2), slice(B - 2, B)):
+        one_end = torch.empty(2, D, N, device=DEV)
+        one = finc.selective_scan_forward(x[at].clone(), dt[at].clone(), A, Bm[at].clone(),
+                                          Cm[at].clone(), state_out=one_end)
+        assert torch.equal(y[at], one) and torch.equal(end[at], one_end)
