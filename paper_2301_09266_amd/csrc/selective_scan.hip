@@ -264,17 +264,16 @@ __device__ inline void convert(typename Vec<E, N>::type v, float (&out)[N]) {
 constexpr int kUnit = 8;   // elements of B and C that a thread moves at once
 
 // What a thread loads of B and C for one part: unit u of 2 N P / 8, the row's last
-// elements where the unit passes its end.
+// elements where the unit passes its end.  `whole`: the raster has a unit's elements.
 __device__ inline int unit_at(int pos, int L) { return L < kUnit ? pos : min(pos, L - kUnit); }
 template <typename E, int T>
 __device__ inline typename Vec<E, kUnit>::type load_tile(const ScanArgs &a, int b, int grp, int u,
-                                                         int p0, int n_pos) {
+                                                         int p0, int n_pos, bool whole) {
     constexpr int Q = 16 * T / kUnit;
     const int r = u / Q, pos = p0 + (u % Q) * kUnit;
     const E *row = (r >= a.N ? a.Cm : a.Bm)
                        .row<const E>(b, (long long)grp * a.N + (r >= a.N ? r - a.N : r));
-    // parts of eight positions a lane are those of longer rasters
-    return load_raw<E, kUnit>(row + unit_at(pos, a.L), n_pos - pos, T == 8 || a.L >= kUnit);
+    return load_raw<E, kUnit>(row + unit_at(pos, a.L), n_pos - pos, whole);
 }
 template <typename E, int T>
 __device__ inline void store_tile(const ScanArgs &a, float *tb, float *tc, int u, int p0, int n_pos,
@@ -301,8 +300,9 @@ __device__ inline void store_tile(const ScanArgs &a, float *tb, float *tc, int u
             to[slot_at<T>(first + k)] = (float)v[k];
 }
 
-// The forward's tiles: two in LDS, and the loads of one more.  Up to K units a thread
-// are loaded ahead, which covers 16 states; the others are loaded as they are stored.
+// The forward's tiles: two in LDS, and the loads of one more; the raster exceeds a unit.
+// Up to K units a thread are loaded ahead, which covers 16 states; the others are loaded as
+// they are stored.
 template <typename E, int T>
 struct Tiles {
     static constexpr int P = 16 * T, K = 2 * 16 * P / kUnit / kThreads > 0 ? 2 * 16 * P / kUnit / kThreads : 1;
@@ -318,7 +318,8 @@ struct Tiles {
         for (int k = 0; k < K; ++k) {
             // fp32's tile leaves no registers for the unit's address (bf16: 3% more time)
             const int u = min((int)threadIdx.x + k * kThreads, units - 1);
-            ahead[k] = load_tile<E, T>(a, b, grp, sizeof(E) == 4 ? afresh(u) : u, part * P, n_pos);
+            ahead[k] =
+                load_tile<E, T>(a, b, grp, sizeof(E) == 4 ? afresh(u) : u, part * P, n_pos, true);
         }
     }
     // The part that was fetched.
@@ -330,7 +331,7 @@ struct Tiles {
                 store_tile<E, T>(a, tb, tc, threadIdx.x + k * kThreads, part * P, n_pos, ahead[k]);
         for (int u = threadIdx.x + K * kThreads; u < units; u += kThreads)
             store_tile<E, T>(a, tb, tc, u, part * P, n_pos,
-                             load_tile<E, T>(a, b, grp, u, part * P, n_pos));
+                             load_tile<E, T>(a, b, grp, u, part * P, n_pos, true));
     }
 };
 
@@ -595,10 +596,10 @@ __device__ inline void short_four(const float *tb, const float *tc, const float 
 
 constexpr int kShortThreads = 256;
 
-// 2^keep positions are a part of the gradients', at whose start the states are kept.
+// The whole raster is one part of the gradients', at whose start the states are kept.
 // ALL: N = 4 S.
 template <typename E, int S, bool ALL>
-__global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a, int keep) {
+__global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a) {
     constexpr int NP = 4 * S;
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const int tid = threadIdx.x, q = tid & 3, n0 = q * S, CB = blockDim.x / 4;
@@ -629,6 +630,8 @@ __global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a, i
     const long long at0 = ((long long)b * a.D + d) * a.N + n0;
     load_upto<float, S>(a.A + (long long)d * a.N + n0, a.N - n0, A2);
     load_upto<float, S>(a.state + at0, a.state ? a.N - n0 : 0, h);
+    if (a.states && live)
+        store_vec<float, S>(a.states + ((long long)b * a.D + d) * NP + n0, h);
 #pragma unroll
     for (int s = 0; s < S; ++s)
         A2[s] = decay(A2[s]);
@@ -663,9 +666,6 @@ __global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a, i
         }
         if (k + 1 < rounds)
             fetch(p0 + 16);
-        if (a.states && live && (p0 >> keep << keep) == p0)
-            store_upto<float, S>(
-                a.states + (((long long)b * a.D + d) * a.parts + (p0 >> keep)) * NP + n0, S, h);
         const float *bp = tb + p0 * NP + n0, *cp = tc + p0 * NP + n0;
         short_four<S, 0, ALL>(bp, cp, delta, dx, A2, a.N - n0, h, q == 0, y);
         if (p0 + 4 < n_pos)
@@ -811,11 +811,12 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
         load_vec<float, S>(at(a.states + (((long long)b * a.D + d) * a.parts + part) * NP, n0), nin);
     };
     const int units = 2 * a.N * (P / kUnit);
+    const bool whole = T == 8 || a.L >= kUnit;   // eight positions a lane: longer rasters
     typename Vec<E, kUnit>::type nt;
     if (parts > 0) {
         if (wave < count)
             fetch(wave, parts - 1);
-        nt = load_tile<E, T>(a, b, grp, min(tid, units - 1), (parts - 1) * P, n_pos);
+        nt = load_tile<E, T>(a, b, grp, min(tid, units - 1), (parts - 1) * P, n_pos, whole);
     }
     for (int part = parts - 1; part >= 0; --part) {
         const int p0 = part * P;
@@ -823,9 +824,9 @@ __global__ __launch_bounds__(64 * kGradWaves) void scan_backward_kernel(GradArgs
             store_tile<E, T>(a, tb, tc, tid, p0, n_pos, nt);
         for (int u = tid + TH; u < units; u += TH)
             store_tile<E, T>(a, tb, tc, u, p0, n_pos,
-                             load_tile<E, T>(a, b, grp, u, p0, n_pos));
+                             load_tile<E, T>(a, b, grp, u, p0, n_pos, whole));
         __syncthreads();
-        nt = load_tile<E, T>(a, b, grp, min(tid, units - 1), max(p0 - P, 0), n_pos);
+        nt = load_tile<E, T>(a, b, grp, min(tid, units - 1), max(p0 - P, 0), n_pos, whole);
         float dB[S][T], dC[S][T];
 #pragma unroll
         for (int s = 0; s < S; ++s)
@@ -1187,9 +1188,16 @@ inline bool scan_shape(int type, int B, int D, int L, int N, int G) {
            (long long)B * G * N < (1ll << 31) && (long long)G * N < (1ll << 31);
 }
 
-// Positions a lane: the gradients' parts and the states' layout depend on it.
-// More than 16 states leave the gradients' registers room for four.
-inline int lane_positions(int L, int N) { return L <= 64 || N > 16 ? 4 : 8; }
+// Positions of a raster that the short form takes, however many rows there are: the bits
+// do not depend on them.  In us, here and by the scan over lanes: 64 positions of 64 x
+// 2048 channels 47 and 137, of 4 x 1024 12 and 7; 32 of those 7.2 and 8.2; but 128 of
+// them 20 and 8.
+constexpr int kShort = 64;
+// Positions a lane: the gradients' parts and the states' layout depend on it.  A short
+// raster is one part of four a lane; more than 16 states leave the gradients' registers
+// room for four.
+inline int lane_positions(int L, int N) { return L <= kShort || N > 16 ? 4 : 8; }
+static_assert(kShort <= 16 * 4, "one part");
 // States a lane of a row in the gradients, a quarter of them all.
 inline int row_states(int N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 inline long long part_count(int L, int N) {
@@ -1214,12 +1222,6 @@ int launch_forward(ScanArgs &c, hipStream_t s) {
     return launched();
 }
 
-// Positions of a raster that the short form takes, however many rows there are: the bits
-// do not depend on them.  In us, here and by the scan over lanes: 64 positions of 64 x
-// 2048 channels 47 and 137, of 4 x 1024 12 and 7; 32 of those 7.2 and 8.2; but 128 of
-// them 20 and 8.
-constexpr int kShort = 64;
-
 template <typename E, int S, bool ALL>
 int launch_short(ScanArgs &c, hipStream_t s) {
     // a wave a workgroup where whole ones would leave compute units without work
@@ -1233,7 +1235,7 @@ int launch_short(ScanArgs &c, hipStream_t s) {
         return FINC_EUNSUPPORTED;
     (void)hipGetLastError();   // the launch check decides
     hipLaunchKernelGGL((scan_short_kernel<E, S, ALL>), grid_of(grid), dim3(threads),
-                       (unsigned)lds, s, c, lane_positions(c.L, c.N) == 4 ? 6 : 7);
+                       (unsigned)lds, s, c);
     return launched();
 }
 template <typename E, int S>
@@ -1250,8 +1252,8 @@ int dispatch_short(ScanArgs &c, hipStream_t s) {
                     : launch_short<E, 16>(c, s);
 }
 
-// The parts of the arguments that both directions check and use.
-bool scan_common(const finc_scan_args *a, ScanArgs &c) {
+// The parts of the arguments that both directions use.
+void scan_common(const finc_scan_args *a, ScanArgs &c) {
     c = ScanArgs{};
     c.x = rows_of(a->x);
     c.dt = rows_of(a->dt);
@@ -1272,7 +1274,6 @@ bool scan_common(const finc_scan_args *a, ScanArgs &c) {
     c.softplus = a->softplus;
     c.parts = (int)part_count(a->L, a->N);
     c.NP = 4 * row_states(a->N);
-    return true;
 }
 
 // Channels of a set: a workgroup a compute unit where there are that many channels,
