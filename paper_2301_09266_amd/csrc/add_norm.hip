@@ -256,10 +256,10 @@ __device__ inline float inv_wide(const float (&r)[V][8], int D, double eps, doub
 
 // R lanes a row, V vectors of 8 a lane: vector v of a lane is lane + v R.  The mean square
 // is in fp32, and again in fp64 for a row where it overflows or, below 2^-80, may have lost
-// squares to underflow.  That costs narrow rows some percent (32768 x 333 in bf16 19.7 us,
-// 18.6 without; in fp64 throughout 20.4) and wide ones nothing.  Bound by memory: 32768 x
-// 2048 in bf16 with an fp32 residual and dropout 150 us, 805 MB at 5.4 TB/s (the last-level
-// cache holds some of them; a copy of 2 GiB reaches 4.8).
+// squares to underflow.  Asked of a scalar that costs nothing (32768 x 333 in bf16 18.7 us;
+// by a comparison of lanes 19.7, in fp64 throughout 20.4).  Bound by memory: 32768 x 2048 in
+// bf16 with an fp32 residual and dropout 150 us, 805 MB at 5.4 TB/s (the last-level cache
+// holds some of them; a copy of 2 GiB reaches 4.8).
 template <typename E, typename F, int R, int V, int TH>
 __global__ __launch_bounds__(TH) void norm_forward_kernel(NormArgs a) {
     __shared__ unsigned lds[2 * (TH / 64)];
@@ -321,8 +321,11 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(NormArgs a) {
         ss = sum_lanes<R>(ss, lds, turn_of);
         const float var = __builtin_fmaf(ss, mean, eps);
         float inv = rsqrtf(var);
-        // the same in all of the row's lanes
-        if (__builtin_expect(!(var >= 0x1p-80f && var < __builtin_inff()), 0))
+        // 2^-80 <= var < inf by its bits, the same in all of the row's lanes
+        int bits = __builtin_bit_cast(int, var);
+        if (R >= 64)
+            bits = __builtin_amdgcn_readfirstlane(bits);
+        if (__builtin_expect((unsigned)bits - (47u << 23) >= (208u << 23), 0))
             inv = inv_wide<R, V>(r, a.D, a.eps, lds64, turn_of64);
         if (live) {
             E *out = (E *)a.y + m * a.sy;
