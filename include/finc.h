@@ -604,7 +604,12 @@ int finc_causal_conv_step(int type, const void *x, long long sx, void *y, long l
  *   state_out: h after each row's length, or NULL; may be state itself.
  *   states: NULL, or for the gradients finc_selective_scan_states_bytes(B, D,
  *   L, N) bytes, 256-byte aligned: h at the starts of the parts that the
- *   backward recomputes, in a private layout. */
+ *   backward recomputes, in a private layout.
+ *   An infinite or NaN input, or a state that overflows, leaves its row's
+ *   channel without finite values from its position on, and no other outputs.
+ *   Up to 64 positions they are the recurrence's; longer rasters, whose parts
+ *   are composed, may have NaN where it keeps an infinity, and so may every
+ *   gradient that the channel has a part in. */
 typedef struct {
     int type, B, D, L, N, G, softplus;
     finc_raster x, dt, z, Bm, Cm, y;

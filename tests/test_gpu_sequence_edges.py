@@ -100,6 +100,22 @@ def test_scan_of_states_without_memory_takes_nothing_from_padding(L, n, N):
                                              if k in ("A", "D", "Bm", "Cm") else 0))
 
 
+@pytest.mark.parametrize("L,at", [(30, 11), (66, 40), (128, 0), (300, 129), (300, 299)])
+@pytest.mark.parametrize("N", [5, 16, 33])
+@pytest.mark.parametrize("what", [INF, -INF, NAN])
+def test_scan_of_one_infinite_input_leaves_the_rest(L, at, N, what):
+    """No finite value of its channel from its position on, and the same bits elsewhere."""
+    t, _, _ = scan_inputs(2, 20, L, N, 1, "gsdbp", F32, L + N)
+    g, kw = scan_kw(t, None, "gsdbp", None)
+    end, end2 = (torch.empty(2, 20, N, device=DEV) for _ in range(2))
+    y = finc.selective_scan_forward(**g, **kw, state_out=end)
+    g["x"][1, 7, at] = what
+    y2 = finc.selective_scan_forward(**g, **kw, state_out=end2)
+    assert not torch.isfinite(y2[1, 7, at:]).any() and not torch.isfinite(end2[1, 7]).any()
+    y2[1, 7, at:], end2[1, 7] = y[1, 7, at:], end[1, 7]
+    assert torch.equal(y2, y) and torch.equal(end2, end)
+
+
 # ---- norm ------------------------------------------------------------------------
 
 
