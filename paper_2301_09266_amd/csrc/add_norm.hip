@@ -665,7 +665,7 @@ enum { kForward, kFp8, kBackward };
 // (gradients of 32768 x 2048 in bf16: 115 us; 276 with four vectors in each lane of a
 // wave a row, whose registers leave a wave a SIMD.  8 bits: 137 us and 185).  Up to
 // 1024 a wave a row, two vectors a lane: with four waves a row a width just below fills
-// two of them (32768 x 1000 in bf16: gradients 63 us and 103, 8 bits 56 and 130).
+// two of them (32768 x 1000 in bf16: gradients 59 us and 103, 8 bits 56 and 130).
 template <typename E, typename F, int KIND, typename Fn>
 void with_width(int D, Fn fn) {
 #define FINC_WIDTH(r, v, th)                                                              \

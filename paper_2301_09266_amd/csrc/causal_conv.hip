@@ -23,7 +23,7 @@ constexpr int kHalo = K <= 1 ? 1 : K <= 2 ? 1 : K <= 3 ? 2 : K <= 5 ? 4 : 8;
 // Elements a thread takes: 16 bytes forward; twice that for the gradients, which
 // recompute K - 1 gradients beside them (8 x 2048 x 4096 in bf16, K 4: 113 us, and 132
 // with 16 bytes; 300 x 9000, where few threads are left, 11.2 and 9.4; with the loads
-// together 94 and 12.0).
+// together 97 and 10.8).
 constexpr int kTileBytes(bool back) { return back ? 32 : 16; }
 template <typename E, bool BACK>
 constexpr int kTile = kTileBytes(BACK) / (int)sizeof(E);
@@ -125,8 +125,8 @@ __global__ __launch_bounds__(kThreads) void conv_forward_kernel(ConvArgs a) {
 
 // One channel and a part of its (row, tile) pairs: dx of the part, and the part's
 // sums for dw and dbias, which stay in registers until the part ends.  Bound by memory:
-// 8 x 2048 x 4096 in bf16, K 4, in 94 us, 4.3 TB/s (111 with each load waited for by
-// itself).
+// 8 x 2048 x 4096 in bf16, K 4, in 97 us in a graph and 88 call by call, 4.2 and 4.6 TB/s
+// (111 in a graph with each load waited for by itself).
 template <typename E, int K, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a) {
     constexpr int V = kTile<E, true>, H = kHalo<K>, Q = K - 1;

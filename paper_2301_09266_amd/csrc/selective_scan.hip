@@ -371,9 +371,9 @@ __device__ inline void sum_rows(const float (&v)[T], float (&out)[T / 4]) {
 // others through LDS; the sums over the states are sums over the rows, and come back
 // to the row that prepared the position.  The block's waves share the tiles of B and
 // C; the next part's tile is stored, and the one after it is under way, while a part
-// is computed.  1 x 2048 x 4096 in bf16, N = 16: 62 us (bytes: 14), and of 4 rows
+// is computed.  1 x 2048 x 4096 in bf16, N = 16: 63 us (bytes: 14), and of 4 rows
 // 198: 393 vector instructions a channel and part of 128, 246 of them the states', which
-// keep the ALU busy 78% of the time with the two waves a SIMD of one row, and throughout
+// keep the ALU busy 77% of the time with the two waves a SIMD of one row, and throughout
 // from four rows on.
 template <typename E, int T>
 __global__ __launch_bounds__(kThreads, 4) void scan_forward_kernel(ScanArgs a) {
@@ -709,7 +709,9 @@ __global__ __launch_bounds__(kShortThreads) void scan_short_kernel(ScanArgs a) {
 // Bound by the vector ALU: 894 instructions a channel and part of 128 positions at N =
 // 16, 568 of them the states' (an exponential and 17 others a position), which two waves
 // a SIMD, all that the gradients of B and C in registers leave, keep 80% busy.  4 x 2048 x
-// 4096 in bf16 with the forward and the sums: 737 us (bytes: 155).
+// 4096 in bf16 with the forward and the sums: 738 us (bytes: 155).  More than 32 states do
+// not fit (43 to 47 vector registers spill), which their time does not show: 4 x 1024 x 1024
+// with 64 states takes 482 us, four times the 123 of 16.
 
 struct GradArgs {
     ScanArgs f;
