@@ -515,7 +515,8 @@ int finc_causal_conv_backward(const finc_conv_args *a, const finc_conv_grads *g,
         if (r2 != FINC_OK)
             return r2;
     }
-    hipLaunchKernelGGL(conv_sum_kernel, grid_of(cdivll((long long)D * (K + 1), 32)), dim3(256), 0, stream, c.partial, c.parts, g->dw, g->dbias, D, K);
+    hipLaunchKernelGGL(conv_sum_kernel, grid_of(cdivll((long long)D * (K + 1), 32)), dim3(256), 0,
+                       stream, c.partial, c.parts, g->dw, g->dbias, D, K);
     return launched();
 }
 

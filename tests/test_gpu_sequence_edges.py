@@ -297,7 +297,8 @@ def back(t, B, L, D, N, dy):
     return finc.selective_scan_backward(**g, **kw, dy=repeated(dy, B), states=states)
 
 
-@pytest.mark.parametrize("B,D,G,N,L", [(1 << 14, 16, 16, 32, 64), (1 << 13, 1 << 10, 1 << 10, 1, 65),
+@pytest.mark.parametrize("B,D,G,N,L", [(1 << 14, 16, 16, 32, 64),
+                                       (1 << 13, 1 << 10, 1 << 10, 1, 65),
                                        (1 << 17, 64, 64, 64, 1)])
 def test_scan_gradients_of_many_rows(B, D, G, N, L):
     """2^24 workgroups' worth of sums of dB and dC, 2^23 workgroups, and 2^30 of sums."""

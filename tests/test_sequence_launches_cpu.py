@@ -110,8 +110,8 @@ def test_ordinary_calls_take_one_row_of_workgroups(drive):
 def test_states_past_the_address_space_are_refused(S, D, N):
     """Entries whose number would wrap to a small one."""
     at = [1 << (40 + i) for i in range(10)]
-    a = finc.SCAN_STEP_ARGS.pack(BF16, 1, S, D, N, 1, 1, at[0], at[1], 0, at[2], at[3], D, D, D, N, N,
-                                 D, at[4], at[5], 0, 0, 0, 0)
+    a = finc.SCAN_STEP_ARGS.pack(BF16, 1, S, D, N, 1, 1, at[0], at[1], 0, at[2], at[3], D, D, D,
+                                 N, N, D, at[4], at[5], 0, 0, 0, 0)
     assert finc.lib().finc_selective_scan_step(a, None) == finc.EINVAL
-    assert finc.lib().finc_causal_conv_step(BF16, at[0], D, at[1], D, at[2], None, None, None, 1, S, D,
-                                            8, 1, None) == finc.EINVAL
+    assert finc.lib().finc_causal_conv_step(BF16, at[0], D, at[1], D, at[2], None, None, None, 1,
+                                            S, D, 8, 1, None) == finc.EINVAL
