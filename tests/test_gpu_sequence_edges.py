@@ -130,6 +130,23 @@ def test_norm_of_large_and_small_rows(D, kind, size):
     ref.close(y, ref.norm(d64(x), d64(w), 0.0), "y", 64 + 2 * D ** 0.5)
 
 
+@pytest.mark.parametrize("D", [3, 333, 1000, 4096])
+@pytest.mark.parametrize("size", [1e22, 1e-25])
+def test_gradients_and_eight_bits_of_large_and_small_rows(D, size):
+    r = Rand(D)
+    x, dy, w = r.normal(9, D, scale=size), r.normal(9, D), 1 + r.normal(D, scale=0.1)
+    chain = 64 + 2 * D ** 0.5
+    x6, w6 = d64(x, True), d64(w, True)
+    want = grads((ref.norm(x6, w6, 0.0) * d64(dy)).sum(), [x6, w6])
+    dx, _, dw = finc.add_norm_backward(dev(dy), dev(x), dev(w), eps=0.0)
+    ref.close(dx, want[0], "dx", chain)
+    ref.close(dw, want[1], "dw", chain + 4 * 9 ** 0.5)
+    q, scale, _ = finc.add_norm_forward(dev(x), dev(w), eps=0.0, fp8=True)
+    want, ws = codes(ref.norm(d64(x), d64(w), 0.0))
+    same_codes(q.cpu(), want)
+    assert torch.equal(scale.cpu(), ws.float())
+
+
 # ---- norm in 8 bits --------------------------------------------------------------
 
 
