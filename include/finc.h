@@ -708,6 +708,130 @@ typedef struct {
 size_t finc_add_norm_workspace_bytes(int M, int D);
 int finc_add_norm_backward(const finc_norm_grad_args *a, hipStream_t stream);
 
+/* Linear attention whose state decays by a factor of its own at every head and
+ * position (the selective scan's recurrence with a DK x DV matrix of states a head),
+ * 1 <= DK, DV <= FINC_MAX_HEAD, G groups of heads that share q and k (G divides H):
+ *   a_t = max(decay[h] + g[b,t,h], -128),
+ *   S_t = exp(a_t) S_{t-1} + k_t v_t^T,   y_t = scale S_t^T q_t.
+ *   Positions are rows, as projections give them: q, k: (B, L, G, DK); v, y:
+ *   (B, L, H, DV); g: (B, L, H) of the type, or absent for 0 (any steps, also of 0: a
+ *   head's decay or a position's is repeated); decay: H fp32, or NULL for 0: a
+ *   constant, for which no gradient is given (a learned one is g's, repeated).
+ *   exp(-128) is 0 in fp32, so that an infinite negative a_t clears the state.
+ *   state: S before the rows, (B, H, DK, DV) fp32, or NULL for 0; state_out: S after
+ *   each row's length, or NULL; may be state itself.
+ *   states: finc_linear_attention_states_bytes(B, L, H, DK, DV) bytes, 256-byte
+ *   aligned: the states at the starts of the parts of FINC_ATTENTION_PART positions
+ *   that are worked on at once, in a private layout, which the gradients read.  NULL
+ *   only where L <= FINC_ATTENTION_PART and no gradients follow.
+ *   Inputs of 16 bits are multiplied exactly, and weights and states beside them
+ *   with 16 bits at least, in sums of fp32.  Positions are worked on in blocks of 64:
+ *   an infinite or NaN input, or one that overflows, leaves its row's heads without
+ *   finite values from the start of its block on (in the gradients: up to its
+ *   block's end), and no other outputs.
+ *   Requirements: B H < 2^24, B L G DK and B L H DV < 2^40 (FINC_EINVAL past them). */
+#define FINC_MAX_HEAD 128
+#define FINC_ATTENTION_PART 512
+
+/* Element (b, t, h, d) at p + b*sb + t*st + h*sh + d (elements; p NULL: absent). */
+typedef struct {
+    void *p;
+    long long sb, st, sh;
+} finc_heads;
+typedef struct {
+    int type, B, L, H, G, DK, DV;
+    finc_heads q, k, v, g, y;
+    const float *decay, *state;
+    float *state_out, *states;
+    const int *lengths;
+    double scale;
+} finc_attention_args;
+size_t finc_linear_attention_states_bytes(int B, int L, int H, int DK, int DV);
+int finc_linear_attention_forward(const finc_attention_args *a, hipStream_t stream);
+
+/* Its gradients, from the states that a forward of the same arguments wrote
+ * (a->state, a->state_out and a->y are not used).  dy (B, L, H, DV), dq, dk, dv and
+ * dg as q, k, v and g (dg may be absent); dstate_out: the gradient of state_out, (B,
+ * H, DK, DV), or NULL for 0; dstate: the gradient of state, or NULL.  workspace:
+ * device, >= finc_linear_attention_workspace_bytes(B, L, H, G, DK, DV) bytes,
+ * 256-byte aligned, overwritten. */
+typedef struct {
+    finc_heads dy, dq, dk, dv, dg;
+    const float *dstate_out;
+    float *dstate;
+    void *workspace;
+} finc_attention_grads;
+size_t finc_linear_attention_workspace_bytes(int B, int L, int H, int G, int DK, int DV);
+int finc_linear_attention_backward(const finc_attention_args *a, const finc_attention_grads *g,
+                                   hipStream_t stream);
+
+/* One position: q, k (B, G, DK), v, y (B, H, DV), g (B, H), whose steps of t are not
+ * used; state (S, H, DK, DV) fp32, contiguous, updated in place. */
+typedef struct {
+    int type, B, S, H, G, DK, DV;
+    finc_heads q, k, v, g, y;
+    const float *decay;
+    float *state;
+    const int *slots;
+    double scale;
+} finc_attention_step_args;
+int finc_linear_attention_step(const finc_attention_step_args *a, hipStream_t stream);
+
+/* Projection of rows, y = act(x w^T + bias) + residual.
+ *   x: (M, K) with rows sx elements apart; w: (N, K), its rows sw apart, of x's type;
+ *   bias: N fp32, or NULL; residual: (M, N), or NULL; y: (M, N), and pre (M, N): x w^T
+ *   + bias, which the gradients read where there is an activation, or NULL; all of the
+ *   type.  act: FINC_ACT_NONE, _RELU, _SILU (p sigmoid(p)) or _GELU (p times the
+ *   normal distribution's function of p).  y may be residual itself, with its rows'
+ *   step.  workspace: device, >= finc_linear_workspace_bytes(type, M, K, N) bytes, 256-byte
+ *   aligned, overwritten (NULL where that is 0).  Sums are fp32, in an order that follows
+ *   from the sizes alone: other than for the other sequence operators, M has a part in
+ *   it.  M N, M K, N K < 2^40 (FINC_EINVAL past them). */
+enum { FINC_ACT_NONE = 0, FINC_ACT_RELU = 1, FINC_ACT_SILU = 2, FINC_ACT_GELU = 3 };
+typedef struct {
+    int type, act, M, K, N;
+    const void *x, *w, *residual;
+    void *y, *pre;
+    long long sx, sw, sres, sy, spre;
+    const float *bias;
+    void *workspace;
+} finc_linear_args;
+size_t finc_linear_workspace_bytes(int type, int M, int K, int N);
+int finc_linear_forward(const finc_linear_args *a, hipStream_t stream);
+
+/* Its gradients, with d = dy act'(pre) rounded to the type (dy itself without an
+ * activation): dx = d w (M, K), dw = d^T x (N, K) and dbias, the sum of d's rows before
+ * they are rounded (N fp32); any of the three may be NULL.  The residual's gradient is
+ * dy.  pre: (M, N) as the forward wrote it, not used without an activation.  dx, dw: the
+ * type.  workspace: device, >= finc_linear_grad_workspace_bytes(type, act, M, K, N)
+ * bytes, 256-byte aligned, overwritten. */
+typedef struct {
+    int type, act, M, K, N;
+    const void *dy, *x, *w, *pre;
+    void *dx, *dw;
+    long long sdy, sx, sw, spre, sdx, sdw;
+    float *dbias;
+    void *workspace;
+} finc_linear_grad_args;
+size_t finc_linear_grad_workspace_bytes(int type, int act, int M, int K, int N);
+int finc_linear_backward(const finc_linear_grad_args *a, hipStream_t stream);
+
+/* Rows of a table: y[m] = scale table[ids[m]], of (V, D) rows st elements apart of
+ * ttype (the type itself or FINC_F32); ids: M ints, or 64-bit ones with wide; an id
+ * outside [0, V) is padding: its row is 0, and it takes part in no gradient. */
+int finc_embed_forward(int type, int ttype, const void *ids, int wide, const void *table,
+                       long long st, void *y, long long sy, int M, int V, int D, double scale,
+                       hipStream_t stream);
+
+/* The table's gradient: dtable[v] = scale times the sum of the rows dy[m] (M, D) with
+ * ids[m] = v, in fp32 and in a fixed order, 0 for a row that no id names; (V, D) fp32,
+ * contiguous.  workspace: device, >= finc_embed_workspace_bytes(M, V, D) bytes, 256-byte
+ * aligned, overwritten. */
+size_t finc_embed_workspace_bytes(int M, int V, int D);
+int finc_embed_backward(int type, const void *ids, int wide, const void *dy, long long sdy,
+                        float *dtable, int M, int V, int D, double scale, void *workspace,
+                        hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

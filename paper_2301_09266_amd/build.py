@@ -19,7 +19,8 @@ SRC = os.path.join(PKG, "csrc", "finc.hip")
 FLOW_SRC = os.path.join(PKG, "csrc", "flow.hip")
 BACKWARD_SRC = os.path.join(PKG, "csrc", "backward.hip")
 SEQ_SRCS = [os.path.join(PKG, "csrc", f)
-            for f in ("selective_scan.hip", "causal_conv.hip", "add_norm.hip")]
+            for f in ("selective_scan.hip", "causal_conv.hip", "add_norm.hip",
+                      "linear_attention.hip", "linear.hip", "embed.hip")]
 LIB = os.path.join(PKG, "csrc", "libfinc.so")
 CALIB_SRC = os.path.join(PKG, "csrc", "calib.hip")
 CALIB_LIB = os.path.join(PKG, "csrc", "libfinc_calib.so")

@@ -1,0 +1,456 @@
+// embed.hip -- rows of a table by their codes, scaled, and the table's gradient
+// (finc_embed_* of finc.h).
+//
+// Both are bound by memory.  The gradient sorts the codes (a radix sort that keeps their
+// order, so that its sums have a fixed one), then sums runs of equal codes: tiles of the
+// sorted list side by side, and what runs on over a tile's end is joined afterwards.
+// Every row of the gradient is written once: by the run that ends in it, or as zeros.
+#include "seq_common.h"
+
+namespace {
+
+using namespace finc_seq;
+
+constexpr int kThreads = 256;
+constexpr int kVec = 8;   // elements a thread takes of a row
+
+struct Ids {
+    const void *p;
+    int wide, V;
+    // the code, or V for padding
+    __device__ unsigned key(long long m) const {
+        const long long v = wide ? ((const long long *)p)[m] : ((const int *)p)[m];
+        return v < 0 || v >= V ? (unsigned)V : (unsigned)v;
+    }
+};
+
+// Eight elements a thread, all of a row's loads under way at once.
+template <typename E, typename R>
+__global__ __launch_bounds__(kThreads) void embed_kernel(Ids ids, const R *table, long long st,
+                                                         E *y, long long sy, int M, int D,
+                                                         FastDiv by_vecs, int vecs, float scale) {
+    const long long i = block_of() * (long long)kThreads + threadIdx.x;
+    if (i >= (long long)M * vecs)
+        return;
+    const int m = fdiv((int)i, by_vecs), col = ((int)i - m * vecs) * kVec;
+    const unsigned k = ids.key(m);
+    const int count = min(D - col, kVec);
+    float v[kVec] = {};
+    if (k < (unsigned)ids.V)
+        load_upto<R, kVec>(table + k * st + col, count, v);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+        v[j] *= scale;
+    if (k >= (unsigned)ids.V)
+#pragma unroll
+        for (int j = 0; j < kVec; ++j)
+            v[j] = 0.0f;
+    store_upto<E, kVec>(y + m * sy + col, count, v);
+}
+
+// ---- the sort ----------------------------------------------------------------------
+// Eight bits a pass from the lowest on.  A block of the list goes to one workgroup, each
+// of whose waves takes a run of it, 64 entries at a time: the lanes of one digit find
+// each other by ballots, and the wave's next place for it is kept in LDS.
+
+constexpr int kDigits = 256, kWaves = kThreads / 64, kItems = 8;
+constexpr int kSortBlock = kThreads * kItems;
+constexpr int kMostBlocks = 512;
+
+struct Sort {
+    Ids ids;
+    const unsigned *key_in;   // NULL: the ids themselves, in order
+    const int *at_in;
+    unsigned *key_out;
+    int *at_out;
+    int *counts;              // (blocks, 256)
+    int M, per, blocks, shift;
+};
+
+__device__ inline unsigned sort_key(const Sort &s, int i) {
+    return s.key_in ? s.key_in[i] : s.ids.key(i);
+}
+
+__global__ __launch_bounds__(kThreads) void count_kernel(Sort s) {
+    __shared__ int n[kDigits];
+    n[threadIdx.x] = 0;
+    __syncthreads();
+    const long long first = (long long)blockIdx.x * s.per;
+    const int end = (int)min(first + s.per, (long long)s.M);
+    for (int i = (int)first + threadIdx.x; i < end; i += kThreads)
+        atomicAdd(&n[sort_key(s, i) >> s.shift & 255u], 1);
+    __syncthreads();
+    s.counts[blockIdx.x * kDigits + threadIdx.x] = n[threadIdx.x];
+}
+
+// Sum of the values of the threads before this one.
+__device__ inline int before(int v, int (&sums)[kThreads]) {
+    const int t = threadIdx.x;
+    sums[t] = v;
+    __syncthreads();
+    for (int d = 1; d < kThreads; d *= 2) {
+        const int u = t >= d ? sums[t - d] : 0;
+        __syncthreads();
+        sums[t] += u;
+        __syncthreads();
+    }
+    const int r = sums[t] - v;
+    __syncthreads();
+    return r;
+}
+
+// The lanes (of those that are `in`) with this lane's digit.
+__device__ inline unsigned long long peers(unsigned digit, bool in) {
+    unsigned long long mask = __ballot(in);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const unsigned long long have = __ballot(digit >> b & 1u);
+        mask &= digit >> b & 1u ? have : ~have;
+    }
+    return mask;
+}
+
+__global__ __launch_bounds__(kThreads) void place_kernel(Sort s) {
+    __shared__ int place[kWaves][kDigits], sums[kThreads];
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6, block = blockIdx.x;
+    // this digit's place: all of the smaller ones, and those of the blocks before
+    int all = 0, earlier = 0;
+    for (int b = 0; b < s.blocks; ++b) {
+        const int n = s.counts[b * kDigits + t];
+        all += n;
+        earlier += b < block ? n : 0;
+    }
+    const int start = before(all, sums) + earlier;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+        place[i][t] = 0;
+    __syncthreads();
+    const long long first = (long long)block * s.per;
+    const int n = (int)(min(first + s.per, (long long)s.M) - first);
+    const int share = (n + kWaves - 1) / kWaves;   // of one wave
+    const int lo = min(w * share, n), hi = min(lo + share, n);
+    for (int i = lo + lane; i < hi; i += 64)
+        atomicAdd(&place[w][sort_key(s, (int)first + i) >> s.shift & 255u], 1);
+    __syncthreads();
+    int at = start;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        const int c = place[i][t];
+        place[i][t] = at;
+        at += c;
+    }
+    __syncthreads();
+    for (int base = lo; base < hi; base += 64) {
+        const int i = base + lane;
+        const bool in = i < hi;
+        const unsigned key = in ? sort_key(s, (int)first + i) : 0u;
+        const unsigned digit = key >> s.shift & 255u;
+        const unsigned long long same = peers(digit, in);
+        const int rank = __popcll(same & ((1ull << lane) - 1ull));
+        const int to = in ? place[w][digit] + rank : 0;
+        wave_exchange();
+        if (in) {
+            s.key_out[to] = key;
+            s.at_out[to] = s.at_in ? s.at_in[(int)first + i] : (int)first + i;
+            if (rank == 0)
+                place[w][digit] += __popcll(same);
+        }
+        wave_exchange();
+    }
+}
+
+// ---- the sums -------------------------------------------------------------------------
+
+constexpr int kTile = 32;   // entries of the sorted list that one wave's lanes add up
+
+struct Sum {
+    const unsigned *key;
+    const int *at;
+    const void *dy;
+    long long sdy;
+    float *dtable, *head, *tail;   // a tile's first and last run where they pass its ends
+    float scale;
+    int M, V, D, tiles, lanes, slices, fill;   // lanes of a row, slices of its columns
+    long long sum_blocks;
+};
+
+// A group of lanes takes a tile of the list and up to 8 columns a lane.
+template <typename E>
+__device__ void sum_tiles(const Sum &s, long long group, int lane) {
+    const int tile = (int)(group / s.slices), slice = (int)(group - (long long)tile * s.slices);
+    if (tile >= s.tiles)
+        return;
+    const int col = (slice * s.lanes + lane) * kVec, count = min(s.D - col, kVec);
+    const int first = tile * kTile, n = min(kTile, s.M - first);
+    const unsigned V = (unsigned)s.V;
+    const unsigned prior = first > 0 ? s.key[first - 1] : ~0u;
+    const unsigned next = first + n < s.M ? s.key[first + n] : ~0u;
+    constexpr int kAhead = 8;
+    float sum[kVec] = {};
+    unsigned run = s.key[first];
+    bool headed = prior == run;   // the run began before the tile
+    auto flush = [&](bool open) {
+        if (run < V && count > 0) {
+            float *to = headed ? s.head + (long long)tile * s.D
+                               : (open ? s.tail + (long long)tile * s.D
+                                       : s.dtable + (long long)run * s.D);
+            if (!headed && !open)
+#pragma unroll
+                for (int j = 0; j < kVec; ++j)
+                    sum[j] *= s.scale;
+            store_upto<float, kVec>(to + col, count, sum);
+        }
+    };
+    for (int e = 0; e < n; e += kAhead) {
+        unsigned k[kAhead];
+        float v[kAhead][kVec];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int at = first + min(e + i, n - 1);
+            k[i] = s.key[at];
+            load_upto<E, kVec>((const E *)s.dy + s.at[at] * s.sdy + col, k[i] < V ? count : 0, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (e + i < n) {
+                if (k[i] != run) {
+                    flush(false);
+                    run = k[i];
+                    headed = false;
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j)
+                        sum[j] = 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < kVec; ++j)
+                    sum[j] += v[i][j];
+            }
+    }
+    flush(next == run);
+}
+
+// Rows that no code names: zeros.  A wave looks for 64 of them in the list.
+__device__ inline void fill_rows(const Sum &s, long long wave, int lane) {
+    const long long v0 = wave * 64;
+    if (v0 >= s.V)
+        return;
+    const int v = (int)min(v0 + lane, (long long)s.V - 1);
+    int lo = 0, hi = s.M;   // the first entry of at least v
+    while (lo < hi) {
+        const int mid = lo + (hi - lo) / 2;
+        if (s.key[mid] < (unsigned)v)
+            lo = mid + 1;
+        else
+            hi = mid;
+    }
+    const bool there = lo < s.M && s.key[lo] == (unsigned)v;
+    unsigned long long absent = __ballot(v0 + lane < s.V && !there);
+    const float zero[4] = {0, 0, 0, 0};
+    while (absent) {
+        const int i = __ffsll((long long)absent) - 1;
+        absent &= absent - 1;
+        float *p = s.dtable + (v0 + i) * s.D;
+        for (int c = lane * 4; c < s.D; c += 256)
+            store_upto<float, 4>(p + c, min(s.D - c, 4), zero);
+    }
+}
+
+template <typename E>
+__global__ __launch_bounds__(kThreads) void sum_kernel(Sum s) {
+    const long long block = block_of();
+    const int t = threadIdx.x;
+    if (block < s.sum_blocks) {
+        const int groups = kThreads / s.lanes;
+        sum_tiles<E>(s, block * groups + t / s.lanes, t & (s.lanes - 1));
+    } else
+        fill_rows(s, (block - s.sum_blocks) * kWaves + (t >> 6), t & 63);
+}
+
+// Runs over several tiles: a workgroup for the one that begins in its tile and passes the
+// end.  Its groups of lanes take a contiguous share of the tiles each.
+__global__ __launch_bounds__(kThreads) void join_runs_kernel(Sum s) {
+    __shared__ float part[kThreads * kVec];
+    __shared__ int more;
+    const int at = block_of(), tile = at / s.slices, slice = at - tile * s.slices;
+    if (tile + 1 >= s.tiles)
+        return;
+    const int t = threadIdx.x, first = tile * kTile, last = first + kTile - 1;
+    const unsigned run = s.key[last];
+    if (run >= (unsigned)s.V || s.key[last + 1] != run || (first > 0 && s.key[first - 1] == run))
+        return;
+    // the tiles that begin with the run
+    int n = 0;
+    for (;;) {
+        if (t == 0)
+            more = kThreads;
+        __syncthreads();
+        const long long u = (long long)tile + 1 + n + t;
+        if (u >= s.tiles || s.key[u * kTile] != run)
+            atomicMin(&more, t);
+        __syncthreads();
+        const int got = more;
+        __syncthreads();
+        n += got;
+        if (got < kThreads)
+            break;
+    }
+    const int groups = kThreads / s.lanes, g = t / s.lanes, lane = t & (s.lanes - 1);
+    const int col = (slice * s.lanes + lane) * kVec, count = min(s.D - col, kVec);
+    const int share = (n + groups - 1) / groups, lo = min(g * share, n), hi = min(lo + share, n);
+    float sum[kVec] = {};
+    if (g == 0)
+        load_upto<float, kVec>(s.tail + (long long)tile * s.D + col, count, sum);
+    for (int i = lo; i < hi; ++i) {
+        float v[kVec];
+        load_upto<float, kVec>(s.head + ((long long)tile + 1 + i) * s.D + col, count, v);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j)
+            sum[j] += v[j];
+    }
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+        part[j * kThreads + t] = sum[j];
+    __syncthreads();
+    if (g == 0) {
+        for (int i = 1; i < groups; ++i)
+#pragma unroll
+            for (int j = 0; j < kVec; ++j)
+                sum[j] += part[j * kThreads + i * s.lanes + lane];
+#pragma unroll
+        for (int j = 0; j < kVec; ++j)
+            sum[j] *= s.scale;
+        if (count > 0)
+            store_upto<float, kVec>(s.dtable + (long long)run * s.D + col, count, sum);
+    }
+}
+
+// ---- the host ----------------------------------------------------------------------------
+
+bool embed_shape(int M, int V, int D) {
+    return M >= 0 && V >= 0 && D >= 1 && (long long)M * ((D + 7) / 8) < (1ll << 31) &&
+           (long long)V * ((D + 7) / 8) < (1ll << 37) && M < (1 << 30) && V < (1 << 30);
+}
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+Region rows(const void *p, long long step, long long M, int D, int size) {
+    return {p, M, step, 1, 0, D, size};
+}
+int tiles_of(int M) { return (M + kTile - 1) / kTile; }
+
+}  // namespace
+
+extern "C" {
+
+int finc_embed_forward(int type, int ttype, const void *ids, int wide, const void *table,
+                       long long st, void *y, long long sy, int M, int V, int D, double scale,
+                       hipStream_t stream) {
+    if (!type_size(type) || (ttype != type && ttype != FINC_F32) || !embed_shape(M, V, D))
+        return FINC_EINVAL;
+    const Region in[] = {flat(ids, M, wide ? 8 : 4), rows(table, st, V, D, type_size(ttype))};
+    const Region out[] = {rows(y, sy, M, D, type_size(type))};
+    for (const Region &r : in)
+        if (!readable(r))
+            return FINC_EINVAL;
+    if (!writable(out[0]) || !disjoint(in, out))
+        return FINC_EINVAL;
+    if (M == 0)
+        return FINC_OK;
+    const int vecs = (D + kVec - 1) / kVec;
+    const dim3 grid = grid_of(cdivll((long long)M * vecs, kThreads));
+    const Ids i = {ids, wide, V};
+    with_type(type, [&](auto e) {
+        typedef decltype(e) E;
+        if (ttype == type)
+            embed_kernel<E, E><<<grid, kThreads, 0, stream>>>(i, (const E *)table, st, (E *)y, sy, M,
+                                                              D, make_fastdiv(vecs), vecs,
+                                                              (float)scale);
+        else
+            embed_kernel<E, float><<<grid, kThreads, 0, stream>>>(
+                i, (const float *)table, st, (E *)y, sy, M, D, make_fastdiv(vecs), vecs,
+                (float)scale);
+    });
+    return launched();
+}
+
+size_t finc_embed_workspace_bytes(int M, int V, int D) {
+    if (!embed_shape(M, V, D))
+        return 0;
+    return 4 * round256((size_t)M * 4) + round256((size_t)kMostBlocks * kDigits * 4) +
+           2 * round256((size_t)tiles_of(M) * D * 4);
+}
+
+int finc_embed_backward(int type, const void *ids, int wide, const void *dy, long long sdy,
+                        float *dtable, int M, int V, int D, double scale, void *workspace,
+                        hipStream_t stream) {
+    if (!type_size(type) || !embed_shape(M, V, D) || ((uintptr_t)workspace & 255u))
+        return FINC_EINVAL;
+    const size_t space = finc_embed_workspace_bytes(M, V, D);
+    const Region in[] = {flat(ids, M, wide ? 8 : 4), rows(dy, sdy, M, D, type_size(type))};
+    const Region out[] = {flat(dtable, (long long)V * D, 4), flat(workspace, (long long)space, 1)};
+    for (const Region &r : in)
+        if (!readable(r))
+            return FINC_EINVAL;
+    for (const Region &r : out)
+        if (!readable(r))
+            return FINC_EINVAL;
+    if (!disjoint(in, out))
+        return FINC_EINVAL;
+    if (V == 0)
+        return FINC_OK;
+    char *ws = (char *)workspace;
+    auto take = [&](size_t bytes) {
+        char *p = ws;
+        ws += round256(bytes);
+        return p;
+    };
+    unsigned *keys[2];
+    int *at[2];
+    for (int i = 0; i < 2; ++i) {
+        keys[i] = (unsigned *)take((size_t)M * 4);
+        at[i] = (int *)take((size_t)M * 4);
+    }
+    Sort o = {};
+    o.ids = {ids, wide, V};
+    o.counts = (int *)take((size_t)kMostBlocks * kDigits * 4);
+    o.M = M;
+    o.per = (int)cdivll(M, kMostBlocks);
+    o.per = o.per < kSortBlock ? kSortBlock : o.per;
+    o.blocks = (int)cdivll(M, o.per);
+    int from = 0;
+    if (M > 0)
+        for (o.shift = 0; o.shift < 32 && (o.shift == 0 || V >> o.shift); o.shift += 8) {
+            o.key_out = keys[from ^ 1];
+            o.at_out = at[from ^ 1];
+            count_kernel<<<o.blocks, kThreads, 0, stream>>>(o);
+            place_kernel<<<o.blocks, kThreads, 0, stream>>>(o);
+            from ^= 1;
+            o.key_in = keys[from];
+            o.at_in = at[from];
+        }
+    Sum s = {};
+    s.key = keys[from];
+    s.at = at[from];
+    s.dy = dy;
+    s.sdy = sdy;
+    s.dtable = dtable;
+    s.tiles = tiles_of(M);
+    s.head = (float *)take((size_t)s.tiles * D * 4);
+    s.tail = (float *)take((size_t)s.tiles * D * 4);
+    s.scale = (float)scale;
+    s.M = M;
+    s.V = V;
+    s.D = D;
+    s.lanes = 1;
+    while (s.lanes < 64 && s.lanes * kVec < D)
+        s.lanes *= 2;
+    s.slices = (D + s.lanes * kVec - 1) / (s.lanes * kVec);
+    s.sum_blocks = cdivll((long long)s.tiles * s.slices, kThreads / s.lanes);
+    const long long blocks = s.sum_blocks + cdivll(V, 64 * kWaves);
+    with_type(type, [&](auto e) {
+        sum_kernel<decltype(e)><<<grid_of(blocks), kThreads, 0, stream>>>(s);
+    });
+    if (s.tiles > 1)
+        join_runs_kernel<<<grid_of((long long)s.tiles * s.slices), kThreads, 0, stream>>>(s);
+    return launched();
+}
+
+}  // extern "C"

@@ -29,11 +29,13 @@ _ull = ctypes.c_ulonglong
 _d = ctypes.c_double
 F32, BF16, F16 = 0, 1, 2
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-MAX_TAPS, MAX_STATE, MAX_ROW = 8, 64, 16384
+MAX_TAPS, MAX_STATE, MAX_ROW, MAX_HEAD, ATTENTION_PART = 8, 64, 16384, 128, 512
+_ACTS = {None: 0, "relu": 1, "silu": 2, "gelu": 3}
 
 # The sequence operators' argument structures, in the header's order of fields and
 # with the platform's alignment (packing takes a fraction of a ctypes structure's
-# time, which counts where a call takes a few microseconds).  A raster is "Pqq".
+# time, which counts where a call takes a few microseconds).  A raster is "Pqq", heads
+# are "Pqqq".
 CONV_ARGS = struct.Struct("@6i Pqq Pqq 5P")
 CONV_GRADS = struct.Struct("@Pqq Pqq 5P")
 SCAN_ARGS = struct.Struct("@7i Pqq Pqq Pqq Pqq Pqq Pqq 7P")
@@ -41,6 +43,11 @@ SCAN_GRADS = struct.Struct("@Pqq Pqq Pqq Pqq Pqq Pqq 6P")
 SCAN_STEP_ARGS = struct.Struct("@7i 5P 6q 6P")
 NORM_ARGS = struct.Struct("@4i 4P 4q 2P 2d 2Q")
 NORM_GRAD_ARGS = struct.Struct("@4i 5P 5q 2P 2d 2Q P")
+ATTENTION_ARGS = struct.Struct("@7i Pqqq Pqqq Pqqq Pqqq Pqqq 5P d")
+ATTENTION_GRADS = struct.Struct("@Pqqq Pqqq Pqqq Pqqq Pqqq 3P")
+ATTENTION_STEP_ARGS = struct.Struct("@7i Pqqq Pqqq Pqqq Pqqq Pqqq 3P d")
+LINEAR_ARGS = struct.Struct("@5i 5P 5q 2P")
+LINEAR_GRAD_ARGS = struct.Struct("@5i 6P 6q 2P")
 
 # name -> (restype, argtypes); mirrors include/finc.h
 SIGNATURES = {
@@ -127,6 +134,18 @@ SIGNATURES = {
     "finc_add_norm_forward": (_i, [_vp, _vp]),
     "finc_add_norm_workspace_bytes": (_sz, [_i, _i]),
     "finc_add_norm_backward": (_i, [_vp, _vp]),
+    "finc_linear_attention_states_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "finc_linear_attention_forward": (_i, [_vp, _vp]),
+    "finc_linear_attention_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
+    "finc_linear_attention_backward": (_i, [_vp, _vp, _vp]),
+    "finc_linear_attention_step": (_i, [_vp, _vp]),
+    "finc_linear_workspace_bytes": (_sz, [_i, _i, _i, _i]),
+    "finc_linear_forward": (_i, [_vp, _vp]),
+    "finc_linear_grad_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "finc_linear_backward": (_i, [_vp, _vp]),
+    "finc_embed_forward": (_i, [_i, _i, _vp, _i, _vp, _ll, _vp, _ll, _i, _i, _i, _d, _vp]),
+    "finc_embed_workspace_bytes": (_sz, [_i, _i, _i]),
+    "finc_embed_backward": (_i, [_i, _vp, _i, _vp, _ll, _vp, _i, _i, _i, _d, _vp, _vp]),
 }
 
 
@@ -1344,3 +1363,276 @@ def add_norm_backward(dy: torch.Tensor, r: torch.Tensor, w: torch.Tensor,
                             ws.data_ptr())
     _check(lib_.finc_add_norm_backward(a, _stream()), "finc_add_norm_backward")
     return dx, dresidual, dw
+
+
+# Rows of positions: q and k are (B, L, G, DK), v and y (B, L, H, DV), g (B, L, H); any
+# steps between rows and heads, so that a projection's parts are taken as they are.
+
+_NO_HEADS = (0, 0, 0, 0)
+
+
+def _heads(t: torch.Tensor | None):
+    """A (B, L, H, D) tensor, or (B, L, H) of single elements, as the ABI's finc_heads."""
+    if t is None:
+        return _NO_HEADS
+    st = t.stride()
+    return t.data_ptr(), st[0], st[1], st[2]
+
+
+def _step_heads(t: torch.Tensor | None):
+    """A (B, H, D) tensor, or (B, H), of one position."""
+    if t is None:
+        return _NO_HEADS
+    st = t.stride()
+    return t.data_ptr(), st[0], 0, st[1]
+
+
+def _element(t: torch.Tensor, name: str, dev: int, dtype, shape):
+    """A tensor of single elements, with any steps."""
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the device of the other tensors")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return t
+
+
+def _attention_inputs(q, k, v, g, decay, rows, form):
+    """(device, type id, groups, DK, heads, DV, the address of decay) of q, k (rows, G, DK),
+    v (rows, H, DV) and g (rows, H)."""
+    G, DK = _dims(q, "q", f"({form}, G, DK)")[rows:]
+    H, DV = _dims(v, "v", f"({form}, H, DV)")[rows:]
+    if not 1 <= DK <= MAX_HEAD or not 1 <= DV <= MAX_HEAD:
+        raise ValueError(f"heads of {DK} and {DV} elements, expected 1 to {MAX_HEAD}")
+    if G < 1 or H < 1 or H % G:
+        raise ValueError(f"{G} groups do not divide {H} heads")
+    dev, kind = _type(q, "q")
+    T = q.dtype
+    _act(k, "k", dev, T, q.shape)
+    _act(v, "v", dev, T, (*q.shape[:rows], H, DV))
+    if g is not None:
+        _element(g, "g", dev, T, (*q.shape[:rows], H))
+    return dev, kind, G, DK, H, DV, _param(decay, "decay", dev, (H,))
+
+
+def linear_attention_states(B: int, L: int, H: int, DK: int, DV: int, device) -> torch.Tensor:
+    """A buffer for the states that a forward keeps for its backward."""
+    n = _require_lib().finc_linear_attention_states_bytes(B, L, H, DK, DV)
+    return torch.empty(max(n, 256) // 4, dtype=torch.float32, device=device)
+
+
+def linear_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *,
+                             g: torch.Tensor | None = None, decay: torch.Tensor | None = None,
+                             scale: float = 1.0, state: torch.Tensor | None = None,
+                             lengths: torch.Tensor | None = None,
+                             out: torch.Tensor | None = None,
+                             state_out: torch.Tensor | None = None,
+                             states: torch.Tensor | None = None):
+    """y (B, L, H, DV) of linear attention with the log decays decay (H) + g (B, L, H):
+    q and k (B, L, G, DK) shared by groups of heads, v (B, L, H, DV) (see
+    finc_linear_attention_forward).  state_out (B, H, DK, DV) is written if given, and
+    may be state; states (linear_attention_states) is what
+    linear_attention_backward reads."""
+    lib_ = _require_lib()
+    dev, kind, G, DK, H, DV, dp = _attention_inputs(q, k, v, g, decay, 2, "B, L")
+    B, L = q.shape[:2]
+    y = _out(out, v, "out", dev)
+    n = lib_.finc_linear_attention_states_bytes(B, L, H, DK, DV)
+    if states is None and L > ATTENTION_PART:
+        states = _space(None, n, dev)
+    sp = 0 if states is None else _space(states, n, dev, "states").data_ptr()
+    st = (B, H, DK, DV)
+    a = ATTENTION_ARGS.pack(kind, B, L, H, G, DK, DV, *_heads(q), *_heads(k), *_heads(v),
+                            *_heads(g), *_heads(y), dp, _param(state, "state", dev, st),
+                            _param(state_out, "state_out", dev, st), sp,
+                            _param(lengths, "lengths", dev, (B,), torch.int32), scale)
+    _check(lib_.finc_linear_attention_forward(a, _stream()), "finc_linear_attention_forward")
+    return y
+
+
+def linear_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                              dy: torch.Tensor, states: torch.Tensor, *,
+                              g: torch.Tensor | None = None, decay: torch.Tensor | None = None,
+                              scale: float = 1.0, lengths: torch.Tensor | None = None,
+                              dstate_out: torch.Tensor | None = None,
+                              dq: torch.Tensor | None = None, dk: torch.Tensor | None = None,
+                              dv: torch.Tensor | None = None,
+                              workspace: torch.Tensor | None = None) -> dict:
+    """The gradients of a linear_attention_forward that wrote `states`, for the gradients
+    dy and dstate_out of its outputs: a dict of dq, dk, dv, dg (None without g) and
+    dstate."""
+    lib_ = _require_lib()
+    dev, kind, G, DK, H, DV, dp = _attention_inputs(q, k, v, g, decay, 2, "B, L")
+    B, L = q.shape[:2]
+    _act(dy, "dy", dev, v.dtype, v.shape)
+    st = (B, H, DK, DV)
+    n = lib_.finc_linear_attention_states_bytes(B, L, H, DK, DV)
+    sp = _space(states, n, dev, "states").data_ptr()
+    dq, dk, dv = _out(dq, q, "dq", dev), _out(dk, k, "dk", dev), _out(dv, v, "dv", dev)
+    dg = None if g is None else _empty(g, g.dtype)
+    dstate = torch.empty(st, dtype=torch.float32, device=q.device)
+    ws = _space(workspace, lib_.finc_linear_attention_workspace_bytes(B, L, H, G, DK, DV), dev)
+    a = ATTENTION_ARGS.pack(kind, B, L, H, G, DK, DV, *_heads(q), *_heads(k), *_heads(v),
+                            *_heads(g), *_NO_HEADS, dp, 0, 0, sp,
+                            _param(lengths, "lengths", dev, (B,), torch.int32), scale)
+    o = ATTENTION_GRADS.pack(*_heads(dy), *_heads(dq), *_heads(dk), *_heads(dv), *_heads(dg),
+                             _param(dstate_out, "dstate_out", dev, st), dstate.data_ptr(),
+                             ws.data_ptr())
+    _check(lib_.finc_linear_attention_backward(a, o, _stream()), "finc_linear_attention_backward")
+    return dict(dq=dq, dk=dk, dv=dv, dg=dg, dstate=dstate)
+
+
+def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                          state: torch.Tensor, *, g: torch.Tensor | None = None,
+                          decay: torch.Tensor | None = None, scale: float = 1.0,
+                          slots: torch.Tensor | None = None, out: torch.Tensor | None = None):
+    """One position: y (B, H, DV) of q, k (B, G, DK), v (B, H, DV) and g (B, H); row b's
+    state is entry slots[b] (or b) of state (S, H, DK, DV), updated in place.  A slot
+    outside [0, S) is an idle row (y 0)."""
+    lib_ = _require_lib()
+    dev, kind, G, DK, H, DV, dp = _attention_inputs(q, k, v, g, decay, 1, "B")
+    B, S = q.shape[0], _dims(state, "state", "(S, H, DK, DV)")[0]
+    y = _out(out, v, "out", dev)
+    a = ATTENTION_STEP_ARGS.pack(kind, B, S, H, G, DK, DV, *_step_heads(q), *_step_heads(k),
+                                 *_step_heads(v), *_step_heads(g), *_step_heads(y), dp,
+                                 _param(state, "state", dev, (S, H, DK, DV)),
+                                 _slots(slots, dev, B, S), scale)
+    _check(lib_.finc_linear_attention_step(a, _stream()), "finc_linear_attention_step")
+    return y
+
+
+def _act_id(act):
+    if act not in _ACTS:
+        raise ValueError(f"act is {act!r}, expected one of {tuple(_ACTS)}")
+    return _ACTS[act]
+
+
+def _matrix(t: torch.Tensor, name: str, dev: int, dtype, shape=None):
+    """A matrix of activations' type, contiguous in its last dimension: its rows' step."""
+    _dims(t, name, "(N, K)")
+    _act(t, name, dev, dtype, t.shape if shape is None else shape)
+    return t.stride(0)
+
+
+def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, *,
+                   act: str | None = None, residual: torch.Tensor | None = None,
+                   out: torch.Tensor | None = None, pre_out: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None):
+    """act(x w^T + bias) + residual of rows x (..., K) and w (N, K) of one type, bias (N)
+    float32; act is None, "relu", "silu" or "gelu" (see finc_linear_forward).  pre_out
+    (..., N) takes x w^T + bias, which linear_backward reads where there is an act; out
+    may be residual."""
+    lib_ = _require_lib()
+    M, K = _row_dims(x)
+    dev, kind = _type(x)
+    sw, N = _matrix(w, "w", dev, x.dtype), w.shape[0]
+    if w.shape[1] != K:
+        raise ValueError(f"w has shape {tuple(w.shape)}, expected (N, {K})")
+    shape = (*x.shape[:-1], N)
+    if out is None:
+        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    else:
+        y = _act(out, "out", dev, x.dtype, shape)
+    rp = rs = pp = ps = 0
+    if residual is not None:
+        rp = _act(residual, "residual", dev, x.dtype, shape).data_ptr()
+        rs = _rows(residual, "residual")
+    if pre_out is not None:
+        pp = _act(pre_out, "pre_out", dev, x.dtype, shape).data_ptr()
+        ps = _rows(pre_out, "pre_out")
+    n, ws = lib_.finc_linear_workspace_bytes(kind, M, K, N), 0
+    if n or workspace is not None:
+        ws = _space(workspace, n, dev).data_ptr()
+    a = LINEAR_ARGS.pack(kind, _act_id(act), M, K, N, x.data_ptr(), w.data_ptr(), rp, y.data_ptr(),
+                         pp, _rows(x, "x"), sw, rs, _rows(y, "out"), ps,
+                         _param(bias, "bias", dev, (N,)), ws)
+    _check(lib_.finc_linear_forward(a, _stream()), "finc_linear_forward")
+    return y
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
+                    pre: torch.Tensor | None = None, *, act: str | None = None,
+                    bias: bool = True, dx: torch.Tensor | None = None,
+                    workspace: torch.Tensor | None = None):
+    """(dx, dw, dbias) of linear_forward for the gradient dy (..., N) of its output, which
+    is the residual's too; pre is what pre_out took, needed with an act.  dx and dw are of
+    x's type, dbias is float32, or None without bias."""
+    lib_ = _require_lib()
+    M, K = _row_dims(x)
+    dev, kind = _type(x)
+    sw, N = _matrix(w, "w", dev, x.dtype), w.shape[0]
+    if w.shape[1] != K:
+        raise ValueError(f"w has shape {tuple(w.shape)}, expected (N, {K})")
+    shape, act = (*x.shape[:-1], N), _act_id(act)
+    _act(dy, "dy", dev, x.dtype, shape)
+    pp = ps = 0
+    if act:
+        if pre is None:
+            raise ValueError("the gradients of an act need pre")
+        pp, ps = _act(pre, "pre", dev, x.dtype, shape).data_ptr(), _rows(pre, "pre")
+    dx = _out(dx, x, "dx", dev)
+    dw = _empty(w, w.dtype)
+    db = torch.empty(N, dtype=torch.float32, device=x.device) if bias else None
+    ws = _space(workspace, lib_.finc_linear_grad_workspace_bytes(kind, act, M, K, N), dev)
+    a = LINEAR_GRAD_ARGS.pack(kind, act, M, K, N, dy.data_ptr(), x.data_ptr(), w.data_ptr(), pp,
+                              dx.data_ptr(), dw.data_ptr(), _rows(dy, "dy"), _rows(x, "x"), sw, ps,
+                              _rows(dx, "dx"), K, 0 if db is None else db.data_ptr(),
+                              ws.data_ptr())
+    _check(lib_.finc_linear_backward(a, _stream()), "finc_linear_backward")
+    return dx, dw, db
+
+
+def _ids(t: torch.Tensor, dev: int | None = None):
+    """(device, whether ids are 64-bit) of a contiguous tensor of ids."""
+    if not t.is_cuda:
+        raise ValueError("ids must be a device tensor")
+    at = t.get_device()
+    if at != (_current_device() if dev is None else dev):
+        raise ValueError("ids must be on the current device")
+    if t.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"ids must be int32 or int64, not {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError("ids must be contiguous")
+    return at, int(t.dtype == torch.int64)
+
+
+def embed_forward(ids: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0, dtype=None,
+                  out: torch.Tensor | None = None):
+    """scale table[ids] (..., D) of ids (...), int32 or int64, and a table (V, D) of the
+    output's type (dtype, or the table's) or float32.  An id outside [0, V) is padding:
+    its row is 0."""
+    lib_ = _require_lib()
+    dev, wide = _ids(ids)
+    V, D = _dims(table, "table", "(V, D)")
+    T = (table.dtype if out is None else out.dtype) if dtype is None else dtype
+    if T not in _TYPES or table.dtype not in (T, torch.float32):
+        raise ValueError(f"table must be {T} or float32, not {table.dtype}")
+    st, shape = _matrix(table, "table", dev, table.dtype), (*ids.shape, D)
+    if out is None:
+        y = torch.empty(shape, dtype=T, device=ids.device)
+    else:
+        y = _act(out, "out", dev, T, shape)
+    _check(lib_.finc_embed_forward(_TYPES[T], _TYPES[table.dtype], ids.data_ptr(), wide,
+                                   table.data_ptr(), st, y.data_ptr(), _rows(y, "out"),
+                                   ids.numel(), V, D, scale, _stream()), "finc_embed_forward")
+    return y
+
+
+def embed_backward(ids: torch.Tensor, dy: torch.Tensor, V: int, *, scale: float = 1.0,
+                   dtable: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """The gradient (V, D), float32, of embed_forward's table for the gradient dy (..., D)
+    of its output: every row is written, those that no id names with 0."""
+    lib_ = _require_lib()
+    dev, kind = _type(dy, "dy")
+    _, wide = _ids(ids, dev)
+    M, D = _row_dims(dy, "dy")
+    if dy.shape[:-1] != ids.shape:
+        raise ValueError(f"dy has shape {tuple(dy.shape)}, expected {(*ids.shape, D)}")
+    if dtable is None:
+        dtable = torch.empty((V, D), dtype=torch.float32, device=dy.device)
+    ws = _space(workspace, lib_.finc_embed_workspace_bytes(M, V, D), dev)
+    _check(lib_.finc_embed_backward(kind, ids.data_ptr(), wide, dy.data_ptr(), _rows(dy, "dy"),
+                                    _param(dtable, "dtable", dev, (V, D)), M, V, D, scale,
+                                    ws.data_ptr(), _stream()), "finc_embed_backward")
+    return dtable
