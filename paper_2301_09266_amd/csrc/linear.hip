@@ -64,6 +64,31 @@ struct Gemm {
     int tiles_m, tiles_n;
 };
 
+// Bias, what the gradients keep, activation and residual of N neighbouring columns.
+template <typename E, int N>
+__device__ __attribute__((always_inline)) inline void finish(const Gemm &o, long long row, int col,
+                                                             int count, float (&v)[N]) {
+    if (o.bias) {
+        float u[N];
+        load_upto<float, N>(o.bias + col, count, u);
+#pragma unroll
+        for (int r = 0; r < N; ++r)
+            v[r] += u[r];
+    }
+    if (o.pre)
+        store_upto<E, N>((E *)o.pre + row * o.sp + col, count, v);
+#pragma unroll
+    for (int r = 0; r < N; ++r)
+        v[r] = act_value(o.act, v[r]);
+    if (o.residual) {
+        float u[N];
+        load_upto<E, N>((const E *)o.residual + row * o.sr + col, count, u);
+#pragma unroll
+        for (int r = 0; r < N; ++r)
+            v[r] += u[r];
+    }
+}
+
 // One operand's tile: ROWS rows by BK positions of the sum, sixteen bytes a thread and
 // step.  ACROSS: BK rows of LDS of ROWS elements.
 template <typename E, int ROWS, int BK, bool ACROSS>
@@ -192,28 +217,337 @@ __global__ __launch_bounds__(kThreads) void gemm_kernel(Gemm o) {
                                      count, v);
                 continue;
             }
-            if (o.bias) {
-                float u[4];
-                load_upto<float, 4>(o.bias + col, count, u);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    v[r] += u[r];
-            }
-            if (o.pre)
-                store_upto<E, 4>((E *)o.pre + row * o.sp + col, count, v);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                v[r] = act_value(o.act, v[r]);
-            if (o.residual) {
-                float u[4];
-                load_upto<E, 4>((const E *)o.residual + row * o.sr + col, count, u);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    v[r] += u[r];
-            }
+            finish<E, 4>(o, row, col, count, v);
             store_upto<E, 4>((E *)o.c + row * o.sc + col, count, v);
         }
     }
+}
+
+// ---- the product of aligned operands -------------------------------------------------
+// Tiles go from memory to LDS without registers between, 16 bytes a lane, a few stages of
+// 32 positions ahead; fragments are read a stage ahead of their products.  The 16-byte
+// chunks of a stage's rows are exchanged by a function of the row so that the lanes of a
+// read, which take the same chunk of sixteen rows, find them in different banks.
+// Positions and rows past the ends come from sixteen zero bytes.
+
+constexpr int kStep = 32;   // positions of the sum of a stage
+
+__device__ const float kZeros[4] = {0, 0, 0, 0};
+
+// Waits until at most N of this wave's loads are under way, and for the other waves.
+template <int N>
+__device__ __attribute__((always_inline)) inline void arrive() {
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <typename E, int ROWS, int WAVES, bool ACROSS>
+struct Stage {
+    static constexpr int V = kPer16<E>, BK = kStep;
+    static constexpr int kLd = ACROSS ? ROWS : BK;                // elements of an LDS row
+    static constexpr int kChunks = kLd / V;                       // chunks of one
+    static constexpr int kBytes = ROWS * BK * (int)sizeof(E);
+    static constexpr int kLoads = kBytes / 1024 / WAVES;          // of a wave
+
+    // What a chunk's place is exchanged with in row `r`.  Reads of 16 bytes go by sixteen
+    // lanes: 0 to 3, 12 to 15 and 20 to 27, the others of the first half, and so on.
+    __device__ static int turn(int r) {
+        const int f = 0x78 >> 2 * (r >> 3 & 3) & 3;   // 0, 2, 3, 1
+        if constexpr (!ACROSS && sizeof(E) == 2)
+            return f;
+        else if constexpr (!ACROSS)
+            return (r >> 1 & 1) | f << 1;
+        else if constexpr (sizeof(E) == 2)   // units of two chunks
+            return ((r & 3) | (r >> 3 & 3) << 2) << 1 & (kChunks - 1);
+        else                                 // units of four
+            return (r >> 3 & 3) << 2;
+    }
+
+    const E *p[kLoads];   // this lane's places of the next stage
+    int at[kLoads];       // their positions of the sum
+    long long step;
+
+    // Rows past the operand's end are its last ones: what comes of them is not stored.
+    __device__ __attribute__((always_inline)) void start(const E *base, long long s, int row0,
+                                                         int rows, int k0, int wave, int lane) {
+        step = ACROSS ? BK * s : BK;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int chunk = (wave * kLoads + i) * 64 + lane;
+            const int r = chunk / kChunks;
+            const int c = (chunk % kChunks ^ turn(r)) * V;
+            if constexpr (ACROSS) {
+                at[i] = k0 + r;
+                p[i] = base + at[i] * s + min(row0 + c, rows - V);
+            } else {
+                at[i] = k0 + c;
+                p[i] = base + min(row0 + r, rows - 1) * s + at[i];
+            }
+        }
+    }
+    __device__ __attribute__((always_inline)) void load(char *lds, int k1, int wave) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const void *from = at[i] < k1 ? (const void *)p[i] : (const void *)kZeros;
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void *)from,
+                (__attribute__((address_space(3))) void *)(lds + (wave * kLoads + i) * 1024), 16, 0,
+                0);
+            p[i] += step;
+            at[i] += BK;
+        }
+    }
+    // Row (of the operand) of index i of tile t of a wave.  Along the sum two tiles take
+    // eight neighbouring rows in turns, so that a lane's results are eight neighbours.
+    __device__ static int row(int t, int i) {
+        return ACROSS ? 16 * t + i : 32 * (t / 2) + 8 * (i / 4) + 4 * (t % 2) + i % 4;
+    }
+    // Where a lane's part of tile 0 of the rows from row0 on lies in a stage.  row0 is a
+    // multiple of 32 (along) or of the rows of a wave, a power of two (across): what a tile
+    // adds to that, frag() gives the reads as an offset, or exchanges the place with.
+    __device__ static int place(int row0, int lane) {
+        const int g = lane >> 4, m = lane & 15;
+        int at;
+        if constexpr (!ACROSS) {
+            const int r = row0 + row(0, m);
+            at = r * kLd + ((sizeof(E) == 2 ? g : 2 * g) ^ turn(r)) * V;
+        } else {
+            const int r = 8 * g + (sizeof(E) == 2 ? m >> 2 : 0);
+            const int col = row0 + (sizeof(E) == 2 ? 4 * (m & 3) : m);
+            at = r * kLd + ((col / V) ^ turn(r)) * V + col % V;
+        }
+        return at * (int)sizeof(E);
+    }
+    __device__ __attribute__((always_inline)) static Frag<E> frag(const char *lds, int place,
+                                                                  int t) {
+        if constexpr (!ACROSS) {
+            const int more = (32 * (t / 2) + 4 * (t % 2)) * kLd * (int)sizeof(E);
+            if constexpr (sizeof(E) == 2)
+                return frag_row<E>((const E *)(lds + place + more));
+            else {
+                typedef float F4 __attribute__((ext_vector_type(4)));
+                const F4 a = *(const F4 *)(lds + place + more);
+                const F4 b = *(const F4 *)(lds + (place ^ 16) + more);
+                return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+        } else if constexpr (sizeof(E) == 2) {
+            const E *q = (const E *)(lds + (place ^ 16 * t * (int)sizeof(E)));
+            const s16x4 a = read_transposed(q), b = read_transposed(q + 4 * kLd);
+            return __builtin_bit_cast(Frag<E>,
+                                      __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const E *q = (const E *)(lds + (place ^ 16 * t * (int)sizeof(E)));
+            Frag<E> v;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                v[i] = q[i * kLd];
+            return v;
+        }
+    }
+};
+
+// Where a lane's results lie: `row0` and `col0` are its wave's first.
+template <typename SA, typename SB>
+struct Place {
+    int row0, col0, lane;
+    __device__ long long row(int i) const { return row0 + SA::row(i, lane & 15); }
+    __device__ int col(int j) const { return col0 + SB::row(j, 4 * (lane >> 4)); }
+};
+
+// From the sums to the outputs, a tile's rows after each other.  WHOLE: no column lies past
+// the end.  PLAIN: a gradient's, whose columns are whole chunks and which has no epilogue.
+// A wait for a load is one for the stores before it: the bias is there beforehand, and four
+// rows' residuals are asked for together.
+template <typename E, bool WHOLE, bool PLAIN, typename P, int TM, int TN>
+__device__ __attribute__((always_inline)) inline void emit(const Gemm &o, int part, const P &at,
+                                                           f32x4 (&acc)[TM][TN]) {
+    constexpr int N = PLAIN ? 4 : 8, J = TN * 4 / N;   // neighbouring columns, and their sets
+    constexpr int A = TM < 4 ? TM : 4;
+    typedef typename Vec<E, N>::type Some;
+    auto put = [&](auto *p, long long row, long long step, const float *v)
+                   __attribute__((always_inline)) {
+        typedef std::remove_reference_t<decltype(*p)> T;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int col = at.col(j * (N / 4));
+            if constexpr (WHOLE || PLAIN) {
+                if (WHOLE || col < o.N)
+                    store_vec<T, N>(p + row * step + col, v + j * N);
+            } else
+                store_upto<T, N>(p + row * step + col, o.N - col, v + j * N);
+        }
+    };
+    float bias[J * N] = {};
+    if (!PLAIN && o.bias && o.split == 1) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int col = at.col(j * (N / 4));
+            load_upto<float, N>(o.bias + col, WHOLE ? N : o.N - col, bias + j * N);
+        }
+    }
+#pragma unroll
+    for (int i0 = 0; i0 < TM; i0 += A) {
+        Some res[A][J];
+        if (!PLAIN && o.residual && o.split == 1) {
+#pragma unroll
+            for (int i = 0; i < A; ++i)
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const int col = at.col(j * (N / 4)), count = o.N - col;
+                    const long long row = min(at.row(i0 + i), (long long)o.M - 1);
+                    const E *p = (const E *)o.residual + row * o.sr + col;
+                    if constexpr (WHOLE)
+                        res[i][j] = *(const Some *)p;
+                    else if (count > 0)
+#pragma unroll
+                        for (int r = 0; r < N; ++r)
+                            res[i][j][r] = p[min(r, count - 1)];
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < A; ++i) {
+            const long long row = at.row(i0 + i);
+            if (row >= o.M)
+                continue;
+            float v[J * N];
+#pragma unroll
+            for (int r = 0; r < J * N; ++r)
+                v[r] = acc[i0 + i][r / 4][r % 4];
+            if (o.split > 1) {
+                put((float *)o.c + part * (long long)o.M * o.N, row, o.N, v);
+                continue;
+            }
+            if constexpr (!PLAIN) {
+#pragma unroll
+                for (int r = 0; r < J * N; ++r)
+                    v[r] += bias[r];
+                if (o.pre)
+                    put((E *)o.pre, row, o.sp, v);
+                auto apply = [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int r = 0; r < J * N; ++r)
+                        v[r] = act_value(decltype(act)::value, v[r]);
+                };
+                if (o.act == FINC_ACT_RELU)
+                    apply(std::integral_constant<int, FINC_ACT_RELU>());
+                else if (o.act == FINC_ACT_SILU)
+                    apply(std::integral_constant<int, FINC_ACT_SILU>());
+                else if (o.act == FINC_ACT_GELU)
+                    apply(std::integral_constant<int, FINC_ACT_GELU>());
+                if (o.residual)
+#pragma unroll
+                    for (int r = 0; r < J * N; ++r)
+                        v[r] += (float)res[i][r / N][r % N];
+            }
+            put((E *)o.c, row, o.sc, v);
+        }
+    }
+}
+
+template <typename E, int BM, int BN, int WM, int WN, int STAGES, bool AA, bool BA>
+__global__ __launch_bounds__(64 * WM * WN, sizeof(E) == 2 ? 2 : 1) void gemm_fast_kernel(Gemm o) {
+    typedef Stage<E, BM, WM * WN, AA> SA;
+    typedef Stage<E, BN, WM * WN, BA> SB;
+    constexpr int BK = kStep, TM = BM / WM / 16, TN = BN / WN / 16;
+    __shared__ __align__(1024) char lds[STAGES][SA::kBytes + SB::kBytes];
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    // Blocks go to the eight dies in turns: each die takes neighbouring tiles, in groups of
+    // eight rows of tiles that are walked column by column, so that its cache holds both.
+    int at = block_of();
+    const int tiles = o.tiles_m * o.tiles_n;
+    const int part = at / tiles;
+    if (part >= o.split)
+        return;
+    at -= part * tiles;
+    {
+        const int die = at & 7, each = tiles / 8, more = tiles & 7;
+        at = die * each + min(die, more) + (at >> 3);
+        const int band = 8 * o.tiles_n, first = at / band * 8, rows = min(8, o.tiles_m - first);
+        const int in = at - first * o.tiles_n;
+        at = (first + in % rows) * o.tiles_n + in / rows;
+    }
+    const int m0 = at / o.tiles_n * BM, n0 = at % o.tiles_n * BN;
+    const int k0 = part * o.per, k1 = min(k0 + o.per, o.K);
+    const int wm = w / WN * (BM / WM), wn = w % WN * (BN / WN);
+
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+            acc[i][j] = f32x4{0, 0, 0, 0};
+    SA a;
+    SB b;
+    a.start((const E *)o.a, o.sa, m0, o.M, k0, w, lane);
+    b.start((const E *)o.b, o.sb, n0, o.N, k0, w, lane);
+    const int steps = (k1 - k0 + BK - 1) / BK;
+    // Stage s + STAGES - 1 is asked for while the fragments of stage s + 1 are read and
+    // those of stage s multiplied.  Past the last one zeros are, so that the counts hold.
+    constexpr int kLoads = SA::kLoads + SB::kLoads;
+    int to = 0;
+    auto ask = [&]() __attribute__((always_inline)) {
+        a.load(lds[to], k1, w);
+        b.load(lds[to] + SA::kBytes, k1, w);
+        to = to + 1 == STAGES ? 0 : to + 1;
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+        ask();
+    // The first half of a stage's rows and its columns are read while the second half of
+    // the stage before is multiplied, the second half while the first one is.
+    constexpr int H = TM / 2;
+    Frag<E> fa[H], fc[H], fb[TN], fd[TN];
+    const int pa = SA::place(wm, lane), pb = SB::place(wn, lane);
+    int from = 0;
+    auto first = [&](Frag<E>(&rb)[TN]) __attribute__((always_inline)) {
+        const char *la = lds[from], *lb = la + SA::kBytes;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+            rb[j] = SB::frag(lb, pb, j);
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+            fa[i] = SA::frag(la, pa, i);
+    };
+    auto second = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+            fc[i] = SA::frag(lds[from], pa, H + i);
+        from = from + 1 == STAGES ? 0 : from + 1;
+    };
+    auto step = [&](Frag<E>(&now)[TN], Frag<E>(&next)[TN]) __attribute__((always_inline)) {
+        ask();
+        second();
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                acc[i][j] = mma(now[j], fa[i], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+        first(next);
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                acc[H + i][j] = mma(now[j], fc[i], acc[H + i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+        arrive<kLoads *(STAGES - 3)>();
+    };
+    arrive<kLoads *(STAGES - 2)>();
+    first(fb);
+    arrive<kLoads *(STAGES - 3)>();
+    for (int s = 0; s < steps; s += 2) {   // an odd one's last has zeros
+        step(fb, fd);
+        step(fd, fb);
+    }
+    // what is still on its way to LDS ends before the workgroup may
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+
+    const Place<SA, SB> at_lane = {m0 + wm, n0 + wn, lane};
+    if (n0 + BN <= o.N)
+        emit<E, true, BA>(o, part, at_lane, acc);
+    else
+        emit<E, false, BA>(o, part, at_lane, acc);
 }
 
 // The parts of split sums in order, and what follows them.
@@ -233,47 +567,36 @@ __global__ __launch_bounds__(kThreads) void split_sum_kernel(Gemm o, const float
         for (int r = 0; r < 4; ++r)
             v[r] += u[r];
     }
-    if (o.bias) {
-        float u[4];
-        load_upto<float, 4>(o.bias + col, count, u);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            v[r] += u[r];
-    }
-    if (o.pre)
-        store_upto<E, 4>((E *)o.pre + row * o.sp + col, count, v);
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-        v[r] = act_value(o.act, v[r]);
-    if (o.residual) {
-        float u[4];
-        load_upto<E, 4>((const E *)o.residual + row * o.sr + col, count, u);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            v[r] += u[r];
-    }
+    finish<E, 4>(o, row, col, count, v);
     store_upto<E, 4>(c + row * o.sc + col, count, v);
 }
 
 // ---- d = dy act'(pre), and the sums of its columns -----------------------------------
 
-constexpr int kSumRows = 128;   // rows of a workgroup: 8 side by side of 32 lanes of 8 columns
+// Rows of a workgroup, 8 side by side of 32 lanes of 8 columns: as many as leave two
+// workgroups a compute unit (gelu' of 1531 x 1000 in fp32: 45 us with 128 rows, 14 with 16).
+int sum_rows(int M, int N) {
+    int rows = 128;
+    while (rows > 16 && cdivll(M, rows) * cdivll(N, 256) < 512)
+        rows /= 2;
+    return rows;
+}
 
 template <typename E>
 __global__ __launch_bounds__(kThreads) void act_grad_kernel(const E *dy, long long sdy,
                                                             const E *pre, long long spre, E *d,
                                                             float *sums, int act, int M, int N,
-                                                            int slices) {
+                                                            int slices, int rows) {
     __shared__ float part[8][32 * 8 + 8];
     const int at = block_of(), block = at / slices, slice = at - block * slices;
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int col = slice * 256 + lane * 8, count = min(N - col, 8);
-    const long long first = (long long)block * kSumRows;
+    const long long first = (long long)block * rows;
     if (first >= M)
         return;
     float sum[8] = {};
 #pragma unroll 4
-    for (int i = 0; i < kSumRows / 8; ++i) {
+    for (int i = 0; i < rows / 8; ++i) {
         const long long row = first + i * 8 + w;
         const int have = row < M ? count : 0;
         float v[8];
@@ -307,20 +630,25 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(const E *dy, long lo
     }
 }
 
-// The blocks' sums in order: 4 shares a column, joined in order.
-__global__ __launch_bounds__(kThreads) void column_sum_kernel(const float *sums, float *out, int N,
-                                                              int blocks) {
-    __shared__ float part[4][64];
+// The blocks' sums in order: sixteen shares a column, joined in order.
+__global__ __launch_bounds__(1024) void column_sum_kernel(const float *sums, float *out, int N,
+                                                          int blocks) {
+    __shared__ float part[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
-    const int share = (blocks + 3) / 4, lo = min(w * share, blocks), hi = min(lo + share, blocks);
+    const int share = (blocks + 15) / 16, lo = min(w * share, blocks), hi = min(lo + share, blocks);
     float s = 0.0f;
-    if (c < N)
+    if (c < N) {
+#pragma unroll 8
         for (int i = lo; i < hi; ++i)
             s += sums[(long long)i * N + c];
+    }
     part[w][lane] = s;
     __syncthreads();
-    if (w == 0 && c < N)
-        out[c] = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+    if (w == 0 && c < N) {
+        for (int i = 1; i < 16; ++i)
+            s += part[i][lane];
+        out[c] = s;
+    }
 }
 
 // ---- the host --------------------------------------------------------------------------
@@ -337,43 +665,108 @@ bool linear_shape(int type, int act, int M, int K, int N) {
            (long long)K * N < (1ll << 40);
 }
 
-// Tile and split of a product.
-struct Plan {
-    int tile, split, per;
-};
-Plan plan(int M, int N, int K) {
-    Plan p;
-    p.tile = cdivll(M, 128) * cdivll(N, 128) >= 256 ? 128 : 64;
-    const long long tiles = cdivll(M, p.tile) * cdivll(N, p.tile);
-    p.split = 1;
-    while (p.split < 16 && tiles * p.split < 256 && K / (p.split * 2) >= 256)
-        p.split *= 2;
-    p.per = (int)(cdivll(cdivll(K > 0 ? K : 1, p.split), 64) * 64);
-    p.split = (int)cdivll(K > 0 ? K : 1, p.per);   // an empty sum is one of zeros
-    return p;
+// Chunks of 16 bytes that lie whole within a row and start at multiples of 16 bytes.
+bool whole(const void *p, long long s, int n, int size) {
+    return (uintptr_t)p % 16 == 0 && s * size % 16 == 0 && (long long)n * size % 16 == 0;
 }
-size_t split_bytes(int M, int N, int K) {
-    const Plan p = plan(M, N, K);
-    return p.split > 1 ? round256((size_t)p.split * M * N * 4) : 0;
+
+// Square tiles of the kernels, and microseconds that 32 positions of the sum take: of a
+// tile alone on a compute unit (along the sum, and with an operand across it, whose rows
+// come from more places), and of each of `side` tiles side by side there.
+struct Tile {
+    int dim, side;
+    double alone, across, each;
+};
+// 16 bits: 2048 x 1024 x 1024 forward takes 11 us with tiles of 64 and 14 with 128; 4096 x
+// 2048 x 2048 takes 75, 42 and 50 with 64, 128 and 256; 32768 x 1024 x 4096 257 with 256.
+const Tile kFast16[] = {{64, 4, 0.13, 0.45, 0.13}, {128, 2, 0.30, 0.58, 0.30},
+                        {256, 1, 0.87, 0.97, 0.87}};
+// 32: 8192 x 2048 x 2048 632 with 64, 557 with 128; 1536 x 336 x 1000 19 and 31.
+const Tile kFast32[] = {{64, 4, 0.65, 0.65, 0.58}, {128, 1, 2.2, 2.2, 2.2}};
+// Operands of other alignments: 8191 x 1001 x 1003 58 and 46 in 16 bits, 177 and 159 in 32.
+const Tile kAny16[] = {{64, 4, 0.55, 0.55, 0.22}, {128, 2, 1.1, 1.1, 0.68}};
+const Tile kAny32[] = {{64, 4, 1.55, 1.55, 0.69}, {128, 2, 4.0, 4.0, 2.4}};
+
+// Tile and split of a product: the cheapest of all by that and by what a launch, a tile's
+// end and the parts of split sums cost (6 us and their way to memory and back at 4 TB/s).
+// The gradient of 2048 x 2048 weights over 16384 rows: 155 us in four parts with tiles of
+// 256, 173 in two with 128, 244 in one with 64; of 64 x 256 over 32768: 456 in one part,
+// 38 in sixteen.
+struct Plan {
+    int dim, split, per;
+    bool fast;
+};
+Plan plan(int M, int N, int K, int size, bool fast, bool across) {
+    const Tile *from = fast ? (size == 2 ? kFast16 : kFast32) : (size == 2 ? kAny16 : kAny32);
+    const int kinds = fast && size == 2 ? 3 : 2, sum = K > 0 ? K : 1;   // none: zeros
+    Plan best = {};
+    best.fast = fast;
+    double least = 0.0;
+    for (int k = 0; k < kinds; ++k) {
+        const Tile &t = from[k];
+        const double tiles = (double)cdivll(M, t.dim) * cdivll(N, t.dim);
+        for (int split = 1; split <= 64; split *= 2) {
+            if (split > 1 && sum / split < 128)
+                break;
+            const int per = (int)(cdivll(cdivll(sum, split), 64) * 64);
+            const int parts = (int)cdivll(sum, per);
+            const double n = ceil(tiles * parts / 256.0), side = n < t.side ? n : t.side;
+            const double step = (across ? t.across : t.alone) > side * t.each
+                                    ? (across ? t.across : t.alone)
+                                    : side * t.each;
+            double us = ceil(n / t.side) * (per / 32.0) * step + n * t.dim * t.dim / 16384.0;
+            if (parts > 1)
+                us += 6.0 + parts * (double)M * N * 8.0 / 4e6;
+            if (best.dim == 0 || us < least) {
+                least = us;
+                best.dim = t.dim;
+                best.split = parts;
+                best.per = per;
+            }
+        }
+    }
+    return best;
+}
+// For operands of any alignment.
+size_t split_bytes(int M, int N, int K, int size, bool across) {
+    const int a = plan(M, N, K, size, true, across).split,
+              b = plan(M, N, K, size, false, across).split, most = a > b ? a : b;
+    return most > 1 ? round256((size_t)most * M * N * 4) : 0;
+}
+
+template <typename E, bool AA, bool BA>
+void launch_gemm(const Plan &p, const Gemm &o, dim3 grid, hipStream_t stream) {
+    if constexpr (sizeof(E) == 2)
+        if (p.fast && p.dim == 256) {
+            gemm_fast_kernel<E, 256, 256, 2, 4, 4, AA, BA><<<grid, 512, 0, stream>>>(o);
+            return;
+        }
+    if (p.fast && p.dim == 128)
+        gemm_fast_kernel<E, 128, 128, 2, 2, 4, AA, BA><<<grid, 256, 0, stream>>>(o);
+    else if (p.fast)
+        gemm_fast_kernel<E, 64, 64, 2, 2, 4, AA, BA><<<grid, 256, 0, stream>>>(o);
+    else if (p.dim == 128)
+        gemm_kernel<E, 128, 128, AA, BA><<<grid, kThreads, 0, stream>>>(o);
+    else
+        gemm_kernel<E, 64, 64, AA, BA><<<grid, kThreads, 0, stream>>>(o);
 }
 
 template <bool AA, bool BA>
 void run_gemm(int type, Gemm o, void *workspace, hipStream_t stream) {
-    const Plan p = plan(o.M, o.N, o.K);
+    const int sz = type_size(type);
+    const bool fast = whole(o.a, o.sa, AA ? o.M : o.K, sz) && whole(o.b, o.sb, BA ? o.N : o.K, sz);
+    const Plan p = plan(o.M, o.N, o.K, sz, fast, BA);
     o.split = p.split;
     o.per = p.per;
-    o.tiles_m = (int)cdivll(o.M, p.tile);
-    o.tiles_n = (int)cdivll(o.N, p.tile);
+    o.tiles_m = (int)cdivll(o.M, p.dim);
+    o.tiles_n = (int)cdivll(o.N, p.dim);
     void *c = o.c;
     if (p.split > 1)
         o.c = workspace;
     const dim3 grid = grid_of((long long)o.tiles_m * o.tiles_n * p.split);
     with_type(type, [&](auto e) {
         typedef decltype(e) E;
-        if (p.tile == 128)
-            gemm_kernel<E, 128, 128, AA, BA><<<grid, kThreads, 0, stream>>>(o);
-        else
-            gemm_kernel<E, 64, 64, AA, BA><<<grid, kThreads, 0, stream>>>(o);
+        launch_gemm<E, AA, BA>(p, o, grid, stream);
         if (p.split > 1) {
             const int vecs = (o.N + 3) / 4;
             split_sum_kernel<E><<<grid_of(cdivll((long long)o.M * vecs, kThreads)), kThreads, 0,
@@ -382,14 +775,15 @@ void run_gemm(int type, Gemm o, void *workspace, hipStream_t stream) {
     });
 }
 
-int sum_blocks(int M) { return (int)cdivll(M, kSumRows); }
+int sum_blocks(int M, int N) { return (int)cdivll(M, sum_rows(M, N)); }
 
 }  // namespace
 
 extern "C" {
 
 size_t finc_linear_workspace_bytes(int type, int M, int K, int N) {
-    return linear_shape(type, FINC_ACT_NONE, M, K, N) ? split_bytes(M, N, K) : 0;
+    return linear_shape(type, FINC_ACT_NONE, M, K, N) ? split_bytes(M, N, K, type_size(type), false)
+                                                       : 0;
 }
 
 int finc_linear_forward(const finc_linear_args *a, hipStream_t stream) {
@@ -439,9 +833,10 @@ int finc_linear_forward(const finc_linear_args *a, hipStream_t stream) {
 size_t finc_linear_grad_workspace_bytes(int type, int act, int M, int K, int N) {
     if (!linear_shape(type, act, M, K, N))
         return 0;
-    const size_t x = split_bytes(M, K, N), w = split_bytes(N, K, M);
-    return (act != FINC_ACT_NONE ? round256((size_t)M * N * type_size(type)) : 0) +
-           round256((size_t)sum_blocks(M) * N * 4) + (x > w ? x : w);
+    const int sz = type_size(type);
+    const size_t x = split_bytes(M, K, N, sz, true), w = split_bytes(N, K, M, sz, true);
+    return (act != FINC_ACT_NONE ? round256((size_t)M * N * sz) : 0) +
+           round256((size_t)sum_blocks(M, N) * N * 4) + (x > w ? x : w);
 }
 
 int finc_linear_backward(const finc_linear_grad_args *a, hipStream_t stream) {
@@ -471,17 +866,17 @@ int finc_linear_backward(const finc_linear_grad_args *a, hipStream_t stream) {
         return p;
     };
     void *d = act ? take((size_t)M * N * sz) : nullptr;
-    float *sums = (float *)take((size_t)sum_blocks(M) * N * 4);
-    const int blocks = sum_blocks(M), slices = (N + 255) / 256;
+    float *sums = (float *)take((size_t)sum_blocks(M, N) * N * 4);
+    const int blocks = sum_blocks(M, N), slices = (N + 255) / 256;
     if (M > 0 && (act || a->dbias))
         with_type(a->type, [&](auto e) {
             typedef decltype(e) E;
             act_grad_kernel<E><<<grid_of((long long)blocks * slices), kThreads, 0, stream>>>(
                 (const E *)a->dy, a->sdy, (const E *)a->pre, a->spre, (E *)d,
-                a->dbias ? sums : nullptr, a->act, M, N, slices);
+                a->dbias ? sums : nullptr, a->act, M, N, slices, sum_rows(M, N));
         });
     if (a->dbias)
-        column_sum_kernel<<<(N + 63) / 64, kThreads, 0, stream>>>(sums, a->dbias, N, blocks);
+        column_sum_kernel<<<(N + 63) / 64, 1024, 0, stream>>>(sums, a->dbias, N, blocks);
     Gemm o = {};
     o.a = act ? d : a->dy;
     o.sa = act ? N : a->sdy;
