@@ -25,9 +25,8 @@ namespace {
 using namespace finc_seq;
 
 constexpr int kBlock = 64;                       // positions of a block
-constexpr int kPart = FINC_ATTENTION_PART;       // positions of a workgroup
+constexpr int kPart = FINC_ATTENTION_PART;       // most positions of a workgroup
 constexpr int kBlocks = kPart / kBlock;
-constexpr int kThreads = 256;
 constexpr float kLeast = -128.0f;                // log decays below count as this
 
 struct Tensor {
@@ -51,6 +50,7 @@ struct Role {
     int sd, sn;             // steps of a state's rows and columns
     float pscale, sscale, kscale;
     bool rev, out_f32;
+    bool exact;             // the state may leave the call: its sums in full
 };
 
 struct Args {
@@ -60,7 +60,7 @@ struct Args {
     const int *lengths;
     float *local, *decays;   // states of the parts alone: (B H, parts + 1, da dn), (B H, parts)
     FastDiv by_bh, by_parts, by_h;
-    int L, H, BH, parts;
+    int L, H, BH, parts, part;   // positions of a part
 };
 
 template <typename E>
@@ -68,88 +68,215 @@ __device__ inline const E *head_rows(const Tensor &t, int b, int h) {
     return (const E *)t.p + b * t.sb + (t.div == 1 ? h : h / t.div) * t.sh;
 }
 
-// ---- tiles on their way to LDS ---------------------------------------------------
+// ---- tiles in LDS --------------------------------------------------------------------
+// 64 rows of D elements.  In 16 bits the 16-byte chunks of a row are exchanged by a
+// function of the row, so that none of the reads below finds two of the lanes that go
+// together in one bank: sixteen bytes of sixteen rows (sixteen lanes at a time: 0 to 3, 12
+// to 15 and 20 to 27, the others of the first half, and so on), eight bytes of sixteen rows
+// (32 lanes), and the transposed reads (32 lanes).
 
-// 64 rows of up to D elements, sixteen bytes a thread and step.
 template <typename E, int D>
-struct Tile {
-    static constexpr int V = kPer16<E>, kRow = D / V, kRows = kThreads / kRow;
-    static constexpr int kSteps = kBlock / kRows, kLd = D + V;
-    typedef typename Vec<E, V>::type Some;
-    Some r[kSteps];
-
-    __device__ void load(const E *p, long long st, int rows, int dim) {
-        const int col = (int)threadIdx.x % kRow * V, row = (int)threadIdx.x / kRow;
+struct Rows {
+    static constexpr int kLd = sizeof(E) == 2 ? D : D + 4;
+    static constexpr int kSize = kBlock * kLd;
+    __device__ static int turn(int r) {
+        if constexpr (D == 128)
+            return (r & 3) << 2 | (0x78 >> 2 * (r >> 2 & 3) & 3);
+        else
+            return (r & 2) | ((r >> 2 ^ r >> 3) & 1) << 2 | (r >> 3 & 1);
+    }
+    __device__ static int at(int r, int col) {
+        if constexpr (sizeof(E) == 2)
+            return r * kLd + ((col / 8 ^ turn(r)) * 8 | col % 8);
+        else
+            return r * kLd + col;
+    }
+    // A lane's places in the first rows and columns; those further on follow from them by
+    // an exchange (a sum in 32 bits) that is formed where it is used: kept, they would take
+    // some forty registers.
+    struct Lane {
+        int row, half, column, below;
+    };
+    __device__ static Lane lane(int l) {
+        const int g = l >> 4, m = l & 15;
+        const int r = sizeof(E) == 2 ? 8 * g + (m >> 2) : 8 * g;
+        const int c = sizeof(E) == 2 ? 4 * (m & 3) : m;
+        return {at(m, 8 * g), at(m, 4 * g), at(r, c), at(r + 4, c)};
+    }
+    __device__ static int there(int place, int r, int col) {   // multiples of 16
+        return (sizeof(E) == 2 ? place ^ col : place + col) + r * kLd;
+    }
+    // Elements 8 g .. 8 g + 7 of the 32 from `col` on, of row r + m.
+    __device__ static Frag<E> row(const E *s, const Lane &l, int r, int col) {
+        return frag_row<E>(s + there(l.row, r, col));
+    }
+    // Elements 4 g .. 4 g + 3 of the 16 from `col` on and of the 16 behind them.
+    __device__ static Frag<E> halves(const E *s, const Lane &l, int r, int col) {
+        typedef E Four __attribute__((ext_vector_type(4)));
+        const Four a = *(const Four *)(s + there(l.half, r, col));
+        const Four b = *(const Four *)(s + there(l.half, r, col + 16));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    // Rows 8 g .. 8 g + 7 of the 32 from `r` on, of column col + m.
+    __device__ static Frag<E> column(const E *s, const Lane &l, int r, int col) {
+        if constexpr (sizeof(E) == 2) {
+            const s16x4 a = read_transposed(s + there(l.column, r, col));
+            const s16x4 b = read_transposed(s + there(l.below, r, col));
+            return __builtin_bit_cast(Frag<E>,
+                                      __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            Frag<E> v;
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const int at = row + i * kRows;
-            Some v = {};
-            if (at < rows && col < dim) {
-                const E *q = p + at * st + col;
-                if (col + V <= dim)
-                    v = *(const Some *)q;
-                else
-                    for (int j = 0; j < V; ++j)
-                        if (col + j < dim)
-                            v[j] = q[j];
-            }
-            r[i] = v;
+            for (int i = 0; i < 8; ++i)
+                v[i] = s[there(l.column, r + i, col)];
+            return v;
         }
     }
-    __device__ void store(E *s) const {
-        typedef E Whole __attribute__((ext_vector_type(V), aligned(16)));
+};
+
+// A tile on its way there, sixteen bytes a thread and step.  The loads have no branches,
+// which would wait for each: rows past the end are the last one, and the chunk that passes
+// a row's end is the row's last sixteen bytes.  What that adds goes on the way to LDS.
+template <typename E, int D, int THREADS>
+struct Tile {
+    static constexpr int V = kPer16<E>, kRow = D / V, kRows = THREADS / kRow;
+    static constexpr int kSteps = kBlock / kRows;
+    typedef typename Vec<E, V>::type Some;
+    typedef E Whole __attribute__((ext_vector_type(V), aligned(16)));
+    Some r[kSteps];
+
+    // Rows of D elements whose steps stay within 31 bits of bytes over a tile.
+    __device__ __attribute__((always_inline)) void load_whole(const E *p, int st, int rows) {
         const int col = (int)threadIdx.x % kRow * V, row = (int)threadIdx.x / kRow;
+        const char *q = (const char *)p;
+        if (rows >= kBlock) {
+            const unsigned at = (row * st + col) * (unsigned)sizeof(E);
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i)
-            *(Whole *)(s + (row + i * kRows) * kLd + col) = r[i];
+            for (int i = 0; i < kSteps; ++i)
+                r[i] = *(const Some *)(q + (long long)(i * kRows) * st * (int)sizeof(E) + at);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+                r[i] = *(const Some *)(q + (unsigned)((min(row + i * kRows, rows - 1) * st + col) *
+                                                      (int)sizeof(E)));
+        }
+    }
+    __device__ __attribute__((always_inline)) void load(const E *p, long long st, int rows,
+                                                        int dim) {
+        const int col = (int)threadIdx.x % kRow * V, row = (int)threadIdx.x / kRow;
+        if (dim >= V) {
+            const E *q = p + min(col, dim - V);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+                r[i] = *(const Some *)(q + min(row + i * kRows, rows - 1) * st);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    r[i][j] = p[min(row + i * kRows, rows - 1) * st + min(j, dim - 1)];
+        }
+    }
+    template <bool WHOLE>
+    __device__ __attribute__((always_inline)) void store(E *s, int rows, int dim) const {
+        const int col = (int)threadIdx.x % kRow * V, row = (int)threadIdx.x / kRow;
+        // sixteen rows on, the chunks lie as they do here
+        static_assert(sizeof(E) == 4 || kRows % 16 == 0, "one place a thread");
+        E *to = s + Rows<E, D>::at(row, col);
+        constexpr int kOn = kRows * Rows<E, D>::kLd;
+        if constexpr (WHOLE) {
+            if (rows >= kBlock) {
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i)
+                    *(Whole *)(to + i * kOn) = r[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i)
+                    *(Whole *)(to + i * kOn) = row + i * kRows < rows ? (Whole)r[i] : (Whole){};
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            typedef unsigned __int128 Bits;
+            constexpr int kBits = 8 * (int)sizeof(E);
+            Bits v = __builtin_bit_cast(Bits, (Whole)r[i]);
+            if (dim % V != 0 && col + V > dim) {
+                // where the load went back by as many elements, and the rest
+                const int have = max(dim - col, 0);
+                v = dim >= V ? v >> (kBits * min(V - have, V - 1)) : v;
+                v = have > 0 ? v & (~(Bits)0 >> (kBits * (V - have))) : 0;
+            }
+            v = row + i * kRows < rows && col < dim ? v : 0;
+            *(Whole *)(to + i * kOn) = __builtin_bit_cast(Whole, v);
+        }
     }
 };
 
 // The weights of 64 queries and keys.
 template <typename E>
 struct Scores {
-    static constexpr int kLd = kBlock + 8;
-    bf16 hi[kBlock * kLd], lo[kBlock * kLd];
-    __device__ void set(int row, int col, f32x4 v) {
+    typedef Rows<bf16, kBlock> R;
+    bf16 hi[R::kSize], lo[R::kSize];
+    // rows and columns from multiples of 16 on: four columns of row m
+    __device__ void set(const typename R::Lane &l, int row, int col, f32x4 v) {
         bf16x4 a, b;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             a[r] = (bf16)v[r];
             b[r] = (bf16)(v[r] - (float)a[r]);
         }
-        *(bf16x4 *)(hi + row * kLd + col) = a;
-        *(bf16x4 *)(lo + row * kLd + col) = b;
+        *(bf16x4 *)(hi + R::there(l.half, row, col)) = a;
+        *(bf16x4 *)(lo + R::there(l.half, row, col)) = b;
     }
-    __device__ Parts get(int row, int col) const {
-        return {frag_row<bf16>(hi + row * kLd + col), frag_row<bf16>(lo + row * kLd + col)};
+    __device__ Parts get(const typename R::Lane &l, int row, int col) const {
+        return {R::row(hi, l, row, col), R::row(lo, l, row, col)};
     }
 };
 template <>
 struct Scores<float> {
-    static constexpr int kLd = kBlock + 4;
-    float v[kBlock * kLd];
-    __device__ void set(int row, int col, f32x4 x) { *(f32x4 *)(v + row * kLd + col) = x; }
-    __device__ f32x8 get(int row, int col) const { return frag_row<float>(v + row * kLd + col); }
+    typedef Rows<float, kBlock> R;
+    float v[R::kSize];
+    __device__ void set(const R::Lane &l, int row, int col, f32x4 x) {
+        *(f32x4 *)(v + R::there(l.half, row, col)) = x;
+    }
+    __device__ f32x8 get(const R::Lane &l, int row, int col) const {
+        return R::row(v, l, row, col);
+    }
 };
-
-struct Nothing {};
+struct Nothing {
+    typedef Rows<float, kBlock> R;
+};
 
 // ---- the kernel ------------------------------------------------------------------
 
 // STATES: the parts' own sums of k v^T alone, and their decays.
-template <typename E, int D, bool STATES>
-__global__ __launch_bounds__(kThreads, sizeof(E) == 2 ? 2 : 1) void attention_kernel(Args a) {
+// A wave has 16 NC columns of v and of the state.  WHOLE: heads of D elements, steps of
+// rows below 2^23 and outputs of the type; the code for all else next to it would take its
+// registers.
+constexpr int threads_of(int D, int NC) { return 4 * D / NC; }
+// Tiles of columns of a wave: with two, what a wave reads of q and k serves twice as much
+// (one long bf16 prompt 139 us, 161 with one).  fp16 inputs are two parts each, for which
+// two tiles leave no registers (the ragged prompts 108 us, 119).
+template <typename E>
+constexpr int columns_of(int D) {
+    return std::is_same_v<E, f16> ? 1 : D / 64;
+}
+template <typename E, int D, int NC, bool STATES, bool WHOLE>
+__global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
+    void attention_kernel(Args a) {
     typedef Mixed<E> M;
-    typedef Tile<E, D> T;
-    constexpr int LD = T::kLd, NC = D / 64;   // column tiles of a wave
-    __shared__ __align__(16) E sk[kBlock * LD];
-    __shared__ __align__(16) E sv[kBlock * LD];
-    __shared__ __align__(16) E sq[STATES ? 8 : kBlock * LD];
-    __shared__ __align__(16) std::conditional_t<STATES, Nothing, Scores<E>> sp;
-    __shared__ __align__(16) float wk[kPart];
-    __shared__ float ghi[kPart], glo[kPart], wq[kPart];
+    typedef Rows<E, D> R;
+    constexpr int WAVES = D / 16 / NC;
+    typedef Tile<E, D, 64 * WAVES> T;
+    __shared__ __align__(16) E sk[R::kSize];
+    __shared__ __align__(16) E sv[R::kSize];
+    __shared__ __align__(16) E sq[STATES ? 8 : R::kSize];
+    typedef std::conditional_t<STATES, Nothing, Scores<E>> P;
+    __shared__ __align__(16) P sp;
+    __shared__ __align__(16) float wk[kPart], ghi[kPart], glo[kPart], wq[kPart];
     __shared__ double total[kBlocks];
-    __shared__ float sdot[4][kBlock];
+    __shared__ float sdot[WAVES][kBlock];
 
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -165,15 +292,71 @@ __global__ __launch_bounds__(kThreads, sizeof(E) == 2 ? 2 : 1) void attention_ke
         return;
     const bool rev = o.rev;
 
-    const int t0 = part * kPart;
+    const int t0 = part * a.part;
     const int end = a.lengths ? min(max(a.lengths[b], 0), a.L) : a.L;
-    const int have = min(max(end - t0, 0), kPart);             // valid positions
+    const int have = min(max(end - t0, 0), a.part);            // valid positions
     const int blocks = (have + kBlock - 1) / kBlock;
+
+    // Loads first, each behind the other: the first tiles, the state, the decays.
+    // A state that leaves the call as fp32 takes its sums in full; for the outputs of 16
+    // bits the two parts of its weights do.
+    const bool exact = STATES || o.exact;
+    const E *kp = head_rows<E>(o.k, b, h), *vp = head_rows<E>(o.v, b, h);
+    const E *qp = STATES ? nullptr : head_rows<E>(o.q, b, h);
+    T tk, tv, tq;
+    auto fetch = [&](int c) __attribute__((always_inline)) {
+        const long long t = t0 + c * kBlock;
+        const int rows = have - c * kBlock;
+        if constexpr (WHOLE) {
+            tk.load_whole(kp + t * o.k.st, (int)o.k.st, rows);
+            tv.load_whole(vp + t * o.v.st, (int)o.v.st, rows);
+            if constexpr (!STATES)
+                tq.load_whole(qp + t * o.q.st, (int)o.q.st, rows);
+        } else {
+            tk.load(kp + t * o.k.st, o.k.st, rows, o.da);
+            tv.load(vp + t * o.v.st, o.v.st, rows, o.dn);
+            if constexpr (!STATES)
+                tq.load(qp + t * o.q.st, o.q.st, rows, o.da);
+        }
+    };
+    if (blocks > 0)
+        fetch(rev ? blocks - 1 : 0);
+
+    // ---- the state ---------------------------------------------------------------
+    // Element r of tile t is row 16 t + 4 g + r of column n: two tiles are the eight
+    // elements that halves() gives of a query.
+    const int n0 = 16 * NC * w;
+    f32x4 S[D / 16][NC];
+    const long long size = (long long)o.da * o.dn;
+    const float *init =
+        !STATES && o.init ? o.init + bh * o.init_bh + part * o.init_p : nullptr;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            S[t][c] = f32x4{0, 0, 0, 0};
+    if (init) {
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if constexpr (WHOLE)
+                        S[t][c][r] = init[(16 * t + r) * o.sd + 16 * c * o.sn +
+                                          (unsigned)(4 * g * o.sd + (n0 + m) * o.sn)];
+                    else
+                        S[t][c][r] = init[min(16 * t + 4 * g + r, o.da - 1) * o.sd +
+                                          min(n0 + 16 * c + m, o.dn - 1) * o.sn];
+    }
+    if (!STATES && o.keep)
+        for (int i = threadIdx.x; i < size; i += 64 * WAVES)
+            o.keep[bh * 2 * size + i] = init ? init[i] : 0.0f;
 
     // ---- the decays of the whole part: a wave a block ---------------------------
     const float base = a.decay ? a.decay[h] : 0.0f;
     const E *gp = a.g.p ? head_rows<E>(a.g, b, h) : nullptr;
-    for (int c = w; c < blocks; c += 4) {
+    for (int c = w; c < blocks; c += WAVES) {
         const int t = c * kBlock + lane;
         float v = 0.0f;
         if (t < have) {
@@ -199,118 +382,108 @@ __global__ __launch_bounds__(kThreads, sizeof(E) == 2 ? 2 : 1) void attention_ke
             total[c] = all;
     }
 
-    // ---- the state ---------------------------------------------------------------
-    // Row 4 g + r of tile t is row d = 32 (t / 2) + 8 g + 4 (t % 2) + r, so that a lane's
-    // values of two tiles are a fragment's eight neighbours.
-    f32x4 S[D / 16][NC];
-    const long long size = (long long)o.da * o.dn;
-    const float *init =
-        !STATES && o.init ? o.init + bh * o.init_bh + part * o.init_p : nullptr;
+    if (!WHOLE && init) {
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t)
+        for (int t = 0; t < D / 16; ++t)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            S[t][c] = f32x4{0, 0, 0, 0};
-            if (init) {
+            for (int c = 0; c < NC; ++c)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int d = 32 * (t / 2) + 8 * g + 4 * (t % 2) + r;
-                    const int n = 16 * (w * NC + c) + m;
-                    const float v = init[min(d, o.da - 1) * o.sd + min(n, o.dn - 1) * o.sn];
-                    S[t][c][r] = d < o.da && n < o.dn ? v : 0.0f;
-                }
-            }
-        }
-    if (!STATES && o.keep)
-        for (int i = threadIdx.x; i < size; i += kThreads)
-            o.keep[bh * 2 * size + i] = init ? init[i] : 0.0f;
+                for (int r = 0; r < 4; ++r)
+                    S[t][c][r] =
+                        16 * t + 4 * g + r < o.da && n0 + 16 * c + m < o.dn ? S[t][c][r] : 0.0f;
+    }
 
     // the tiles of scores that the products read but no block writes
     if constexpr (!STATES) {
         if (w < 2) {
             const int q = rev ? 2 * w + 1 : 2 * w, k = rev ? 2 * w : 2 * w + 1;
-            sp.set(16 * q + m, 16 * k + 4 * g, f32x4{0, 0, 0, 0});
+            sp.set(P::R::lane(lane), 16 * q, 16 * k, f32x4{0, 0, 0, 0});
         }
     }
 
-    const E *kp = head_rows<E>(o.k, b, h), *vp = head_rows<E>(o.v, b, h);
-    const E *qp = STATES ? nullptr : head_rows<E>(o.q, b, h);
-    T tk, tv, tq;
-    auto fetch = [&](int c) __attribute__((always_inline)) {
-        const long long t = t0 + c * kBlock;
-        const int rows = have - c * kBlock;
-        tk.load(kp + t * o.k.st, o.k.st, rows, o.da);
-        tv.load(vp + t * o.v.st, o.v.st, rows, o.dn);
-        if constexpr (!STATES)
-            tq.load(qp + t * o.q.st, o.q.st, rows, o.da);
-    };
-    if (blocks > 0)
-        fetch(rev ? blocks - 1 : 0);
-
+    const typename R::Lane first = R::lane(lane);
+    const typename P::R::Lane first_p = P::R::lane(lane);
     for (int i = 0; i < blocks; ++i) {
         const int c = rev ? blocks - 1 - i : i;
-        tk.store(sk);
-        tv.store(sv);
+        const typename R::Lane l = {afresh(first.row), afresh(first.half), afresh(first.column),
+                                    afresh(first.below)};
+        const typename P::R::Lane lp = {afresh(first_p.row), afresh(first_p.half), 0, 0};
+        tk.template store<WHOLE>(sk, have - c * kBlock, o.da);
+        tv.template store<WHOLE>(sv, have - c * kBlock, o.dn);
         if constexpr (!STATES)
-            tq.store(sq);
+            tq.template store<WHOLE>(sq, have - c * kBlock, o.da);
         __syncthreads();
+        // asked for ahead of the next block's tiles, behind which a wait would be one for them
+        typedef typename Vec<E, 4>::type Four;
+        Four dot[4][NC];
+        if (!STATES && o.dots) {
+            const E *p = head_rows<E>(o.dot, b, h) + (t0 + c * kBlock) * o.dot.st;
+            const int rows = have - c * kBlock;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int e = 0; e < NC; ++e) {
+                    const int row = min(16 * q + m, rows - 1), col = n0 + 16 * e + 4 * g;
+                    if constexpr (WHOLE)
+                        dot[q][e] = *(const Four *)((const char *)p + (unsigned)((row * (int)o.dot.st + col) * (int)sizeof(E)));
+                    else if (o.dn % 4 == 0)
+                        dot[q][e] = *(const Four *)(p + row * o.dot.st + min(col, o.dn - 4));
+                    else
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            dot[q][e][r] = p[row * o.dot.st + min(col + r, o.dn - 1)];
+                }
+        }
         if (i + 1 < blocks)
             fetch(rev ? c - 1 : c + 1);
 
-        // this wave's columns of v
-        auto values = [&](int j, int n) __attribute__((always_inline)) {
-            return frag_column<4>(sv + 32 * j * LD + 16 * (w * NC + n), LD, lane);
-        };
         if constexpr (!STATES) {
             // the scores' ten tiles that hold any, by their transposes
-#pragma unroll
-            for (int n = 0; n < 3; ++n) {
-                const int tile = w + 4 * n;
+#pragma unroll 1   // their fragments take the registers of one at a time
+            for (int i = 0; i < (10 + WAVES - 1) / WAVES; ++i) {
+                const int tile = w + WAVES * i;
                 if (tile < 10) {
                     const int big = (int)(0x3333222110ull >> 4 * tile) & 15;
                     const int small = (int)(0x3210210100ull >> 4 * tile) & 15;
                     const int qt = 16 * (rev ? small : big), kt = 16 * (rev ? big : small);
                     f32x4 p = {0, 0, 0, 0};
 #pragma unroll
-                    for (int s = 0; s < D; s += 32)
-                        p = mma(frag_row<E>(sk + (kt + m) * LD + s + 8 * g),
-                                frag_row<E>(sq + (qt + m) * LD + s + 8 * g), p);
+                    for (int d = 0; d < D; d += 32)
+                        p = mma(R::row(sk, l, kt, d), R::row(sq, l, qt, d), p);
                     const int qi = c * kBlock + qt + m, ki = c * kBlock + kt + 4 * g;
                     const float qh = ghi[qi], ql = glo[qi];
+                    const f32x4 kh = *(const f32x4 *)(ghi + ki), kl = *(const f32x4 *)(glo + ki);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        float e = (qh - ghi[ki + r]) + (ql - glo[ki + r]);
-                        e = rev ? -e : e;
-                        const bool in = rev ? ki + r >= qi : ki + r <= qi;
-                        p[r] = in ? p[r] * (__builtin_amdgcn_exp2f(e) * o.pscale) : 0.0f;
+                        float e = (qh - kh[r]) + (ql - kl[r]);
+                        e = __builtin_amdgcn_exp2f(rev ? -e : e) * o.pscale * p[r];
+                        p[r] = (rev ? ki + r >= qi : ki + r <= qi) ? e : 0.0f;
                     }
-                    sp.set(qt + m, kt + 4 * g, p);
+                    sp.set(lp, qt, kt, p);
                 }
             }
-        }
 
-        f32x4 acc[4][NC];
-        if constexpr (!STATES) {
             // the state's part, transposed: lane 16 g + m holds columns 4 g .. of row m
+            f32x4 acc[4][NC];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int n = 0; n < NC; ++n)
-                    acc[q][n] = f32x4{0, 0, 0, 0};
+                for (int e = 0; e < NC; ++e)
+                    acc[q][e] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int s = 0; s < D / 32; ++s) {
+            for (int d = 0; d < D / 32; ++d) {
+                __builtin_amdgcn_sched_barrier(0);
                 typename M::Value st[NC];
 #pragma unroll
-                for (int n = 0; n < NC; ++n)
-                    st[n] = M::value(__builtin_shufflevector(S[2 * s][n], S[2 * s + 1][n], 0, 1, 2,
+                for (int e = 0; e < NC; ++e)
+                    st[e] = M::value(__builtin_shufflevector(S[2 * d][e], S[2 * d + 1][e], 0, 1, 2,
                                                              3, 4, 5, 6, 7));
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const auto f =
-                        M::input(frag_row<E>(sq + (16 * q + m) * LD + 32 * s + 8 * g));
+                    const auto f = M::input(R::halves(sq, l, 16 * q, 32 * d));
 #pragma unroll
-                    for (int n = 0; n < NC; ++n)
-                        acc[q][n] = M::mma(st[n], f, acc[q][n]);
+                    for (int e = 0; e < NC; ++e)
+                        acc[q][e] = M::mma(st[e], f, acc[q][e]);
                 }
             }
             __syncthreads();   // the scores
@@ -318,57 +491,81 @@ __global__ __launch_bounds__(kThreads, sizeof(E) == 2 ? 2 : 1) void attention_ke
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int n = 0; n < NC; ++n)
-                    v[j][n] = M::input(values(j, n));
+                for (int e = 0; e < NC; ++e)
+                    v[j][e] = M::input(R::column(sv, l, 32 * j, n0 + 16 * e));
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float u = wq[c * kBlock + 16 * q + m];
 #pragma unroll
-                for (int n = 0; n < NC; ++n)
-                    acc[q][n] *= u;
+                for (int e = 0; e < NC; ++e)
+                    acc[q][e] *= u;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     if (rev ? (j == 0 && q >= 2) : (j == 1 && q < 2))
                         continue;
-                    const typename M::Value f = sp.get(16 * q + m, 32 * j + 8 * g);
+                    const auto f = sp.get(lp, 16 * q, 32 * j);
 #pragma unroll
-                    for (int n = 0; n < NC; ++n)
-                        acc[q][n] = M::mma(v[j][n], f, acc[q][n]);
+                    for (int e = 0; e < NC; ++e)
+                        acc[q][e] = M::mma(v[j][e], f, acc[q][e]);
                 }
             }
-        }
 
-        if constexpr (!STATES) {
             // ---- the rows, and their products with `dot`
+            const int rows = have - c * kBlock;   // past them: 0
+            const long long row0 = b * o.ob + (t0 + c * kBlock) * o.ot + h * o.oh;
+            if constexpr (WHOLE) {
+                char *p = (char *)((E *)o.out + row0);
+                const int size = (int)sizeof(E), stop = a.L - t0 - c * kBlock;
+                const unsigned at = (m * (int)o.ot + n0 + 4 * g) * size;
+                if (rows < kBlock)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int t = c * kBlock + 16 * q + m;
-                const long long row = t0 + t;
-                float sum = 0.0f;
+                    for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int n = 0; n < NC; ++n) {
-                    const int col = 16 * (w * NC + n) + 4 * g, count = min(o.dn - col, 4);
-                    float x[4];
+                        for (int e = 0; e < NC; ++e)
+                            acc[q][e] = 16 * q + m < rows ? acc[q][e] : f32x4{0, 0, 0, 0};
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        x[r] = t < have ? acc[q][n][r] : 0.0f;
-                    if (row < a.L && count > 0) {
-                        const long long i = b * o.ob + row * o.ot + h * o.oh + col;
-                        if (o.out_f32)
-                            store_upto<float, 4>((float *)o.out + i, count, x);
-                        else
-                            store_upto<E, 4>((E *)o.out + i, count, x);
-                        if (o.dots && t < have) {
-                            float y[4];
-                            load_upto<E, 4>(head_rows<E>(o.dot, b, h) + row * o.dot.st + col, count,
-                                            y);
+                for (int q = 0; q < 4; ++q) {
+                    if (16 * q + m < stop)
+#pragma unroll
+                        for (int e = 0; e < NC; ++e) {
+                            float x[4];
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
-                                sum = __builtin_fmaf(x[r], y[r], sum);
+                                x[r] = acc[q][e][r];
+                            store_vec<E, 4>((E *)(p + (16ll * q * o.ot + 16 * e) * size + at), x);
+                        }
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int e = 0; e < NC; ++e) {
+                        const int col = n0 + 16 * e + 4 * g, count = min(o.dn - col, 4);
+                        const int t = 16 * q + m;
+                        float x[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            acc[q][e][r] = x[r] = t < rows ? acc[q][e][r] : 0.0f;
+                        if (t0 + c * kBlock + t < a.L && count > 0) {
+                            const long long i = row0 + t * o.ot + col;
+                            if (o.out_f32)
+                                store_upto<float, 4>((float *)o.out + i, count, x);
+                            else
+                                store_upto<E, 4>((E *)o.out + i, count, x);
                         }
                     }
-                }
-                if (o.dots) {
+            }
+            if (o.dots) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < NC; ++e)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float u = acc[q][e][r] * (float)dot[q][e][r];
+                            sum += WHOLE || n0 + 16 * e + 4 * g + r < o.dn ? u : 0.0f;
+                        }
                     sum += __shfl_xor(sum, 16);
                     sum += __shfl_xor(sum, 32);
                     if (g == 0)
@@ -379,35 +576,48 @@ __global__ __launch_bounds__(kThreads, sizeof(E) == 2 ? 2 : 1) void attention_ke
 
         // ---- the state after the block
         const float f = __builtin_amdgcn_exp2f((float)total[c]);
-        typename M::Value vw[2][NC];
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+            for (int e = 0; e < NC; ++e)
+                S[t][e] *= f;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const f32x8 u = frag_row<float>(wk + c * kBlock + 32 * j + 8 * g);
+            f32x8 weighted[NC];
+            typename M::Value v[NC];
 #pragma unroll
-            for (int n = 0; n < NC; ++n)
-                vw[j][n] = M::value(__builtin_convertvector(values(j, n), f32x8) * u);
-        }
+            for (int e = 0; e < NC; ++e) {
+                weighted[e] = __builtin_convertvector(R::column(sv, l, 32 * j, n0 + 16 * e), f32x8) * u;
+                v[e] = M::value(weighted[e]);
+            }
+            if (exact) {
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) {
+                for (int e = 0; e < NC; ++e) {
+                    const auto rest = M::rest(weighted[e], v[e]);
 #pragma unroll
-            for (int n = 0; n < NC; ++n)
-                S[t][n] *= f;
+                    for (int t = 0; t < D / 16; ++t)
+                        S[t][e] = M::mma_rest(M::input(R::column(sk, l, 32 * j, 16 * t)), v[e], rest,
+                                              S[t][e]);
+                }
+            }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const auto k = M::input(frag_column<8>(
-                    sk + 32 * j * LD + 32 * (t / 2) + 4 * (t % 2), LD, lane));
+            for (int t = 0; t < D / 16; ++t) {
+                const auto k = M::input(R::column(sk, l, 32 * j, 16 * t));
 #pragma unroll
-                for (int n = 0; n < NC; ++n)
-                    S[t][n] = M::mma(k, vw[j][n], S[t][n]);
+                for (int e = 0; e < NC; ++e)
+                    S[t][e] = M::mma(k, v[e], S[t][e]);
             }
         }
-
         __syncthreads();
         if (!STATES && o.dots && w == 0) {
             const int t = c * kBlock + lane;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i)
+                sum += sdot[i][lane];
             if (t < have)
-                o.dots[(long long)bh * a.L + t0 + t] =
-                    (sdot[0][lane] + sdot[1][lane]) + (sdot[2][lane] + sdot[3][lane]);
+                o.dots[(long long)bh * a.L + t0 + t] = sum;
         }
     }
 
@@ -430,22 +640,22 @@ __global__ __launch_bounds__(kThreads, sizeof(E) == 2 ? 2 : 1) void attention_ke
         if (!p)
             continue;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int n = 16 * (w * NC + c) + m;
+        for (int e = 0; e < NC; ++e) {
+            const int n = n0 + 16 * e + m;
 #pragma unroll
             for (int t = 0; t < D / 16; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int d = 32 * (t / 2) + 8 * g + 4 * (t % 2) + r;
+                    const int d = 16 * t + 4 * g + r;
                     if (d < o.da && n < o.dn)
-                        p[d * o.sd + n * o.sn] = S[t][c][r];
+                        p[d * o.sd + n * o.sn] = S[t][e][r];
                 }
         }
     }
     if constexpr (!STATES) {
         // rows past the length, behind the last block
-        const int stop = min(a.L - t0, kPart);
-        for (int t = blocks * kBlock + w; t < stop; t += 4)
+        const int stop = min(a.L - t0, a.part);
+        for (int t = blocks * kBlock + w; t < stop; t += WAVES)
             for (int n = lane; n < o.dn; n += 64) {
                 const long long i = b * o.ob + (t0 + t) * o.ot + h * o.oh + n;
                 if (o.out_f32)
@@ -466,12 +676,23 @@ __global__ __launch_bounds__(256) void join_kernel(float *buf, const float *deca
     if (i >= size)
         return;
     float *p = buf + bh * (long long)(parts + 1) * size + i;
+    const float *d = decays + (long long)bh * parts;
     float s = first ? first[bh * (long long)size + i] : 0.0f;
-    for (int n = 0; n < parts; ++n) {
-        const int c = rev ? parts - 1 - n : n;
-        const float l = p[(long long)c * size];
-        p[(long long)c * size] = s;
-        s = __builtin_fmaf(s, decays[(long long)bh * parts + c], l);
+    constexpr int kAhead = 8;
+    for (int n0 = 0; n0 < parts; n0 += kAhead) {
+        float l[kAhead];
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) {
+            const int at = min(n0 + n, parts - 1), c = rev ? parts - 1 - at : at;
+            l[n] = p[(long long)c * size];
+        }
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n)
+            if (n0 + n < parts) {
+                const int c = rev ? parts - 1 - (n0 + n) : n0 + n;
+                p[(long long)c * size] = s;
+                s = __builtin_fmaf(s, d[c], l[n]);
+            }
     }
     p[(long long)parts * size] = s;
     if (last)
@@ -483,7 +704,7 @@ template <typename E>
 __global__ __launch_bounds__(256) void decay_grad_kernel(
     const float *qdots, const float *kdots, const float *states, const float *grads, long long gbh,
     const float *after, E *dg, long long sb, long long st, long long sh, const int *lengths,
-    int size, int L, int H, int parts) {
+    int size, int L, int H, int parts, int span) {
     __shared__ double sums[256];
     const int at = block_of(), bh = at / parts, part = at - bh * parts;
     const int b = bh / H, h = bh - b * H, tid = threadIdx.x;
@@ -492,9 +713,20 @@ __global__ __launch_bounds__(256) void decay_grad_kernel(
     const float *x = part + 1 < parts ? grads + bh * gbh + part * (long long)size
                                       : (after ? after + bh * (long long)size : nullptr);
     double over = 0.0;
-    if (x)
-        for (int i = tid; i < size; i += 256)
-            over += (double)s[i] * x[i];
+    if (x) {
+        // four sums of fp32 side by side, of 16 products each at most
+        float part[4] = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int i = 4 * tid; i < size; i += 1024) {
+            float u[4], v[4];
+            load_upto<float, 4>(s + i, size - i, u);
+            load_upto<float, 4>(x + i, size - i, v);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                part[r] = __builtin_fmaf(u[r], v[r], part[r]);
+        }
+        over = ((double)part[0] + part[1]) + ((double)part[2] + part[3]);
+    }
     sums[tid] = over;
     __syncthreads();
     for (int d = 128; d > 0; d /= 2) {
@@ -505,12 +737,12 @@ __global__ __launch_bounds__(256) void decay_grad_kernel(
     over = sums[0];
     __syncthreads();
     // the sums from position t on: two positions a thread
-    const int t0 = part * kPart + 2 * tid;
+    const int t0 = part * span + 2 * tid;
     double v[2];
     for (int j = 0; j < 2; ++j) {
         const int t = t0 + j;
         const long long i = bh * (long long)L + t;
-        v[j] = t < end && 2 * tid + j < kPart ? (double)qdots[i] - kdots[i] : 0.0;
+        v[j] = t < end && 2 * tid + j < span ? (double)qdots[i] - kdots[i] : 0.0;
     }
     sums[tid] = v[0] + v[1];
     __syncthreads();
@@ -523,7 +755,7 @@ __global__ __launch_bounds__(256) void decay_grad_kernel(
     const double behind = tid + 1 < 256 ? sums[tid + 1] : 0.0;
     for (int j = 0; j < 2; ++j) {
         const int t = t0 + j;
-        if (t < L)
+        if (t < L && 2 * tid + j < span)
             dg[b * sb + t * st + h * sh] =
                 (E)(t < end ? (float)(over + behind + (j ? v[1] : v[0] + v[1])) : 0.0f);
     }
@@ -635,7 +867,11 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepArgs a) {
 
 // ---- the host ------------------------------------------------------------------------
 
-int parts_of(int L) { return L <= kPart ? 1 : (L + kPart - 1) / kPart; }
+// Positions of a part, by the row's length alone: a short row's parts are halves, so that
+// there are more of them side by side (six rows of up to 1531 positions with 12 heads of
+// 100: 108 us, 160 with parts of 512).
+int part_of(int L) { return L > kPart && L <= 4 * kPart ? kPart / 2 : kPart; }
+int parts_of(int L) { return L <= kPart ? 1 : (L + part_of(L) - 1) / part_of(L); }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 bool attention_shape(int type, int B, int L, int H, int G, int DK, int DV) {
@@ -695,23 +931,43 @@ bool good_out(const Heads &x) { return x.distinct && readable(x.r); }
 
 Tensor tensor(const finc_heads &x, int div) { return {x.p, x.sb, x.st, x.sh, div}; }
 
-// f with the type and the padded head dimension.
+// Whether a role's heads fill their tiles, with steps that stay within 31 bits of bytes
+// over a block.
+bool fills(const Role &o, int size) {
+    const long long far = (1ll << 31) / (kBlock * size);
+    return (o.da == 64 || o.da == 128) && o.dn == o.da && !o.out_f32 && o.k.st < far &&
+           o.v.st < far && (!o.out || (o.q.st < far && o.ot < far)) &&
+           (!o.dots || o.dot.st < far);
+}
+
+// f with the type, the padded head dimension and whether the heads fill it.
 template <typename F>
-void with_kernel(int type, int dim, F f) {
+void with_kernel(int type, const Role *o, int roles, F f) {
+    const int dim = o->da > o->dn ? o->da : o->dn;
+    bool whole = true;
+    for (int i = 0; i < roles; ++i)
+        whole = whole && fills(o[i], type_size(type));
     with_type(type, [&](auto e) {
+        auto sized = [&](auto d) {
+            if (whole)
+                f(e, d, std::true_type());
+            else
+                f(e, d, std::false_type());
+        };
         if (dim <= 64)
-            f(e, std::integral_constant<int, 64>());
+            sized(std::integral_constant<int, 64>());
         else
-            f(e, std::integral_constant<int, 128>());
+            sized(std::integral_constant<int, 128>());
     });
 }
 
 // The parts' sums and the states between them.
 void run_states(int type, Args &s, const float *first, float *last, hipStream_t stream) {
     const Role &o = s.role[0];
-    with_kernel(type, o.da > o.dn ? o.da : o.dn, [&](auto e, auto d) {
-        attention_kernel<decltype(e), decltype(d)::value, true>
-            <<<grid_of((long long)s.BH * s.parts), kThreads, 0, stream>>>(s);
+    with_kernel(type, &o, 1, [&](auto e, auto d, auto whole) {
+        constexpr int D = decltype(d)::value, NC = columns_of<decltype(e)>(D);
+        attention_kernel<decltype(e), D, NC, true, decltype(whole)::value>
+            <<<grid_of((long long)s.BH * s.parts), threads_of(D, NC), 0, stream>>>(s);
     });
     const int size = o.da * o.dn, blocks = (size + 255) / 256;
     join_kernel<<<grid_of((long long)s.BH * blocks), 256, 0, stream>>>(
@@ -719,10 +975,10 @@ void run_states(int type, Args &s, const float *first, float *last, hipStream_t 
 }
 
 void run_roles(int type, const Args &s, int roles, hipStream_t stream) {
-    const Role &o = s.role[0];
-    with_kernel(type, o.da > o.dn ? o.da : o.dn, [&](auto e, auto d) {
-        attention_kernel<decltype(e), decltype(d)::value, false>
-            <<<grid_of((long long)s.BH * s.parts * roles), kThreads, 0, stream>>>(s);
+    with_kernel(type, s.role, roles, [&](auto e, auto d, auto whole) {
+        constexpr int D = decltype(d)::value, NC = columns_of<decltype(e)>(D);
+        attention_kernel<decltype(e), D, NC, false, decltype(whole)::value>
+            <<<grid_of((long long)s.BH * s.parts * roles), threads_of(D, NC), 0, stream>>>(s);
     });
 }
 
@@ -735,6 +991,7 @@ Args common(const finc_attention_args *a) {
     s.H = a->H;
     s.BH = a->B * a->H;
     s.parts = parts_of(a->L);
+    s.part = part_of(a->L);
     s.by_bh = make_fastdiv(s.BH);
     s.by_parts = make_fastdiv(s.parts);
     s.by_h = make_fastdiv(s.H);
@@ -810,6 +1067,7 @@ int finc_linear_attention_forward(const finc_attention_args *a, hipStream_t stre
         o.init_bh = size;
         o.keep = a->states;
         o.last = a->state_out;
+        o.exact = true;
     }
     // rows of no position hand their state on: there is nothing to write but that
     if (L == 0 && !o.keep && !o.last)
@@ -945,6 +1203,7 @@ int finc_linear_attention_backward(const finc_attention_args *a, const finc_atte
         rv.init = rk.init = g->dstate_out;
         rv.init_bh = rk.init_bh = size;
         rv.last = g->dstate;
+        rv.exact = true;
     }
     if (L == 0 && !g->dstate)
         return FINC_OK;
@@ -966,7 +1225,7 @@ int finc_linear_attention_backward(const finc_attention_args *a, const finc_atte
         if (dots)
             decay_grad_kernel<E><<<grid_of((long long)s.BH * s.parts), 256, 0, stream>>>(
                 qdots, kdots, a->states, dstates, (s.parts + 1) * size, g->dstate_out,
-                (E *)g->dg.p, g->dg.sb, g->dg.st, g->dg.sh, a->lengths, (int)size, L, H, s.parts);
+                (E *)g->dg.p, g->dg.sb, g->dg.st, g->dg.sh, a->lengths, (int)size, L, H, s.parts, s.part);
     });
     return launched();
 }

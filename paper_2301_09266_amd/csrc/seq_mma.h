@@ -77,8 +77,9 @@ __device__ inline Frag<E> frag_column(const E *p, int ld, int lane) {
 // ---- sums of inputs and of fp32 values ------------------------------------------------
 // The products of an input of 16 bits with an fp32 value take the value as two bf16
 // parts, the second the rest of the first: 16 bits of it at least (an error of 2^-17 of
-// the value), with the range of fp32.  An fp16 input is two bf16 parts itself, exactly;
-// of its four products the smallest is left out (2^-17).  In fp32 all is fp32.
+// the value), with the range of fp32; a third part, the rest of both, holds all of it.  An
+// fp16 input is two bf16 parts itself, exactly; of its products with two parts the
+// smallest is left out (2^-17), with three what is below 2^-25.  In fp32 all is fp32.
 
 struct Parts {
     bf16x8 hi, lo;
@@ -91,6 +92,14 @@ __device__ inline Parts split(const f32x8 &v) {
         p.lo[i] = (bf16)(v[i] - (float)p.hi[i]);
     }
     return p;
+}
+
+__device__ inline bf16x8 third(const f32x8 &v, const Parts &p) {
+    bf16x8 r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        r[i] = (bf16)((v[i] - (float)p.hi[i]) - (float)p.lo[i]);
+    return r;
 }
 
 // What an fp32 value is held as beside inputs of type E, and the inputs beside it.
@@ -107,6 +116,11 @@ struct Mixed {
     __device__ static f32x4 mma(const Input &a, const Value &b, f32x4 c) {
         return finc_seq::mma(a, b.hi, finc_seq::mma(a, b.lo, c));
     }
+    // what the third part adds
+    __device__ static bf16x8 rest(const f32x8 &v, const Value &p) { return third(v, p); }
+    __device__ static f32x4 mma_rest(const Input &a, const Value &, bf16x8 r, f32x4 c) {
+        return finc_seq::mma(a, r, c);
+    }
 };
 template <>
 struct Mixed<f16> {
@@ -121,6 +135,10 @@ struct Mixed<f16> {
         c = finc_seq::mma(a.hi, b.lo, c);
         return finc_seq::mma(a.hi, b.hi, c);
     }
+    __device__ static bf16x8 rest(const f32x8 &v, const Value &p) { return third(v, p); }
+    __device__ static f32x4 mma_rest(const Parts &a, const Parts &b, bf16x8 r, f32x4 c) {
+        return finc_seq::mma(a.hi, r, finc_seq::mma(a.lo, b.lo, c));
+    }
 };
 template <>
 struct Mixed<float> {
@@ -131,6 +149,8 @@ struct Mixed<float> {
     __device__ static f32x4 mma(const f32x8 &a, const f32x8 &b, f32x4 c) {
         return finc_seq::mma(a, b, c);
     }
+    __device__ static int rest(const f32x8 &, const Value &) { return 0; }
+    __device__ static f32x4 mma_rest(const f32x8 &, const f32x8 &, int, f32x4 c) { return c; }
 };
 
 }  // namespace finc_seq
