@@ -550,6 +550,79 @@ __global__ __launch_bounds__(64 * WM * WN, sizeof(E) == 2 ? 2 : 1) void gemm_fas
         emit<E, false, BA>(o, part, at_lane, acc);
 }
 
+// ---- few rows -------------------------------------------------------------------------
+// Up to 16 TM rows: what counts is how many of the weights' loads are under way.  A
+// workgroup has sixteen columns, a wave an eighth of the sum, whose fragments it loads as
+// they are; the eight sums meet in LDS, in order.
+
+constexpr int kFewWaves = 8, kFewAhead = 4;
+
+template <typename E, int TM>
+__global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(Gemm o) {
+    __shared__ f32x4 part[kFewWaves][TM][64];
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = block_of() * 16;
+    if (n0 >= o.N)
+        return;
+    // whole steps of 32 positions, as many for each wave as there are
+    const int steps = (o.K + 31) / 32, share = (steps + kFewWaves - 1) / kFewWaves;
+    const int first = min(w * share, steps), last = min(first + share, steps);
+    const E *b = (const E *)o.b + min(n0 + m, o.N - 1) * o.sb;
+    const E *a[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+        a[i] = (const E *)o.a + min(16 * i + m, o.M - 1) * o.sa;
+    f32x4 acc[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+        acc[i] = f32x4{0, 0, 0, 0};
+    typedef E Eight __attribute__((ext_vector_type(8), aligned(16)));
+    for (int s = first; s < last; s += kFewAhead) {
+        Frag<E> fb[kFewAhead], fa[kFewAhead][TM];
+#pragma unroll
+        for (int j = 0; j < kFewAhead; ++j) {
+            // past the end, what is there before it, times 0
+            const int k = min((s + j) * 32 + 8 * g, o.K - 8);
+            fb[j] = *(const Eight *)(b + k);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+                fa[j][i] = *(const Eight *)(a[i] + k);
+        }
+#pragma unroll
+        for (int j = 0; j < kFewAhead; ++j) {
+            const bool in = s + j < last && (s + j) * 32 + 8 * g < o.K;
+            const Frag<E> none = {};
+            fb[j] = in ? fb[j] : none;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                fa[j][i] = in ? fa[j][i] : none;
+                acc[i] = mma(fb[j], fa[j][i], acc[i]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+        part[w][i][lane] = acc[i];
+    __syncthreads();
+    if (w >= TM)
+        return;
+    // a wave a tile of rows
+    f32x4 sum = part[0][w][lane];
+#pragma unroll
+    for (int j = 1; j < kFewWaves; ++j)
+        sum += part[j][w][lane];
+    const int row = 16 * w + m, col = n0 + 4 * g, count = min(o.N - col, 4);
+    if (row >= o.M || count <= 0)
+        return;
+    float v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        v[r] = sum[r];
+    finish<E, 4>(o, row, col, count, v);
+    store_upto<E, 4>((E *)o.c + row * o.sc + col, count, v);
+}
+
 // The parts of split sums in order, and what follows them.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void split_sum_kernel(Gemm o, const float *part, E *c,
@@ -744,11 +817,22 @@ void launch_gemm(const Plan &p, const Gemm &o, dim3 grid, hipStream_t stream) {
     if (p.fast && p.dim == 128)
         gemm_fast_kernel<E, 128, 128, 2, 2, 4, AA, BA><<<grid, 256, 0, stream>>>(o);
     else if (p.fast)
-        gemm_fast_kernel<E, 64, 64, 2, 2, 4, AA, BA><<<grid, 256, 0, stream>>>(o);
+        // more stages hide more of a short row of tiles' latency (256 x 4096 x 4096 bf16 21
+        // us, 28 with four), but take the places of tiles side by side
+        gemm_fast_kernel<E, 64, 64, 2, 2, sizeof(E) == 2 && !BA ? 6 : 4, AA, BA>
+            <<<grid, 256, 0, stream>>>(o);
     else if (p.dim == 128)
         gemm_kernel<E, 128, 128, AA, BA><<<grid, kThreads, 0, stream>>>(o);
     else
         gemm_kernel<E, 64, 64, AA, BA><<<grid, kThreads, 0, stream>>>(o);
+}
+
+// Whether the kernel of few rows is the faster one (2048 x 2048 in bf16: 4.6 us for one row,
+// 6.0 for sixteen and 7.9 for 32, by tiles 7.7, 8.9 and 9.3; 2048 x 16384: 13.9, 17.9 and
+// 24.9 against 15.8, 16.3 and 16.5; sums over 8192: 10.8 and 16.3 against 10.7 and 12.6).
+bool few(int M, int N, int K) {
+    return K >= 8 && K <= 4096 &&
+           (M == 1 || (M <= 32 && cdivll(M, 16) * N * (long long)K <= 1ll << 24));
 }
 
 template <bool AA, bool BA>
@@ -760,6 +844,17 @@ void run_gemm(int type, Gemm o, void *workspace, hipStream_t stream) {
     o.per = p.per;
     o.tiles_m = (int)cdivll(o.M, p.dim);
     o.tiles_n = (int)cdivll(o.N, p.dim);
+    if (!AA && !BA && fast && few(o.M, o.N, o.K)) {
+        with_type(type, [&](auto e) {
+            typedef decltype(e) E;
+            const dim3 grid = grid_of(cdivll(o.N, 16));
+            if (o.M <= 16)
+                gemm_few_kernel<E, 1><<<grid, 64 * kFewWaves, 0, stream>>>(o);
+            else
+                gemm_few_kernel<E, 2><<<grid, 64 * kFewWaves, 0, stream>>>(o);
+        });
+        return;
+    }
     void *c = o.c;
     if (p.split > 1)
         o.c = workspace;
