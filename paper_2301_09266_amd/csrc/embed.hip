@@ -85,20 +85,23 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Sort s) {
     s.counts[blockIdx.x * kDigits + threadIdx.x] = n[threadIdx.x];
 }
 
-// Sum of the values of the threads before this one.
-__device__ inline int before(int v, int (&sums)[kThreads]) {
-    const int t = threadIdx.x;
-    sums[t] = v;
-    __syncthreads();
-    for (int d = 1; d < kThreads; d *= 2) {
-        const int u = t >= d ? sums[t - d] : 0;
-        __syncthreads();
-        sums[t] += u;
-        __syncthreads();
+// Sum of the values of the threads before this one, of the first 256 (all of the
+// workgroup's threads call).
+__device__ inline int before(int v, int (&waves)[4]) {
+    const int t = threadIdx.x, lane = t & 63;
+    int s = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int u = __shfl_up(s, d);
+        s += lane >= d ? u : 0;
     }
-    const int r = sums[t] - v;
+    if (lane == 63 && t < 256)
+        waves[t >> 6] = s;
     __syncthreads();
-    return r;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        s += t >> 6 > i ? waves[i] : 0;
+    return s - v;
 }
 
 // The lanes (of those that are `in`) with this lane's digit.
@@ -113,7 +116,7 @@ __device__ inline unsigned long long peers(unsigned digit, bool in) {
 }
 
 __global__ __launch_bounds__(kThreads) void place_kernel(Sort s) {
-    __shared__ int place[kWaves][kDigits], sums[kThreads];
+    __shared__ int place[kWaves][kDigits], sums[4];
     const int t = threadIdx.x, lane = t & 63, w = t >> 6, block = blockIdx.x;
     // this digit's place: all of the smaller ones, and those of the blocks before
     int all = 0, earlier = 0;
@@ -159,6 +162,67 @@ __global__ __launch_bounds__(kThreads) void place_kernel(Sort s) {
                 place[w][digit] += __popcll(same);
         }
         wave_exchange();
+    }
+}
+
+// Short lists in one launch: a workgroup keeps them in LDS from pass to pass.
+constexpr int kShort = 4096, kShortThreads = 1024, kShortWaves = kShortThreads / 64;
+
+__global__ __launch_bounds__(kShortThreads) void sort_short_kernel(Sort s) {
+    __shared__ unsigned key[2][kShort];
+    __shared__ int at[2][kShort];
+    __shared__ int place[kShortWaves][kDigits], totals[4];
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    for (int i = t; i < s.M; i += kShortThreads) {
+        key[0][i] = s.ids.key(i);
+        at[0][i] = i;
+    }
+    const int share = (s.M + kShortWaves - 1) / kShortWaves;
+    const int lo = min(w * share, s.M), hi = min(lo + share, s.M);
+    int from = 0;
+    for (int shift = 0; shift < 32 && (shift == 0 || s.ids.V >> shift); shift += 8) {
+        for (int i = t; i < kShortWaves * kDigits; i += kShortThreads)
+            (&place[0][0])[i] = 0;
+        __syncthreads();
+        for (int i = lo + lane; i < hi; i += 64)
+            atomicAdd(&place[w][key[from][i] >> shift & 255u], 1);
+        __syncthreads();
+        // a digit's first place, then that of every wave
+        int all = 0, of[kShortWaves];
+        if (t < kDigits)
+#pragma unroll
+            for (int i = 0; i < kShortWaves; ++i)
+                all += of[i] = place[i][t];
+        int first = before(all, totals);
+        if (t < kDigits)
+#pragma unroll
+            for (int i = 0; i < kShortWaves; ++i) {
+                place[i][t] = first;
+                first += of[i];
+            }
+        __syncthreads();
+        for (int base = lo; base < hi; base += 64) {
+            const int i = base + lane;
+            const bool in = i < hi;
+            const unsigned k = in ? key[from][i] : 0u, digit = k >> shift & 255u;
+            const unsigned long long same = peers(digit, in);
+            const int rank = __popcll(same & ((1ull << lane) - 1ull));
+            const int to = in ? place[w][digit] + rank : 0;
+            wave_exchange();
+            if (in) {
+                key[from ^ 1][to] = k;
+                at[from ^ 1][to] = at[from][i];
+                if (rank == 0)
+                    place[w][digit] += __popcll(same);
+            }
+            wave_exchange();
+        }
+        __syncthreads();
+        from ^= 1;
+    }
+    for (int i = t; i < s.M; i += kShortThreads) {
+        s.key_out[i] = key[from][i];
+        s.at_out[i] = at[from][i];
     }
 }
 
@@ -232,12 +296,13 @@ __device__ void sum_tiles(const Sum &s, long long group, int lane) {
     flush(next == run);
 }
 
-// Rows that no code names: zeros.  A wave looks for 64 of them in the list.
+// Rows that no code names: zeros.  A wave looks for a few rows in the list, a lane each.
+constexpr int kFillRows = 8;
 __device__ inline void fill_rows(const Sum &s, long long wave, int lane) {
-    const long long v0 = wave * 64;
+    const long long v0 = wave * kFillRows;
     if (v0 >= s.V)
         return;
-    const int v = (int)min(v0 + lane, (long long)s.V - 1);
+    const int v = (int)min(v0 + (lane & (kFillRows - 1)), (long long)s.V - 1);
     int lo = 0, hi = s.M;   // the first entry of at least v
     while (lo < hi) {
         const int mid = lo + (hi - lo) / 2;
@@ -247,7 +312,7 @@ __device__ inline void fill_rows(const Sum &s, long long wave, int lane) {
             hi = mid;
     }
     const bool there = lo < s.M && s.key[lo] == (unsigned)v;
-    unsigned long long absent = __ballot(v0 + lane < s.V && !there);
+    unsigned long long absent = __ballot(lane < kFillRows && v0 + lane < s.V && !there);
     const float zero[4] = {0, 0, 0, 0};
     while (absent) {
         const int i = __ffsll((long long)absent) - 1;
@@ -303,12 +368,19 @@ __global__ __launch_bounds__(kThreads) void join_runs_kernel(Sum s) {
     float sum[kVec] = {};
     if (g == 0)
         load_upto<float, kVec>(s.tail + (long long)tile * s.D + col, count, sum);
-    for (int i = lo; i < hi; ++i) {
-        float v[kVec];
-        load_upto<float, kVec>(s.head + ((long long)tile + 1 + i) * s.D + col, count, v);
+    constexpr int kAhead = 8;
+    for (int i = lo; i < hi; i += kAhead) {
+        float v[kAhead][kVec];
 #pragma unroll
-        for (int j = 0; j < kVec; ++j)
-            sum[j] += v[j];
+        for (int e = 0; e < kAhead; ++e)
+            load_upto<float, kVec>(
+                s.head + ((long long)tile + 1 + min(i + e, hi - 1)) * s.D + col, count, v[e]);
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+            if (i + e < hi)
+#pragma unroll
+                for (int j = 0; j < kVec; ++j)
+                    sum[j] += v[e][j];
     }
 #pragma unroll
     for (int j = 0; j < kVec; ++j)
@@ -419,7 +491,11 @@ int finc_embed_backward(int type, const void *ids, int wide, const void *dy, lon
     o.per = o.per < kSortBlock ? kSortBlock : o.per;
     o.blocks = (int)cdivll(M, o.per);
     int from = 0;
-    if (M > 0)
+    if (M > 0 && M <= kShort) {
+        o.key_out = keys[0];
+        o.at_out = at[0];
+        sort_short_kernel<<<1, kShortThreads, 0, stream>>>(o);
+    } else if (M > 0)
         for (o.shift = 0; o.shift < 32 && (o.shift == 0 || V >> o.shift); o.shift += 8) {
             o.key_out = keys[from ^ 1];
             o.at_out = at[from ^ 1];
@@ -447,7 +523,7 @@ int finc_embed_backward(int type, const void *ids, int wide, const void *dy, lon
         s.lanes *= 2;
     s.slices = (D + s.lanes * kVec - 1) / (s.lanes * kVec);
     s.sum_blocks = cdivll((long long)s.tiles * s.slices, kThreads / s.lanes);
-    const long long blocks = s.sum_blocks + cdivll(V, 64 * kWaves);
+    const long long blocks = s.sum_blocks + cdivll(V, kFillRows * kWaves);
     with_type(type, [&](auto e) {
         sum_kernel<decltype(e)><<<grid_of(blocks), kThreads, 0, stream>>>(s);
     });

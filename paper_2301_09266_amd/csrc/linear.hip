@@ -565,7 +565,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(Gemm o) {
     const int n0 = block_of() * 16;
     if (n0 >= o.N)
         return;
-    // whole steps of 32 positions, as many for each wave as there are
+    // steps of 32 positions, as many for each wave as there are; a lane's eight of them lie
+    // below K or past it
     const int steps = (o.K + 31) / 32, share = (steps + kFewWaves - 1) / kFewWaves;
     const int first = min(w * share, steps), last = min(first + share, steps);
     const E *b = (const E *)o.b + min(n0 + m, o.N - 1) * o.sb;
@@ -831,7 +832,7 @@ void launch_gemm(const Plan &p, const Gemm &o, dim3 grid, hipStream_t stream) {
 // 6.0 for sixteen and 7.9 for 32, by tiles 7.7, 8.9 and 9.3; 2048 x 16384: 13.9, 17.9 and
 // 24.9 against 15.8, 16.3 and 16.5; sums over 8192: 10.8 and 16.3 against 10.7 and 12.6).
 bool few(int M, int N, int K) {
-    return K >= 8 && K <= 4096 &&
+    return K % 8 == 0 && K <= 4096 &&   // a lane's eight positions at once
            (M == 1 || (M <= 32 && cdivll(M, 16) * N * (long long)K <= 1ll << 24));
 }
 

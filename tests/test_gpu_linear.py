@@ -42,7 +42,8 @@ SIZES = [  # M, K, N, type, wide
     (100, 200, 300, F16, False), (1, 2048, 512, BF16, False), (64, 2048, 512, BF16, False),
     (63, 1031, 70, F32, True), (700, 64, 40, BF16, True), (1531, 333, 250, F32, False),
     (2100, 96, 2050, BF16, False), (2049, 40, 2056, F32, True), (2049, 130, 2055, F16, True),
-    (300, 5000, 17, F16, False), (5, 16, 4097, BF16, False), (129, 257, 16, F32, True),
+    (20, 12, 9, F32, False), (5, 20, 64, F32, False), (17, 40, 130, BF16, False),
+    (1, 4096, 33, F16, False), (32, 1000, 100, F32, False), (300, 5000, 17, F16, False), (5, 16, 4097, BF16, False), (129, 257, 16, F32, True),
 ]
 
 
