@@ -184,5 +184,4 @@ def test_the_binding_refuses():
     with pytest.raises(finc.FincError):
         finc.embed_forward(ids, table, out=table[:4])
     with pytest.raises(finc.FincError):
-        finc.embed_backward(ids, dy, -1, dtable=None) if False else finc.embed_backward(
-            ids, table[:4], 5, dtable=table)
+        finc.embed_backward(ids, table[:4], 5, dtable=table)
