@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kThreads) void gemm_kernel(Gemm o) {
 
 constexpr int kStep = 32;   // positions of the sum of a stage
 
-__device__ const float kZeros[4] = {0, 0, 0, 0};
+__device__ __align__(16) const float kZeros[4] = {0, 0, 0, 0};
 
 // Waits until at most N of this wave's loads are under way, and for the other waves.
 template <int N>
@@ -708,7 +708,7 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(const E *dy, long lo
 __global__ __launch_bounds__(1024) void column_sum_kernel(const float *sums, float *out, int N,
                                                           int blocks) {
     __shared__ float part[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = block_of() * 64 + lane;
     const int share = (blocks + 15) / 16, lo = min(w * share, blocks), hi = min(lo + share, blocks);
     float s = 0.0f;
     if (c < N) {
@@ -972,7 +972,7 @@ int finc_linear_backward(const finc_linear_grad_args *a, hipStream_t stream) {
                 a->dbias ? sums : nullptr, a->act, M, N, slices, sum_rows(M, N));
         });
     if (a->dbias)
-        column_sum_kernel<<<(N + 63) / 64, 1024, 0, stream>>>(sums, a->dbias, N, blocks);
+        column_sum_kernel<<<grid_of(cdivll(N, 64)), 1024, 0, stream>>>(sums, a->dbias, N, blocks);
     Gemm o = {};
     o.a = act ? d : a->dy;
     o.sa = act ? N : a->sdy;

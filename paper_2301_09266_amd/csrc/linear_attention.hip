@@ -670,10 +670,10 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
 // place), or (rev) their gradients after every part and before the first one.
 __global__ __launch_bounds__(256) void join_kernel(float *buf, const float *decays,
                                                    const float *first, float *last, int size,
-                                                   int parts, int blocks, bool rev) {
+                                                   int BH, int parts, int blocks, bool rev) {
     const int at = block_of(), bh = at / blocks;
     const int i = (at - bh * blocks) * 256 + (int)threadIdx.x;
-    if (i >= size)
+    if (bh >= BH || i >= size)
         return;
     float *p = buf + bh * (long long)(parts + 1) * size + i;
     const float *d = decays + (long long)bh * parts;
@@ -704,9 +704,11 @@ template <typename E>
 __global__ __launch_bounds__(256) void decay_grad_kernel(
     const float *qdots, const float *kdots, const float *states, const float *grads, long long gbh,
     const float *after, E *dg, long long sb, long long st, long long sh, const int *lengths,
-    int size, int L, int H, int parts, int span) {
+    int size, int BH, int L, int H, int parts, int span) {
     __shared__ double sums[256];
     const int at = block_of(), bh = at / parts, part = at - bh * parts;
+    if (bh >= BH)
+        return;
     const int b = bh / H, h = bh - b * H, tid = threadIdx.x;
     const int end = lengths ? min(max(lengths[b], 0), L) : L;
     const float *s = states + (bh * (long long)(parts + 1) + part + 1) * size;
@@ -796,7 +798,7 @@ struct StepArgs {
     float *state;
     const int *slots;
     float scale;
-    int S, H, DK, DV, cols;
+    int B, S, H, DK, DV, cols;
     FastDiv by_cols, by_h;
 };
 
@@ -810,6 +812,8 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepArgs a) {
     int at = block_of();
     const int bh = fdiv(at, a.by_cols), block = at - bh * a.cols;
     const int b = fdiv(bh, a.by_h), h = bh - b * a.H;
+    if (b >= a.B)
+        return;
     const int col = block * 32 + (lane & 7) * 4, count = a.DV - col;
     const int row = w * 8 + (lane >> 3);
     const int slot = a.slots ? a.slots[b] : b;
@@ -971,7 +975,7 @@ void run_states(int type, Args &s, const float *first, float *last, hipStream_t 
     });
     const int size = o.da * o.dn, blocks = (size + 255) / 256;
     join_kernel<<<grid_of((long long)s.BH * blocks), 256, 0, stream>>>(
-        s.local, s.decays, first, last, size, s.parts, blocks, o.rev);
+        s.local, s.decays, first, last, size, s.BH, s.parts, blocks, o.rev);
 }
 
 void run_roles(int type, const Args &s, int roles, hipStream_t stream) {
@@ -1225,7 +1229,8 @@ int finc_linear_attention_backward(const finc_attention_args *a, const finc_atte
         if (dots)
             decay_grad_kernel<E><<<grid_of((long long)s.BH * s.parts), 256, 0, stream>>>(
                 qdots, kdots, a->states, dstates, (s.parts + 1) * size, g->dstate_out,
-                (E *)g->dg.p, g->dg.sb, g->dg.st, g->dg.sh, a->lengths, (int)size, L, H, s.parts, s.part);
+                (E *)g->dg.p, g->dg.sb, g->dg.st, g->dg.sh, a->lengths, (int)size, s.BH, L, H,
+                s.parts, s.part);
     });
     return launched();
 }
@@ -1263,6 +1268,7 @@ int finc_linear_attention_step(const finc_attention_step_args *a, hipStream_t st
     s.state = a->state;
     s.slots = a->slots;
     s.scale = (float)a->scale;
+    s.B = B;
     s.S = a->S;
     s.H = H;
     s.DK = DK;

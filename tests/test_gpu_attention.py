@@ -423,6 +423,39 @@ def test_offsets_past_31_bits():
     assert float(cache[:S - 1].abs().max()) == 0.0
 
 
+def test_more_workgroups_than_a_row_of_the_grid():
+    """Launches past 2^21 workgroups lie in rows of the grid, the last one partly without
+    work: parts, their join and the decays' gradient; single positions.  All rows are the
+    same, and so are their bits."""
+    B, L = (1 << 21) + 5, 513
+    x = [torch.randn(1, L, 1, 1, dtype=BF16, device=DEV).expand(B, L, 1, 1) for _ in range(4)]
+    g = -x[3][..., 0].exp() * 0.05
+    few = [t[:2].contiguous() for t in (*x, g)]
+
+    def run(q, k, v, dy, g):
+        n = q.shape[0]
+        states = finc.linear_attention_states(n, L, 1, 1, 1, DEV)
+        guard = torch.full((n + 64,), 7.0, device=DEV)
+        end = guard[:n].view(n, 1, 1, 1)
+        y = finc.linear_attention_forward(q, k, v, g=g, states=states, state_out=end)
+        assert bool((guard[n:] == 7.0).all())
+        o = finc.linear_attention_backward(q, k, v, dy, states, g=g)
+        return y, end, o["dq"], o["dk"], o["dv"], o["dg"]
+
+    want = run(*few)
+    for t, w in zip(run(*x, g), want):
+        assert bool((t == w[:1]).all())
+    del t
+    B, H, D = (1 << 19) + 3, 1, 128
+    guard = torch.zeros((B + 8) * H * D, device=DEV)
+    cache = guard[:B * D].view(B, H, 1, D)
+    slots = torch.arange(B + 4096, dtype=torch.int32, device=DEV).clamp_(max=B)[:B].contiguous()
+    one = torch.ones(1, 1, 1, dtype=BF16, device=DEV).expand(B, 1, 1)
+    v = torch.ones(1, 1, D, dtype=BF16, device=DEV).expand(B, 1, D)
+    y = finc.linear_attention_step(one, one, v, cache, slots=slots)
+    assert bool((y == 1).all()) and bool((cache == 1).all()) and not guard[B * D:].any()
+
+
 def test_the_binding_refuses():
     x = torch.zeros(2, 8, 2, 16, device=DEV)
     S = torch.zeros(2, 2, 16, 16, device=DEV)

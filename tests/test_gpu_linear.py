@@ -218,6 +218,16 @@ def test_offsets_past_31_bits():
     ref.close(dx, y.cpu().double() @ w.double(), "dx", CHAIN)
 
 
+def test_more_columns_than_a_row_of_the_grid():
+    N = (1 << 28) + 65
+    dy = torch.ones(1, 1, dtype=BF16, device=DEV).expand(1, N).contiguous()
+    dy[0, -1] = 3.0
+    x, w = torch.ones(1, 1, dtype=BF16, device=DEV), torch.ones(N, 1, dtype=BF16, device=DEV)
+    dx, dw, db = finc.linear_backward(dy, x, w)
+    assert bool((dw[:, 0] == dy[0]).all()) and float(dx) > N / 2
+    assert float(db[-1]) == 3.0 and bool((db[:-1] == 1).all())
+
+
 def test_the_binding_refuses():
     x, w = torch.zeros(4, 16, device=DEV), torch.zeros(8, 16, device=DEV)
     y = torch.zeros(4, 8, device=DEV)
