@@ -60,7 +60,7 @@ struct Args {
     const int *lengths;
     float *local, *decays;   // states of the parts alone: (B H, parts + 1, da dn), (B H, parts)
     FastDiv by_bh, by_parts, by_h;
-    int L, H, BH, parts, part;   // positions of a part
+    int L, H, BH, parts, part, roles;   // positions of a part; roles of the launch
 };
 
 template <typename E>
@@ -251,26 +251,28 @@ struct Nothing {
 // ---- the kernel ------------------------------------------------------------------
 
 // STATES: the parts' own sums of k v^T alone, and their decays.
-// A wave has 16 NC columns of v and of the state.  WHOLE: heads of D elements, steps of
-// rows below 2^23 and outputs of the type; the code for all else next to it would take its
-// registers.
-constexpr int threads_of(int D, int NC) { return 4 * D / NC; }
+// DA, DN: elements of q and k, and of v, that the tiles hold.  A wave has 16 NC columns of
+// v and of the state.  WHOLE: heads of DA and DN elements, steps of rows below 2^23 and
+// outputs of the type; the code for all else next to it would take its registers.
+constexpr int threads_of(int DN, int NC) { return 4 * DN / NC; }
 // Tiles of columns of a wave: with two, what a wave reads of q and k serves twice as much
 // (one long bf16 prompt 139 us, 161 with one).  fp16 inputs are two parts each, for which
 // two tiles leave no registers (the ragged prompts 108 us, 119).
 template <typename E>
-constexpr int columns_of(int D) {
-    return std::is_same_v<E, f16> ? 1 : D / 64;
+constexpr int columns_of(int DN) {
+    return std::is_same_v<E, f16> ? 1 : DN / 64;
 }
-template <typename E, int D, int NC, bool STATES, bool WHOLE>
-__global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
+template <typename E, int DA, int DN, int NC, bool STATES, bool WHOLE>
+__global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
     void attention_kernel(Args a) {
     typedef Mixed<E> M;
-    typedef Rows<E, D> R;
-    constexpr int WAVES = D / 16 / NC;
-    typedef Tile<E, D, 64 * WAVES> T;
+    typedef Rows<E, DA> R;
+    typedef Rows<E, DN> RV;
+    constexpr int WAVES = DN / 16 / NC;
+    typedef Tile<E, DA, 64 * WAVES> T;
+    typedef Tile<E, DN, 64 * WAVES> TV;
     __shared__ __align__(16) E sk[R::kSize];
-    __shared__ __align__(16) E sv[R::kSize];
+    __shared__ __align__(16) E sv[RV::kSize];
     __shared__ __align__(16) E sq[STATES ? 8 : R::kSize];
     typedef std::conditional_t<STATES, Nothing, Scores<E>> P;
     __shared__ __align__(16) P sp;
@@ -281,15 +283,13 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int at = block_of();
-    if (at >= a.BH * a.parts * (int)(STATES ? 1 : 3))   // the host gives whole roles
+    if (at >= a.BH * a.parts * (STATES ? 1 : a.roles))
         return;
     const int part = at - fdiv(at, a.by_parts) * a.parts;
     at = fdiv(at, a.by_parts);
     const int which = fdiv(at, a.by_bh), bh = at - which * a.BH;
     const int b = fdiv(bh, a.by_h), h = bh - b * a.H;
     const Role &o = a.role[which];
-    if (!STATES && !o.out)
-        return;
     const bool rev = o.rev;
 
     const int t0 = part * a.part;
@@ -303,7 +303,8 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
     const bool exact = STATES || o.exact;
     const E *kp = head_rows<E>(o.k, b, h), *vp = head_rows<E>(o.v, b, h);
     const E *qp = STATES ? nullptr : head_rows<E>(o.q, b, h);
-    T tk, tv, tq;
+    T tk, tq;
+    TV tv;
     auto fetch = [&](int c) __attribute__((always_inline)) {
         const long long t = t0 + c * kBlock;
         const int rows = have - c * kBlock;
@@ -326,18 +327,18 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
     // Element r of tile t is row 16 t + 4 g + r of column n: two tiles are the eight
     // elements that halves() gives of a query.
     const int n0 = 16 * NC * w;
-    f32x4 S[D / 16][NC];
+    f32x4 S[DA / 16][NC];
     const long long size = (long long)o.da * o.dn;
     const float *init =
         !STATES && o.init ? o.init + bh * o.init_bh + part * o.init_p : nullptr;
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t)
+    for (int t = 0; t < DA / 16; ++t)
 #pragma unroll
         for (int c = 0; c < NC; ++c)
             S[t][c] = f32x4{0, 0, 0, 0};
     if (init) {
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t)
+        for (int t = 0; t < DA / 16; ++t)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -384,7 +385,7 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
 
     if (!WHOLE && init) {
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t)
+        for (int t = 0; t < DA / 16; ++t)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -402,11 +403,14 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
     }
 
     const typename R::Lane first = R::lane(lane);
+    const typename RV::Lane first_v = RV::lane(lane);
     const typename P::R::Lane first_p = P::R::lane(lane);
     for (int i = 0; i < blocks; ++i) {
         const int c = rev ? blocks - 1 - i : i;
         const typename R::Lane l = {afresh(first.row), afresh(first.half), afresh(first.column),
                                     afresh(first.below)};
+        const typename RV::Lane lv = {0, 0, DA == DN ? l.column : afresh(first_v.column),
+                                      DA == DN ? l.below : afresh(first_v.below)};
         const typename P::R::Lane lp = {afresh(first_p.row), afresh(first_p.half), 0, 0};
         tk.template store<WHOLE>(sk, have - c * kBlock, o.da);
         tv.template store<WHOLE>(sv, have - c * kBlock, o.dn);
@@ -448,7 +452,7 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
                     const int qt = 16 * (rev ? small : big), kt = 16 * (rev ? big : small);
                     f32x4 p = {0, 0, 0, 0};
 #pragma unroll
-                    for (int d = 0; d < D; d += 32)
+                    for (int d = 0; d < DA; d += 32)
                         p = mma(R::row(sk, l, kt, d), R::row(sq, l, qt, d), p);
                     const int qi = c * kBlock + qt + m, ki = c * kBlock + kt + 4 * g;
                     const float qh = ghi[qi], ql = glo[qi];
@@ -471,7 +475,7 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
                 for (int e = 0; e < NC; ++e)
                     acc[q][e] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d) {
+            for (int d = 0; d < DA / 32; ++d) {
                 __builtin_amdgcn_sched_barrier(0);
                 typename M::Value st[NC];
 #pragma unroll
@@ -492,7 +496,7 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < NC; ++e)
-                    v[j][e] = M::input(R::column(sv, l, 32 * j, n0 + 16 * e));
+                    v[j][e] = M::input(RV::column(sv, lv, 32 * j, n0 + 16 * e));
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float u = wq[c * kBlock + 16 * q + m];
@@ -577,7 +581,7 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
         // ---- the state after the block
         const float f = __builtin_amdgcn_exp2f((float)total[c]);
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t)
+        for (int t = 0; t < DA / 16; ++t)
 #pragma unroll
             for (int e = 0; e < NC; ++e)
                 S[t][e] *= f;
@@ -588,7 +592,7 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
             typename M::Value v[NC];
 #pragma unroll
             for (int e = 0; e < NC; ++e) {
-                weighted[e] = __builtin_convertvector(R::column(sv, l, 32 * j, n0 + 16 * e), f32x8) * u;
+                weighted[e] = __builtin_convertvector(RV::column(sv, lv, 32 * j, n0 + 16 * e), f32x8) * u;
                 v[e] = M::value(weighted[e]);
             }
             if (exact) {
@@ -596,13 +600,13 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
                 for (int e = 0; e < NC; ++e) {
                     const auto rest = M::rest(weighted[e], v[e]);
 #pragma unroll
-                    for (int t = 0; t < D / 16; ++t)
+                    for (int t = 0; t < DA / 16; ++t)
                         S[t][e] = M::mma_rest(M::input(R::column(sk, l, 32 * j, 16 * t)), v[e], rest,
                                               S[t][e]);
                 }
             }
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t) {
+            for (int t = 0; t < DA / 16; ++t) {
                 const auto k = M::input(R::column(sk, l, 32 * j, 16 * t));
 #pragma unroll
                 for (int e = 0; e < NC; ++e)
@@ -643,7 +647,7 @@ __global__ __launch_bounds__(threads_of(D, NC), sizeof(E) == 2 ? 2 : 1)
         for (int e = 0; e < NC; ++e) {
             const int n = n0 + 16 * e + m;
 #pragma unroll
-            for (int t = 0; t < D / 16; ++t)
+            for (int t = 0; t < DA / 16; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int d = 16 * t + 4 * g + r;
@@ -939,51 +943,69 @@ Tensor tensor(const finc_heads &x, int div) { return {x.p, x.sb, x.st, x.sh, div
 // over a block.
 bool fills(const Role &o, int size) {
     const long long far = (1ll << 31) / (kBlock * size);
-    return (o.da == 64 || o.da == 128) && o.dn == o.da && !o.out_f32 && o.k.st < far &&
+    return (o.da == 64 || o.da == 128) && (o.dn == 64 || o.dn == 128) && !o.out_f32 && o.k.st < far &&
            o.v.st < far && (!o.out || (o.q.st < far && o.ot < far)) &&
            (!o.dots || o.dot.st < far);
 }
 
-// f with the type, the padded head dimension and whether the heads fill it.
+// f with the type, the elements that the tiles hold and whether the heads fill them.
 template <typename F>
 void with_kernel(int type, const Role *o, int roles, F f) {
-    const int dim = o->da > o->dn ? o->da : o->dn;
     bool whole = true;
     for (int i = 0; i < roles; ++i)
         whole = whole && fills(o[i], type_size(type));
     with_type(type, [&](auto e) {
-        auto sized = [&](auto d) {
+        auto sized = [&](auto da, auto dn) {
             if (whole)
-                f(e, d, std::true_type());
+                f(e, da, dn, std::true_type());
             else
-                f(e, d, std::false_type());
+                f(e, da, dn, std::false_type());
         };
-        if (dim <= 64)
-            sized(std::integral_constant<int, 64>());
+        const std::integral_constant<int, 64> half;
+        const std::integral_constant<int, 128> full;
+        if (o->da <= 64 && o->dn <= 64)
+            sized(half, half);
+        else if (o->da <= 64)
+            sized(half, full);
+        else if (o->dn <= 64)
+            sized(full, half);
         else
-            sized(std::integral_constant<int, 128>());
+            sized(full, full);
     });
 }
 
 // The parts' sums and the states between them.
 void run_states(int type, Args &s, const float *first, float *last, hipStream_t stream) {
     const Role &o = s.role[0];
-    with_kernel(type, &o, 1, [&](auto e, auto d, auto whole) {
-        constexpr int D = decltype(d)::value, NC = columns_of<decltype(e)>(D);
-        attention_kernel<decltype(e), D, NC, true, decltype(whole)::value>
-            <<<grid_of((long long)s.BH * s.parts), threads_of(D, NC), 0, stream>>>(s);
+    with_kernel(type, &o, 1, [&](auto e, auto da, auto dn, auto whole) {
+        constexpr int DA = decltype(da)::value, DN = decltype(dn)::value;
+        constexpr int NC = columns_of<decltype(e)>(DN);
+        attention_kernel<decltype(e), DA, DN, NC, true, decltype(whole)::value>
+            <<<grid_of((long long)s.BH * s.parts), threads_of(DN, NC), 0, stream>>>(s);
     });
     const int size = o.da * o.dn, blocks = (size + 255) / 256;
     join_kernel<<<grid_of((long long)s.BH * blocks), 256, 0, stream>>>(
         s.local, s.decays, first, last, size, s.BH, s.parts, blocks, o.rev);
 }
 
-void run_roles(int type, const Args &s, int roles, hipStream_t stream) {
-    with_kernel(type, s.role, roles, [&](auto e, auto d, auto whole) {
-        constexpr int D = decltype(d)::value, NC = columns_of<decltype(e)>(D);
-        attention_kernel<decltype(e), D, NC, false, decltype(whole)::value>
-            <<<grid_of((long long)s.BH * s.parts * roles), threads_of(D, NC), 0, stream>>>(s);
-    });
+// Roles of one shape of tiles in one launch.
+void run_roles(int type, Args s, int roles, hipStream_t stream) {
+    while (roles > 0) {
+        const Role &o = s.role[0];
+        int n = 1;
+        while (n < roles && (s.role[n].da > 64) == (o.da > 64) && (s.role[n].dn > 64) == (o.dn > 64))
+            ++n;
+        s.roles = n;
+        with_kernel(type, &o, n, [&](auto e, auto da, auto dn, auto whole) {
+            constexpr int DA = decltype(da)::value, DN = decltype(dn)::value;
+            constexpr int NC = columns_of<decltype(e)>(DN);
+            attention_kernel<decltype(e), DA, DN, NC, false, decltype(whole)::value>
+                <<<grid_of((long long)s.BH * s.parts * n), threads_of(DN, NC), 0, stream>>>(s);
+        });
+        for (int i = n; i < roles; ++i)
+            s.role[i - n] = s.role[i];
+        roles -= n;
+    }
 }
 
 Args common(const finc_attention_args *a) {
@@ -1076,8 +1098,6 @@ int finc_linear_attention_forward(const finc_attention_args *a, hipStream_t stre
     // rows of no position hand their state on: there is nothing to write but that
     if (L == 0 && !o.keep && !o.last)
         return FINC_OK;
-    if (L == 0 && !o.out)
-        o.out = (void *)(o.keep ? o.keep : o.last);   // not written: no row
     run_roles(a->type, s, 1, stream);
     return launched();
 }
@@ -1211,8 +1231,6 @@ int finc_linear_attention_backward(const finc_attention_args *a, const finc_atte
     }
     if (L == 0 && !g->dstate)
         return FINC_OK;
-    if (L == 0 && !rv.out)
-        rv.out = g->dstate;   // not written: no row
     run_roles(a->type, s, L == 0 ? 1 : 3, stream);
     if (L == 0)
         return launched();
