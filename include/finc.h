@@ -725,7 +725,8 @@ int finc_add_norm_backward(const finc_norm_grad_args *a, hipStream_t stream);
  *   that are worked on at once, in a private layout, which the gradients read.  NULL
  *   only where L <= FINC_ATTENTION_PART and no gradients follow.
  *   Inputs of 16 bits are multiplied exactly, and weights and states beside them
- *   with 16 bits at least, in sums of fp32.  Positions are worked on in blocks of 64:
+ *   with 16 bits at least, in sums of fp32 (beside fp16 inputs, fewer of a state's
+ *   element that is below 2^-22 of the largest in its column).  Positions are worked on in blocks of 64:
  *   an infinite or NaN input, or one that overflows, leaves its row's heads without
  *   finite values from the start of its block on (in the gradients: up to its
  *   block's end), and no other outputs.

@@ -248,6 +248,21 @@ struct Nothing {
     typedef Rows<float, kBlock> R;
 };
 
+// Beside fp16 inputs a column of the state is held as 2^k times itself, its largest element
+// in [2^13, 2^14), so that it goes into the products as two fp16 parts and the inputs as
+// they are: two products where two bf16 parts of both took three, and the inputs' were
+// formed by every wave (4 x 4096 x 16 heads of 128: 152 us, 264 before, and 399 for 656 of
+// the gradients).  The power for `most`, the largest absolute value of this lane's part of
+// a column that four lanes share.
+__device__ inline int power(float most) {
+    most = __builtin_fmaxf(most, __shfl_xor(most, 16));
+    most = __builtin_fmaxf(most, __shfl_xor(most, 32));
+    const int e = __builtin_bit_cast(int, most) >> 23;   // 255: infinite, which stays so
+    return 13 + 127 - e;
+}
+// 2^k, |k| < 127
+__device__ inline float two_to(int k) { return __builtin_bit_cast(float, (127 + k) << 23); }
+
 // ---- the kernel ------------------------------------------------------------------
 
 // STATES: the parts' own sums of k v^T alone, and their decays.
@@ -256,12 +271,8 @@ struct Nothing {
 // outputs of the type; the code for all else next to it would take its registers.
 constexpr int threads_of(int DN, int NC) { return 4 * DN / NC; }
 // Tiles of columns of a wave: with two, what a wave reads of q and k serves twice as much
-// (one long bf16 prompt 139 us, 161 with one).  fp16 inputs are two parts each, for which
-// two tiles leave no registers (the ragged prompts 108 us, 119).
-template <typename E>
-constexpr int columns_of(int DN) {
-    return std::is_same_v<E, f16> ? 1 : DN / 64;
-}
+// (one long bf16 prompt 139 us, 161 with one).
+constexpr int columns_of(int DN) { return DN / 64; }
 template <typename E, int DA, int DN, int NC, bool STATES, bool WHOLE>
 __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
     void attention_kernel(Args a) {
@@ -269,6 +280,7 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
     typedef Rows<E, DA> R;
     typedef Rows<E, DN> RV;
     constexpr int WAVES = DN / 16 / NC;
+    constexpr bool SCALED = std::is_same_v<E, f16>;   // the state's columns
     typedef Tile<E, DA, 64 * WAVES> T;
     typedef Tile<E, DN, 64 * WAVES> TV;
     __shared__ __align__(16) E sk[R::kSize];
@@ -300,7 +312,7 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
     // Loads first, each behind the other: the first tiles, the state, the decays.
     // A state that leaves the call as fp32 takes its sums in full; for the outputs of 16
     // bits the two parts of its weights do.
-    const bool exact = STATES || o.exact;
+    const bool exact = std::is_same_v<E, bf16> && (STATES || o.exact);
     const E *kp = head_rows<E>(o.k, b, h), *vp = head_rows<E>(o.v, b, h);
     const E *qp = STATES ? nullptr : head_rows<E>(o.q, b, h);
     T tk, tq;
@@ -402,6 +414,33 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
         }
     }
 
+    int k2[NC];   // the state is 2^-k2 times what is held (fp16)
+#pragma unroll
+    for (int e = 0; e < NC; ++e)
+        k2[e] = init ? 0 : 126;
+    auto rescale = [&]() __attribute__((always_inline)) {
+        if constexpr (SCALED)
+#pragma unroll
+            for (int e = 0; e < NC; ++e) {
+                float most = 0.0f;
+#pragma unroll
+                for (int t = 0; t < DA / 16; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        most = __builtin_fmaxf(most, __builtin_fabsf(S[t][e][r]));
+                // a column of zeros has the largest power, below what is added to it next
+                const int k = power(most) > 126 ? 126 - k2[e]
+                                                : max(min(power(most), 126 - k2[e]), -126 - k2[e]);
+                const float f = two_to(max(min(k, 126), -126));
+                k2[e] += k;
+#pragma unroll
+                for (int t = 0; t < DA / 16; ++t)
+                    S[t][e] *= f;
+            }
+    };
+    if (init)
+        rescale();
+
     const typename R::Lane first = R::lane(lane);
     const typename RV::Lane first_v = RV::lane(lane);
     const typename P::R::Lane first_p = P::R::lane(lane);
@@ -477,19 +516,31 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
 #pragma unroll
             for (int d = 0; d < DA / 32; ++d) {
                 __builtin_amdgcn_sched_barrier(0);
-                typename M::Value st[NC];
+                typename M::Scaled st[NC];
 #pragma unroll
                 for (int e = 0; e < NC; ++e)
-                    st[e] = M::value(__builtin_shufflevector(S[2 * d][e], S[2 * d + 1][e], 0, 1, 2,
+                    st[e] = M::scaled(__builtin_shufflevector(S[2 * d][e], S[2 * d + 1][e], 0, 1, 2,
                                                              3, 4, 5, 6, 7));
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const auto f = M::input(R::halves(sq, l, 16 * q, 32 * d));
+                    const auto f = M::beside(R::halves(sq, l, 16 * q, 32 * d));
 #pragma unroll
                     for (int e = 0; e < NC; ++e)
                         acc[q][e] = M::mma(st[e], f, acc[q][e]);
                 }
             }
+            if constexpr (SCALED)
+#pragma unroll
+                for (int e = 0; e < NC; ++e) {
+                    const float f = two_to(-k2[e]);
+                    f32x4 of;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        of[r] = __shfl(f, 4 * g + r);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        acc[q][e] *= of;
+                }
             __syncthreads();   // the scores
             typename M::Input v[2][NC];
 #pragma unroll
@@ -580,39 +631,73 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
 
         // ---- the state after the block
         const float f = __builtin_amdgcn_exp2f((float)total[c]);
-#pragma unroll
-        for (int t = 0; t < DA / 16; ++t)
+        auto weigh = [&](int j, int e, f32x8 u) __attribute__((always_inline)) {
+            return __builtin_convertvector(RV::column(sv, lv, 32 * j, n0 + 16 * e), f32x8) * u;
+        };
+        float by[NC];
+        if constexpr (SCALED) {
 #pragma unroll
             for (int e = 0; e < NC; ++e)
-                S[t][e] *= f;
+                by[e] = f * two_to(-k2[e]) * 0x1p14f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const f32x8 u = frag_row<float>(wk + c * kBlock + 32 * j + 8 * g);
+#pragma unroll
+                for (int e = 0; e < NC; ++e) {
+                    const f32x8 v = weigh(j, e, u);
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        by[e] = __builtin_fmaxf(by[e], __builtin_fabsf(v[r]));
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < NC; ++e) {
+                const int k = min(power(by[e]), 126);
+                by[e] = two_to(k);
+                const float decay = f * two_to(-k2[e]) * by[e];
+                k2[e] = k;
+#pragma unroll
+                for (int t = 0; t < DA / 16; ++t)
+                    S[t][e] *= decay;
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < DA / 16; ++t)
+#pragma unroll
+                for (int e = 0; e < NC; ++e)
+                    S[t][e] *= f;
+        }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const f32x8 u = frag_row<float>(wk + c * kBlock + 32 * j + 8 * g);
             f32x8 weighted[NC];
-            typename M::Value v[NC];
+            typename M::Scaled v[NC];
 #pragma unroll
             for (int e = 0; e < NC; ++e) {
-                weighted[e] = __builtin_convertvector(RV::column(sv, lv, 32 * j, n0 + 16 * e), f32x8) * u;
-                v[e] = M::value(weighted[e]);
+                weighted[e] = weigh(j, e, u);
+                if constexpr (SCALED)
+                    weighted[e] *= by[e];
+                v[e] = M::scaled(weighted[e]);
             }
-            if (exact) {
+            if constexpr (std::is_same_v<E, bf16>)
+                if (exact) {
 #pragma unroll
-                for (int e = 0; e < NC; ++e) {
-                    const auto rest = M::rest(weighted[e], v[e]);
+                    for (int e = 0; e < NC; ++e) {
+                        const bf16x8 rest = third(weighted[e], v[e]);
 #pragma unroll
-                    for (int t = 0; t < DA / 16; ++t)
-                        S[t][e] = M::mma_rest(M::input(R::column(sk, l, 32 * j, 16 * t)), v[e], rest,
-                                              S[t][e]);
+                        for (int t = 0; t < DA / 16; ++t)
+                            S[t][e] = mma(R::column(sk, l, 32 * j, 16 * t), rest, S[t][e]);
+                    }
                 }
-            }
 #pragma unroll
             for (int t = 0; t < DA / 16; ++t) {
-                const auto k = M::input(R::column(sk, l, 32 * j, 16 * t));
+                const auto k = M::beside(R::column(sk, l, 32 * j, 16 * t));
 #pragma unroll
                 for (int e = 0; e < NC; ++e)
                     S[t][e] = M::mma(k, v[e], S[t][e]);
             }
         }
+        rescale();
         __syncthreads();
         if (!STATES && o.dots && w == 0) {
             const int t = c * kBlock + lane;
@@ -624,6 +709,13 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
                 o.dots[(long long)bh * a.L + t0 + t] = sum;
         }
     }
+
+    if constexpr (SCALED)
+#pragma unroll
+        for (int e = 0; e < NC; ++e)
+#pragma unroll
+            for (int t = 0; t < DA / 16; ++t)
+                S[t][e] *= two_to(-k2[e]);
 
     float *ends[2] = {nullptr, nullptr};
     if constexpr (STATES) {
@@ -722,7 +814,6 @@ __global__ __launch_bounds__(256) void decay_grad_kernel(
     if (x) {
         // four sums of fp32 side by side, of 16 products each at most
         float part[4] = {0, 0, 0, 0};
-#pragma unroll 4
         for (int i = 4 * tid; i < size; i += 1024) {
             float u[4], v[4];
             load_upto<float, 4>(s + i, size - i, u);
@@ -979,7 +1070,7 @@ void run_states(int type, Args &s, const float *first, float *last, hipStream_t 
     const Role &o = s.role[0];
     with_kernel(type, &o, 1, [&](auto e, auto da, auto dn, auto whole) {
         constexpr int DA = decltype(da)::value, DN = decltype(dn)::value;
-        constexpr int NC = columns_of<decltype(e)>(DN);
+        constexpr int NC = columns_of(DN);
         attention_kernel<decltype(e), DA, DN, NC, true, decltype(whole)::value>
             <<<grid_of((long long)s.BH * s.parts), threads_of(DN, NC), 0, stream>>>(s);
     });
@@ -998,7 +1089,7 @@ void run_roles(int type, Args s, int roles, hipStream_t stream) {
         s.roles = n;
         with_kernel(type, &o, n, [&](auto e, auto da, auto dn, auto whole) {
             constexpr int DA = decltype(da)::value, DN = decltype(dn)::value;
-            constexpr int NC = columns_of<decltype(e)>(DN);
+            constexpr int NC = columns_of(DN);
             attention_kernel<decltype(e), DA, DN, NC, false, decltype(whole)::value>
                 <<<grid_of((long long)s.BH * s.parts * n), threads_of(DN, NC), 0, stream>>>(s);
         });

@@ -75,11 +75,13 @@ __device__ inline Frag<E> frag_column(const E *p, int ld, int lane) {
 }
 
 // ---- sums of inputs and of fp32 values ------------------------------------------------
-// The products of an input of 16 bits with an fp32 value take the value as two bf16
-// parts, the second the rest of the first: 16 bits of it at least (an error of 2^-17 of
-// the value), with the range of fp32; a third part, the rest of both, holds all of it.  An
-// fp16 input is two bf16 parts itself, exactly; of its products with two parts the
-// smallest is left out (2^-17), with three what is below 2^-25.  In fp32 all is fp32.
+// The products of an input of 16 bits with an fp32 value take the value as two parts, the
+// second the rest of the first.  Two bf16 parts are 16 bits of it at least (an error of
+// 2^-17 of the value), with the range of fp32; a third part, the rest of both, holds all of
+// it.  An fp16 input beside them is two bf16 parts itself, exactly; the smallest of its
+// products is left out (2^-17).  Where values can be brought near each other by a power of
+// two they are two fp16 parts beside the input as it is: 22 bits of the largest, and of
+// all that are within 2^-16 of it.  In fp32 all is fp32.
 
 struct Parts {
     bf16x8 hi, lo;
@@ -102,7 +104,23 @@ __device__ inline bf16x8 third(const f32x8 &v, const Parts &p) {
     return r;
 }
 
-// What an fp32 value is held as beside inputs of type E, and the inputs beside it.
+struct Halves {
+    f16x8 hi, lo;
+};
+// of values below 2^15
+__device__ inline Halves halve(const f32x8 &v) {
+    Halves p;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        p.hi[i] = (f16)v[i];
+        p.lo[i] = (f16)(v[i] - (float)p.hi[i]);
+    }
+    return p;
+}
+
+// What an fp32 value is held as beside inputs of type E, and the inputs beside it: of any
+// size (Value, Input), and of the state, whose columns have a scale in fp16 (Scaled,
+// Beside).
 template <typename E>
 struct Mixed {
     typedef Parts Value;
@@ -116,11 +134,10 @@ struct Mixed {
     __device__ static f32x4 mma(const Input &a, const Value &b, f32x4 c) {
         return finc_seq::mma(a, b.hi, finc_seq::mma(a, b.lo, c));
     }
-    // what the third part adds
-    __device__ static bf16x8 rest(const f32x8 &v, const Value &p) { return third(v, p); }
-    __device__ static f32x4 mma_rest(const Input &a, const Value &, bf16x8 r, f32x4 c) {
-        return finc_seq::mma(a, r, c);
-    }
+    typedef Value Scaled;
+    typedef Input Beside;
+    __device__ static Scaled scaled(const f32x8 &v) { return split(v); }
+    __device__ static Beside beside(const Frag<E> &v) { return v; }
 };
 template <>
 struct Mixed<f16> {
@@ -135,9 +152,15 @@ struct Mixed<f16> {
         c = finc_seq::mma(a.hi, b.lo, c);
         return finc_seq::mma(a.hi, b.hi, c);
     }
-    __device__ static bf16x8 rest(const f32x8 &v, const Value &p) { return third(v, p); }
-    __device__ static f32x4 mma_rest(const Parts &a, const Parts &b, bf16x8 r, f32x4 c) {
-        return finc_seq::mma(a.hi, r, finc_seq::mma(a.lo, b.lo, c));
+    typedef Halves Scaled;
+    typedef f16x8 Beside;
+    __device__ static Scaled scaled(const f32x8 &v) { return halve(v); }
+    __device__ static Beside beside(const f16x8 &v) { return v; }
+    __device__ static f32x4 mma(const Halves &a, const f16x8 &b, f32x4 c) {
+        return finc_seq::mma(a.hi, b, finc_seq::mma(a.lo, b, c));
+    }
+    __device__ static f32x4 mma(const f16x8 &a, const Halves &b, f32x4 c) {
+        return finc_seq::mma(a, b.hi, finc_seq::mma(a, b.lo, c));
     }
 };
 template <>
@@ -149,8 +172,10 @@ struct Mixed<float> {
     __device__ static f32x4 mma(const f32x8 &a, const f32x8 &b, f32x4 c) {
         return finc_seq::mma(a, b, c);
     }
-    __device__ static int rest(const f32x8 &, const Value &) { return 0; }
-    __device__ static f32x4 mma_rest(const f32x8 &, const f32x8 &, int, f32x4 c) { return c; }
+    typedef f32x8 Scaled;
+    typedef f32x8 Beside;
+    __device__ static Scaled scaled(const f32x8 &v) { return v; }
+    __device__ static Beside beside(const f32x8 &v) { return v; }
 };
 
 }  // namespace finc_seq

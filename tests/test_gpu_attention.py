@@ -138,6 +138,13 @@ CASES = [  # B, L, H, G, DK, DV, options, type, view
     (1, 1100, 2, 2, 128, 128, "gds", BF16, None),
     (2, 1030, 1, 1, 72, 100, "gsl", F16, "rows"),
     (3, 1025, 2, 2, 40, 9, "sl", F32, None),
+    (2, 200, 2, 2, 128, 64, "gds", BF16, None),
+    (2, 300, 4, 2, 64, 128, "gdsl", F16, None),
+    (2, 600, 2, 2, 128, 64, "gdl", F16, None),
+    (3, 130, 2, 1, 40, 100, "gdsl", BF16, "rows"),
+    (1, 560, 2, 2, 64, 128, "gds", F32, "heads"),
+    (2, 140, 3, 3, 101, 61, "gdsl", F32, "rows"),
+    (2, 700, 2, 2, 128, 128, "gds", F16, None),
     (0, 5, 2, 1, 8, 8, "gdsl", BF16, None),
     (3, 0, 2, 1, 8, 12, "gdsl", F32, None),
 ]
@@ -148,6 +155,31 @@ def test_forward_and_gradients(B, L, H, G, DK, DV, opt, kind, view):
     t = inputs(B, L, H, G, DK, DV, opt, kind, seed=L + DK)
     got, want = run(t, kind, view)
     check(got, want, kind, t)
+
+
+@pytest.mark.parametrize("L,D", [(200, 128), (600, 64)])
+def test_fp16_columns_of_all_sizes(L, D):
+    """Values that differ by 2^30 from column to column and from block to block, columns of
+    zeros, states far above fp16's range, an empty column that fills later."""
+    t = inputs(2, L, 2, 2, D, D, "gds", F16, seed=D)
+    size = torch.exp2(torch.randint(-12, 13, (2, 1, 2, D), generator=torch.Generator().manual_seed(1)))
+    t["v"] = (t["v"].double() * size).to(F16)
+    t["v"][:, 64:128] *= 2.0 ** -10
+    t["v"][:, :, :, 3] = 0
+    t["v"][:, : L // 2, :, 5] = 0
+    t["state"][:, :, :, 1] *= 2.0 ** 60
+    t["state"][:, :, :, 2:6] = 0
+    t["state"][:, :, :, 6] *= 2.0 ** -90
+    t["g"][:, 130] = -3.0
+    got, want = run(t, F16, train=False)
+    # column by column: each has its own size
+    for d in range(D):
+        y, end = want["y"][..., d], want["end"][..., d]
+        if d == 1:      # past fp16's largest value from the start on
+            assert not torch.isfinite(got["y"][:, 0, :, 1]).any()
+        else:
+            rows.close(got["y"][..., d], y, f"y {d}", F16)
+        rows.close(got["end"][..., d], end, f"end {d}", F16)
 
 
 @pytest.mark.parametrize("kind", [F32, BF16])
