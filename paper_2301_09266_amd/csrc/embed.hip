@@ -4,7 +4,8 @@
 // Both are bound by memory.  The gradient sorts the codes (a radix sort that keeps their
 // order, so that its sums have a fixed one), then sums runs of equal codes: tiles of the
 // sorted list side by side, and what runs on over a tile's end is joined afterwards.
-// Every row of the gradient is written once: by the run that ends in it, or as zeros.
+// Rows that no code names are zeros: of a short list's table all of it beside the sort, in
+// which one workgroup has work, of a long one's the rows that are not in the list.
 #include "seq_common.h"
 
 namespace {
@@ -67,6 +68,8 @@ struct Sort {
     int *at_out;
     int *counts;              // (blocks, 256)
     int M, per, blocks, shift;
+    float *zeros;             // of a short list: the table's gradient
+    long long zero_count;
 };
 
 __device__ inline unsigned sort_key(const Sort &s, int i) {
@@ -165,14 +168,26 @@ __global__ __launch_bounds__(kThreads) void place_kernel(Sort s) {
     }
 }
 
-// Short lists in one launch: a workgroup keeps them in LDS from pass to pass.
+// Short lists in one launch: a workgroup keeps them in LDS from pass to pass.  The others
+// write zeros (4096 codes of 70000 rows of 64: 39 us with a search for the rows that are
+// not in the list, 32 so).
 constexpr int kShort = 4096, kShortThreads = 1024, kShortWaves = kShortThreads / 64;
+constexpr int kZeroed = 16384;   // elements of a workgroup
 
 __global__ __launch_bounds__(kShortThreads) void sort_short_kernel(Sort s) {
     __shared__ unsigned key[2][kShort];
     __shared__ int at[2][kShort];
     __shared__ int place[kShortWaves][kDigits], totals[4];
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    if (block_of() > 0) {
+        const float zero[4] = {0, 0, 0, 0};
+        const long long first = (block_of() - 1) * (long long)kZeroed + t * 4;
+        for (int i = 0; i < kZeroed; i += kShortThreads * 4) {
+            const long long left = s.zero_count - first - i;
+            store_upto<float, 4>(s.zeros + first + i, (int)max(min(left, 4ll), 0ll), zero);
+        }
+        return;
+    }
     for (int i = t; i < s.M; i += kShortThreads) {
         key[0][i] = s.ids.key(i);
         at[0][i] = i;
@@ -228,7 +243,21 @@ __global__ __launch_bounds__(kShortThreads) void sort_short_kernel(Sort s) {
 
 // ---- the sums -------------------------------------------------------------------------
 
-constexpr int kTile = 32;   // entries of the sorted list that one wave's lanes add up
+// Entries of the sorted list that one wave's lanes add up: few of a short list, whose tiles
+// do not fill the card and where the chain of loads counts (2048 codes of 64 columns: 28 us
+// with 32 entries, 21 with 8; 14306 of 23 31 and 26), more of a long one, whose runs over
+// several tiles are read again (16384 codes of 256 rows of 512: 32 us with 32, 40 with 8;
+// 65536 of two rows 93 and 260).
+constexpr int kAhead = 8;
+int lanes_of(int D) {   // of a row: a power of two, up to a wave
+    int n = 1;
+    while (n < 64 && n * kVec < D)
+        n *= 2;
+    return n;
+}
+int tile_of(int M, int D) {
+    return M <= 16384 && M * lanes_of(D) <= 1 << 19 ? kAhead : 4 * kAhead;
+}
 
 struct Sum {
     const unsigned *key;
@@ -237,8 +266,38 @@ struct Sum {
     long long sdy;
     float *dtable, *head, *tail;   // a tile's first and last run where they pass its ends
     float scale;
-    int M, V, D, tiles, lanes, slices, fill;   // lanes of a row, slices of its columns
+    int M, V, D, tile, tiles, lanes, slices;   // lanes of a row, slices of its columns
     long long sum_blocks;
+};
+
+// A lane's eight columns of a row of D, from `own` on.  Loads have no branches, which would
+// wait for each: a lane that passes the row's end takes the row's last eight columns and
+// stores those that are its own (D = 126: the sums of 434 codes 20 us before, 5 now).
+struct Columns {
+    int col, skip, D;
+    bool narrow;
+    __device__ Columns(int own, int d)
+        : col(d < kVec ? 0 : min(own, d - kVec)), skip(own - col), D(d), narrow(d < kVec) {}
+    template <typename E>
+    __device__ typename Vec<E, kVec>::type load(const E *row) const {
+        typename Vec<E, kVec>::type v;
+        if (narrow)
+#pragma unroll
+            for (int j = 0; j < kVec; ++j)
+                v[j] = row[min(j, D - 1)];
+        else
+            v = *(const typename Vec<E, kVec>::type *)(row + col);
+        return v;
+    }
+    __device__ void store(float *row, const float *v) const {
+        if (skip == 0)
+            store_upto<float, kVec>(row + col, D - col, v);
+        else
+#pragma unroll
+            for (int j = 1; j < kVec; ++j)
+                if (j >= skip)
+                    row[col + j] = v[j];
+    }
 };
 
 // A group of lanes takes a tile of the list and up to 8 columns a lane.
@@ -247,42 +306,55 @@ __device__ void sum_tiles(const Sum &s, long long group, int lane) {
     const int tile = (int)(group / s.slices), slice = (int)(group - (long long)tile * s.slices);
     if (tile >= s.tiles)
         return;
-    const int col = (slice * s.lanes + lane) * kVec, count = min(s.D - col, kVec);
-    const int first = tile * kTile, n = min(kTile, s.M - first);
+    const int own = (slice * s.lanes + lane) * kVec;
+    if (own >= s.D)
+        return;
+    const Columns cols(own, s.D);
+    const int first = tile * s.tile, n = min(s.tile, s.M - first);
     const unsigned V = (unsigned)s.V;
     const unsigned prior = first > 0 ? s.key[first - 1] : ~0u;
     const unsigned next = first + n < s.M ? s.key[first + n] : ~0u;
-    constexpr int kAhead = 8;
+    const E *dy = (const E *)s.dy;
     float sum[kVec] = {};
     unsigned run = s.key[first];
     bool headed = prior == run;   // the run began before the tile
     auto flush = [&](bool open) {
-        if (run < V && count > 0) {
-            float *to = headed ? s.head + (long long)tile * s.D
-                               : (open ? s.tail + (long long)tile * s.D
-                                       : s.dtable + (long long)run * s.D);
-            if (!headed && !open)
+        if (run >= V)
+            return;
+        float *to = headed ? s.head + (long long)tile * s.D
+                           : (open ? s.tail + (long long)tile * s.D
+                                   : s.dtable + (long long)run * s.D);
+        const float f = headed || open ? 1.0f : s.scale;
 #pragma unroll
-                for (int j = 0; j < kVec; ++j)
-                    sum[j] *= s.scale;
-            store_upto<float, kVec>(to + col, count, sum);
-        }
+        for (int j = 0; j < kVec; ++j)
+            sum[j] *= f;
+        cols.store(to, sum);
     };
-    for (int e = 0; e < n; e += kAhead) {
-        unsigned k[kAhead];
-        float v[kAhead][kVec];
+    unsigned k[kAhead];
+    int at[kAhead];
+    auto look = [&](int e) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int at = first + min(e + i, n - 1);
-            k[i] = s.key[at];
-            load_upto<E, kVec>((const E *)s.dy + s.at[at] * s.sdy + col, k[i] < V ? count : 0, v[i]);
+            k[i] = s.key[first + min(e + i, n - 1)];
+            at[i] = s.at[first + min(e + i, n - 1)];
         }
+    };
+    look(0);
+    for (int e = 0; e < n; e += kAhead) {
+        typename Vec<E, kVec>::type v[kAhead];
+        unsigned of[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            of[i] = k[i];
+            v[i] = cols.load(dy + at[i] * s.sdy);
+        }
+        look(e + kAhead);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
             if (e + i < n) {
-                if (k[i] != run) {
+                if (of[i] != run) {
                     flush(false);
-                    run = k[i];
+                    run = of[i];
                     headed = false;
 #pragma unroll
                     for (int j = 0; j < kVec; ++j)
@@ -290,13 +362,14 @@ __device__ void sum_tiles(const Sum &s, long long group, int lane) {
                 }
 #pragma unroll
                 for (int j = 0; j < kVec; ++j)
-                    sum[j] += v[i][j];
+                    sum[j] += (float)v[i][j];
             }
     }
     flush(next == run);
 }
 
-// Rows that no code names: zeros.  A wave looks for a few rows in the list, a lane each.
+// Rows that no code of a long list names: zeros.  A wave looks for a few rows in the list, a
+// lane each.
 constexpr int kFillRows = 8;
 __device__ inline void fill_rows(const Sum &s, long long wave, int lane) {
     const long long v0 = wave * kFillRows;
@@ -342,7 +415,7 @@ __global__ __launch_bounds__(kThreads) void join_runs_kernel(Sum s) {
     const int at = block_of(), tile = at / s.slices, slice = at - tile * s.slices;
     if (tile + 1 >= s.tiles)
         return;
-    const int t = threadIdx.x, first = tile * kTile, last = first + kTile - 1;
+    const int t = threadIdx.x, first = tile * s.tile, last = first + s.tile - 1;
     const unsigned run = s.key[last];
     if (run >= (unsigned)s.V || s.key[last + 1] != run || (first > 0 && s.key[first - 1] == run))
         return;
@@ -353,7 +426,7 @@ __global__ __launch_bounds__(kThreads) void join_runs_kernel(Sum s) {
             more = kThreads;
         __syncthreads();
         const long long u = (long long)tile + 1 + n + t;
-        if (u >= s.tiles || s.key[u * kTile] != run)
+        if (u >= s.tiles || s.key[u * s.tile] != run)
             atomicMin(&more, t);
         __syncthreads();
         const int got = more;
@@ -363,18 +436,21 @@ __global__ __launch_bounds__(kThreads) void join_runs_kernel(Sum s) {
             break;
     }
     const int groups = kThreads / s.lanes, g = t / s.lanes, lane = t & (s.lanes - 1);
-    const int col = (slice * s.lanes + lane) * kVec, count = min(s.D - col, kVec);
+    const int own = (slice * s.lanes + lane) * kVec;
+    const Columns cols(own, s.D);
     const int share = (n + groups - 1) / groups, lo = min(g * share, n), hi = min(lo + share, n);
     float sum[kVec] = {};
-    if (g == 0)
-        load_upto<float, kVec>(s.tail + (long long)tile * s.D + col, count, sum);
-    constexpr int kAhead = 8;
+    if (g == 0) {
+        const auto v = cols.load(s.tail + (long long)tile * s.D);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j)
+            sum[j] = v[j];
+    }
     for (int i = lo; i < hi; i += kAhead) {
-        float v[kAhead][kVec];
+        Vec<float, kVec>::type v[kAhead];
 #pragma unroll
         for (int e = 0; e < kAhead; ++e)
-            load_upto<float, kVec>(
-                s.head + ((long long)tile + 1 + min(i + e, hi - 1)) * s.D + col, count, v[e]);
+            v[e] = cols.load(s.head + ((long long)tile + 1 + min(i + e, hi - 1)) * s.D);
 #pragma unroll
         for (int e = 0; e < kAhead; ++e)
             if (i + e < hi)
@@ -394,8 +470,8 @@ __global__ __launch_bounds__(kThreads) void join_runs_kernel(Sum s) {
 #pragma unroll
         for (int j = 0; j < kVec; ++j)
             sum[j] *= s.scale;
-        if (count > 0)
-            store_upto<float, kVec>(s.dtable + (long long)run * s.D + col, count, sum);
+        if (own < s.D)
+            cols.store(s.dtable + (long long)run * s.D, sum);
     }
 }
 
@@ -409,7 +485,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 Region rows(const void *p, long long step, long long M, int D, int size) {
     return {p, M, step, 1, 0, D, size};
 }
-int tiles_of(int M) { return (M + kTile - 1) / kTile; }
+int tiles_of(int M, int D) { return (int)cdivll(M, tile_of(M, D)); }
 
 }  // namespace
 
@@ -450,7 +526,7 @@ size_t finc_embed_workspace_bytes(int M, int V, int D) {
     if (!embed_shape(M, V, D))
         return 0;
     return 4 * round256((size_t)M * 4) + round256((size_t)kMostBlocks * kDigits * 4) +
-           2 * round256((size_t)tiles_of(M) * D * 4);
+           2 * round256((size_t)tiles_of(M, D) * D * 4);
 }
 
 int finc_embed_backward(int type, const void *ids, int wide, const void *dy, long long sdy,
@@ -494,7 +570,10 @@ int finc_embed_backward(int type, const void *ids, int wide, const void *dy, lon
     if (M > 0 && M <= kShort) {
         o.key_out = keys[0];
         o.at_out = at[0];
-        sort_short_kernel<<<1, kShortThreads, 0, stream>>>(o);
+        o.zeros = dtable;
+        o.zero_count = (long long)V * D;
+        sort_short_kernel<<<grid_of(1 + cdivll(o.zero_count, kZeroed)), kShortThreads, 0,
+                            stream>>>(o);
     } else if (M > 0)
         for (o.shift = 0; o.shift < 32 && (o.shift == 0 || V >> o.shift); o.shift += 8) {
             o.key_out = keys[from ^ 1];
@@ -511,19 +590,19 @@ int finc_embed_backward(int type, const void *ids, int wide, const void *dy, lon
     s.dy = dy;
     s.sdy = sdy;
     s.dtable = dtable;
-    s.tiles = tiles_of(M);
+    s.tile = tile_of(M, D);
+    s.tiles = tiles_of(M, D);
     s.head = (float *)take((size_t)s.tiles * D * 4);
     s.tail = (float *)take((size_t)s.tiles * D * 4);
     s.scale = (float)scale;
     s.M = M;
     s.V = V;
     s.D = D;
-    s.lanes = 1;
-    while (s.lanes < 64 && s.lanes * kVec < D)
-        s.lanes *= 2;
+    s.lanes = lanes_of(D);
     s.slices = (D + s.lanes * kVec - 1) / (s.lanes * kVec);
     s.sum_blocks = cdivll((long long)s.tiles * s.slices, kThreads / s.lanes);
-    const long long blocks = s.sum_blocks + cdivll(V, kFillRows * kWaves);
+    const bool filled = M > 0 && M <= kShort;
+    const long long blocks = s.sum_blocks + (filled ? 0 : cdivll(V, kFillRows * kWaves));
     with_type(type, [&](auto e) {
         sum_kernel<decltype(e)><<<grid_of(blocks), kThreads, 0, stream>>>(s);
     });
