@@ -18,9 +18,38 @@ constexpr int kThreads = 256;
 
 // ---- activations -----------------------------------------------------------------
 
-// The normal distribution's function: half of erfc on both sides, so that far negative p
-// keep its relative precision.
-__device__ inline float normal_cdf(float p) { return 0.5f * erfcf(-0.70710678118654752f * p); }
+// The normal distribution's function and density.  Below 0 the function is exp(-p^2 / 2)
+// times a smooth function of |p| that falls as 1 / |p|: t P(t) with t = 1 / (1 + |p| / 4), P a
+// fit of degree 9 (relative error 4e-8), so that far negative p keep its relative precision
+// (1e-6 of it; the exponent's rounding is added back).  32768 x 1024 x 4096 with GELU: ERFC us
+// with the library's erfc, FIT so.
+struct Normal {
+    float cdf, density;
+};
+__device__ inline Normal normal(float p) {
+    const float x = __builtin_fminf(__builtin_fabsf(p), 1e15f);
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, x, 1.0f));
+    float r = 0.019782036376224436f;
+    r = __builtin_fmaf(r, t, -0.08087742544062713f);
+    r = __builtin_fmaf(r, t, 0.09559727708714869f);
+    r = __builtin_fmaf(r, t, -0.03171769001371136f);
+    r = __builtin_fmaf(r, t, 0.0636991908558743f);
+    r = __builtin_fmaf(r, t, 0.05897512916000919f);
+    r = __builtin_fmaf(r, t, 0.08160311151676858f);
+    r = __builtin_fmaf(r, t, 0.09346635515367649f);
+    r = __builtin_fmaf(r, t, 0.09973643161775542f);
+    r = __builtin_fmaf(r, t, 0.09973556672301861f);
+    // exp(-x^2 / 2) = 2^(h + rest), in which rest is what h and its factors round away
+    constexpr float L = -0.7213475108146667f, kRest = -9.629815e-09f;
+    const float q = x * x, h = q * L;
+    float rest = __builtin_fmaf(q, L, -h);
+    rest = __builtin_fmaf(q, kRest, rest);
+    rest = __builtin_fmaf(__builtin_fmaf(x, x, -q), L, rest);
+    const float e = __builtin_amdgcn_exp2f(h);
+    const float f = __builtin_fmaf(e * 0.69314718055994531f, x < 64.0f ? rest : 0.0f, e);
+    const float low = f * (r * t), cdf = p < 0.0f ? low : 1.0f - low;
+    return {p == p ? cdf : p, 0.39894228040143268f * f};
+}
 __device__ inline float act_value(int act, float p) {
     switch (act) {
     case FINC_ACT_RELU:
@@ -28,7 +57,7 @@ __device__ inline float act_value(int act, float p) {
     case FINC_ACT_SILU:
         return silu(p);
     case FINC_ACT_GELU:
-        return __builtin_fmaxf(p, -1e30f) * normal_cdf(p);
+        return __builtin_fmaxf(p, -1e30f) * normal(p).cdf;
     default:
         return p;
     }
@@ -40,8 +69,8 @@ __device__ inline float act_grad(int act, float p) {
     case FINC_ACT_SILU:
         return silu_grad(p, sigmoid(p));
     default: {
-        const float q = __builtin_amdgcn_fmed3f(p, -1e15f, 1e15f);
-        return normal_cdf(p) + q * 0.39894228040143268f * exp_fast(-0.5f * q * q);
+        const Normal n = normal(p);
+        return __builtin_fmaf(__builtin_amdgcn_fmed3f(p, -1e15f, 1e15f), n.density, n.cdf);
     }
     }
 }
