@@ -539,7 +539,7 @@ int finc_conv1x1_inverse(const float *y, float *x, const float *Wm, int B, int C
  *    differ from each other.
  *  - Outputs overlapping inputs, the workspace or each other: FINC_EINVAL,
  *    except where a call names an alias it takes.
- *  - Deterministic: fixed summation orders, no atomics.  A row's outputs and the
+ *  - Deterministic: fixed summation orders, no atomics on sums.  A row's outputs and the
  *    gradients of its own inputs do not depend on the other rows or their number
  *    (those of the parameters, sums over the batch, depend on it through their
  *    fixed order, as do dBm and dCm, whose order over the channels it sets). */
@@ -721,8 +721,8 @@ int finc_add_norm_backward(const finc_norm_grad_args *a, hipStream_t stream);
  *   state: S before the rows, (B, H, DK, DV) fp32, or NULL for 0; state_out: S after
  *   each row's length, or NULL; may be state itself.
  *   states: finc_linear_attention_states_bytes(B, L, H, DK, DV) bytes, 256-byte
- *   aligned: the states at the starts of the parts of FINC_ATTENTION_PART positions
- *   that are worked on at once, in a private layout, which the gradients read.  NULL
+ *   aligned: the states at the starts of the parts of up to FINC_ATTENTION_PART
+ *   positions that are worked on side by side, in a private layout, which the gradients read.  NULL
  *   only where L <= FINC_ATTENTION_PART and no gradients follow.
  *   Inputs of 16 bits are multiplied exactly, and weights and states beside them
  *   with 16 bits at least, in sums of fp32 (beside fp16 inputs, fewer of a state's

@@ -21,8 +21,8 @@ constexpr int kThreads = 256;
 // The normal distribution's function and density.  Below 0 the function is exp(-p^2 / 2)
 // times a smooth function of |p| that falls as 1 / |p|: t P(t) with t = 1 / (1 + |p| / 4), P a
 // fit of degree 9 (relative error 4e-8), so that far negative p keep its relative precision
-// (1e-6 of it; the exponent's rounding is added back).  32768 x 1024 x 4096 with GELU: ERFC us
-// with the library's erfc, FIT so.
+// (1e-6 of it; the exponent's rounding is added back).  32768 x 1024 x 4096 with GELU: 444 us
+// with erfcf, 367 so, 268 without.
 struct Normal {
     float cdf, density;
 };

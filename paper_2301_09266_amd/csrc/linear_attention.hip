@@ -13,9 +13,14 @@
 //   dg_t = sum_{s >= t} (q_s . dq_s - k_s . dk_s) + <S, dS>.
 // One kernel does all four, a role a tensor.
 //
-// A workgroup takes a part of 512 positions of one head, block by block, with S in its
-// registers.  Longer rows have their parts' own sums formed first and joined by a scan,
+// A workgroup takes a part of up to 512 positions of one head, block by block, with S in
+// its registers.  Longer rows have their parts' own sums formed first and joined by a scan,
 // so that a single long row fills the card; which form is used follows from L alone.
+//
+// What bounds it: instructions.  One row of 16384 positions with 16 heads of 128 in bf16
+// takes 146 us (45 the parts' sums, 18 their joining, 90 the rows), 268 MB, 52 us by memory;
+// the vector ALU is busy 44% of the time and the matrix units 24%, with the two waves a SIMD
+// that 256 registers a lane leave.
 #include <type_traits>
 
 #include "seq_mma.h"

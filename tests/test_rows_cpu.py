@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import rows_ref as rows
+import test_kernel_resources_cpu
 from paper_2301_09266_amd import finc
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -241,7 +242,9 @@ def test_sizes():
     part = finc.ATTENTION_PART
     assert L.finc_linear_attention_states_bytes(2, 64, 3, 129, 8) == 0
     assert L.finc_linear_attention_workspace_bytes(2, 64, 3, 2, 8, 8) == 0
-    for n, parts in ((1, 1), (part, 1), (part + 1, 2), (10 * part, 10)):
+    # parts of half the length in rows of up to four
+    for n, parts in ((1, 1), (part, 1), (part + 1, 3), (4 * part, 8), (4 * part + 1, 5),
+                     (10 * part, 10)):
         size = L.finc_linear_attention_states_bytes(4, n, 8, 32, 16)
         assert size == 4 * 8 * (parts + 1) * 32 * 16 * 4 + -(-4 * 8 * parts * 4 // 256) * 256
         for G in (1, 8):
@@ -251,6 +254,17 @@ def test_sizes():
     assert L.finc_linear_grad_workspace_bytes(1, 2, 100, 40, 30) >= 100 * 30 * 2
     assert L.finc_embed_workspace_bytes(-1, 4, 4) == 0 and L.finc_embed_workspace_bytes(4, 4, 0) == 0
     assert L.finc_embed_workspace_bytes(1000, 4, 64) % 256 == 0
+
+
+def test_kernels_keep_their_registers():
+    """No scratch in the kernels of heads that fill their tiles, of aligned projections and
+    of the tables' gradients; little where heads of 128 do not."""
+    ks = {n: k for n, k in test_kernel_resources_cpu.kernels().items()
+          if re.search("attention_kernel|gemm_fast_kernel|gemm_few|10sum_kernel|join", n)}
+    assert sum("16attention_kernelI" in n for n in ks) == 48
+    for n, k in ks.items():
+        some = re.search("16attention_kernelI.*Li128ELi128ELi2ELb0ELb0", n)
+        assert k[".private_segment_fixed_size"] <= (128 if some else 0), n
 
 
 def test_host_tensors_are_refused():
