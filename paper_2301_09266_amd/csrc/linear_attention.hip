@@ -227,9 +227,12 @@ struct Scores {
     __device__ void set(const typename R::Lane &l, int row, int col, f32x4 v) {
         bf16x4 a, b;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            a[r] = (bf16)v[r];
-            b[r] = (bf16)(v[r] - (float)a[r]);
+        for (int r = 0; r < 4; r += 2) {
+            float u[2] = {v[r], v[r + 1]};
+            const bf16x2 h = part_of_two(u);
+            const bf16x2 l = __builtin_convertvector((f32x2{u[0], u[1]}), bf16x2);
+            a[r] = h[0], a[r + 1] = h[1];
+            b[r] = l[0], b[r + 1] = l[1];
         }
         *(bf16x4 *)(hi + R::there(l.half, row, col)) = a;
         *(bf16x4 *)(lo + R::there(l.half, row, col)) = b;
@@ -514,11 +517,6 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
             // the state's part, transposed: lane 16 g + m holds columns 4 g .. of row m
             f32x4 acc[4][NC];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int e = 0; e < NC; ++e)
-                    acc[q][e] = f32x4{0, 0, 0, 0};
-#pragma unroll
             for (int d = 0; d < DA / 32; ++d) {
                 __builtin_amdgcn_sched_barrier(0);
                 typename M::Scaled st[NC];
@@ -531,7 +529,7 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
                     const auto f = M::beside(R::halves(sq, l, 16 * q, 32 * d));
 #pragma unroll
                     for (int e = 0; e < NC; ++e)
-                        acc[q][e] = M::mma(st[e], f, acc[q][e]);
+                        acc[q][e] = M::mma(st[e], f, d > 0 ? acc[q][e] : f32x4{0, 0, 0, 0});
                 }
             }
             if constexpr (SCALED)
@@ -688,7 +686,8 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
                 if (exact) {
 #pragma unroll
                     for (int e = 0; e < NC; ++e) {
-                        const bf16x8 rest = third(weighted[e], v[e]);
+                        bf16x8 rest;
+                        v[e] = split(weighted[e], rest);
 #pragma unroll
                         for (int t = 0; t < DA / 16; ++t)
                             S[t][e] = mma(R::column(sk, l, 32 * j, 16 * t), rest, S[t][e]);

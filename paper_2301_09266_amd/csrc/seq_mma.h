@@ -83,25 +83,49 @@ __device__ inline Frag<E> frag_column(const E *p, int ld, int lane) {
 // two they are two fp16 parts beside the input as it is: 22 bits of the largest, and of
 // all that are within 2^-16 of it.  In fp32 all is fp32.
 
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef f16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// Two values' bf16 parts: the nearest, whose halves of a register are the fp32 values that
+// they stand for, and what they leave of `v`.  (Element by element the compiler rounds each
+// of them a second time alone to take it back.)
+__device__ inline bf16x2 part_of_two(float (&v)[2]) {
+    const bf16x2 h = __builtin_convertvector((f32x2{v[0], v[1]}), bf16x2);
+    const unsigned u = __builtin_bit_cast(unsigned, h);
+    v[0] -= __builtin_bit_cast(float, u << 16);
+    v[1] -= __builtin_bit_cast(float, u & 0xffff0000u);
+    return h;
+}
+
 struct Parts {
     bf16x8 hi, lo;
 };
 __device__ inline Parts split(const f32x8 &v) {
     Parts p;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        p.hi[i] = (bf16)v[i];
-        p.lo[i] = (bf16)(v[i] - (float)p.hi[i]);
+    for (int i = 0; i < 8; i += 2) {
+        float r[2] = {v[i], v[i + 1]};
+        const bf16x2 a = part_of_two(r);
+        const bf16x2 b = __builtin_convertvector((f32x2{r[0], r[1]}), bf16x2);
+        p.hi[i] = a[0], p.hi[i + 1] = a[1];
+        p.lo[i] = b[0], p.lo[i + 1] = b[1];
     }
     return p;
 }
-
-__device__ inline bf16x8 third(const f32x8 &v, const Parts &p) {
-    bf16x8 r;
+// The same with the rest of both.
+__device__ inline Parts split(const f32x8 &v, bf16x8 &rest) {
+    Parts p;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        r[i] = (bf16)((v[i] - (float)p.hi[i]) - (float)p.lo[i]);
-    return r;
+    for (int i = 0; i < 8; i += 2) {
+        float r[2] = {v[i], v[i + 1]};
+        const bf16x2 a = part_of_two(r), b = part_of_two(r);
+        const bf16x2 c = __builtin_convertvector((f32x2{r[0], r[1]}), bf16x2);
+        p.hi[i] = a[0], p.hi[i + 1] = a[1];
+        p.lo[i] = b[0], p.lo[i + 1] = b[1];
+        rest[i] = c[0], rest[i + 1] = c[1];
+    }
+    return p;
 }
 
 struct Halves {
@@ -111,9 +135,15 @@ struct Halves {
 __device__ inline Halves halve(const f32x8 &v) {
     Halves p;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        p.hi[i] = (f16)v[i];
-        p.lo[i] = (f16)(v[i] - (float)p.hi[i]);
+    for (int i = 0; i < 8; i += 2) {
+        const f16x2 h = __builtin_convertvector((f32x2{v[i], v[i + 1]}), f16x2);
+        unsigned u = __builtin_bit_cast(unsigned, h);
+        asm("" : "+v"(u));   // both halves from the register that holds them, as above
+        const f16x2 a = __builtin_bit_cast(f16x2, u);
+        const f32x2 r = {v[i] - (float)a[0], v[i + 1] - (float)a[1]};
+        const f16x2 b = __builtin_convertvector(r, f16x2);
+        p.hi[i] = a[0], p.hi[i + 1] = a[1];
+        p.lo[i] = b[0], p.lo[i + 1] = b[1];
     }
     return p;
 }
