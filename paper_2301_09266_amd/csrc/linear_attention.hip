@@ -446,7 +446,7 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
                     S[t][e] *= f;
             }
     };
-    if (init)
+    if (init && blocks > 0)   // an empty row's state goes on as it is
         rescale();
 
     const typename R::Lane first = R::lane(lane);

@@ -455,6 +455,25 @@ def test_offsets_past_31_bits():
     assert float(cache[:S - 1].abs().max()) == 0.0
 
 
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("L", [40, 600])
+def test_an_empty_rows_state_goes_on_as_it_is(kind, L):
+    """All of fp32's range beside each other in a column, and what is not finite."""
+    t = inputs(2, L, 1, 1, 16, 16, "gs", kind, seed=21)
+    state = t["state"].to(DEV)
+    state[0, 0, 0] = 2.0 ** 100
+    state[0, 0, 1] = 2.0 ** -100
+    state[0, 0, 2, 3] = INF
+    state[0, 0, 4, 5] = NAN
+    end = torch.empty_like(state)
+    n = torch.tensor([0, 1], dtype=torch.int32, device=DEV)
+    y = finc.linear_attention_forward(
+        t["q"].to(DEV), t["k"].to(DEV), t["v"].to(DEV), g=t["g"].to(DEV), state=state,
+        lengths=n, states=finc.linear_attention_states(2, L, 1, 16, 16, DEV), state_out=end)
+    assert torch.equal(end[0].view(torch.int32), state[0].view(torch.int32))
+    assert not y[0].any() and not y[1, 1:].any() and torch.isfinite(y[1]).all()
+
+
 def test_more_workgroups_than_a_row_of_the_grid():
     """Launches past 2^21 workgroups lie in rows of the grid, the last one partly without
     work: parts, their join and the decays' gradient; single positions.  All rows are the
