@@ -478,7 +478,7 @@ __global__ __launch_bounds__(64 * WM * WN, sizeof(E) == 2 ? 2 : 1) void gemm_fas
     typedef Stage<E, BN, WM * WN, BA> SB;
     constexpr int BK = kStep, TM = BM / WM / 16, TN = BN / WN / 16;
     __shared__ __align__(1024) char lds[STAGES][SA::kBytes + SB::kBytes];
-    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     // Blocks go to the eight dies in turns: each die takes neighbouring tiles, in groups of
@@ -733,24 +733,70 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(const E *dy, long lo
     }
 }
 
-// The blocks' sums in order: sixteen shares a column, joined in order.
-__global__ __launch_bounds__(1024) void column_sum_kernel(const float *sums, float *out, int N,
-                                                          int blocks) {
-    __shared__ float part[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = block_of() * 64 + lane;
-    const int share = (blocks + 15) / 16, lo = min(w * share, blocks), hi = min(lo + share, blocks);
+// What is left of the gradients, in one launch: the parts of the two products in order, and
+// the blocks' sums of the columns of d, in eight shares that are joined in order (as three
+// launches 17 us of the gradients of 1531 x 333 x 1000 in fp32, 8 so).
+struct Product {
+    const float *part;   // (split, M, N)
+    void *c;
+    long long sc;
+    int M, N, split, vecs, blocks;
+};
+struct Columns {
+    const float *sums;   // (rows, N)
+    float *out;
+    int rows, N, blocks;
+};
+constexpr int kColumns = 32, kShares = kThreads / kColumns;
+
+template <typename E>
+__device__ inline void sum_parts(const Product &p, int block) {
+    const long long i = block * (long long)kThreads + threadIdx.x, row = i / p.vecs;
+    if (row >= p.M)
+        return;
+    const int col = (int)(i - row * p.vecs) * 4, count = min(p.N - col, 4);
+    float v[4] = {0, 0, 0, 0};
+    for (int s = 0; s < p.split; ++s) {
+        float u[4];
+        load_upto<float, 4>(p.part + (s * (long long)p.M + row) * p.N + col, count, u);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            v[r] += u[r];
+    }
+    store_upto<E, 4>((E *)p.c + row * p.sc + col, count, v);
+}
+
+template <typename E>
+__global__ __launch_bounds__(kThreads) void grad_sums_kernel(Product dx, Product dw, Columns db) {
+    __shared__ float part[kShares][kColumns];
+    int at = block_of();
+    if (at < dx.blocks) {
+        sum_parts<E>(dx, at);
+        return;
+    }
+    at -= dx.blocks;
+    if (at < dw.blocks) {
+        sum_parts<E>(dw, at);
+        return;
+    }
+    at -= dw.blocks;
+    if (at >= db.blocks)
+        return;
+    const int lane = threadIdx.x % kColumns, w = threadIdx.x / kColumns, c = at * kColumns + lane;
+    const int share = (db.rows + kShares - 1) / kShares;
+    const int lo = min(w * share, db.rows), hi = min(lo + share, db.rows);
     float s = 0.0f;
-    if (c < N) {
+    if (c < db.N) {
 #pragma unroll 8
         for (int i = lo; i < hi; ++i)
-            s += sums[(long long)i * N + c];
+            s += db.sums[(long long)i * db.N + c];
     }
     part[w][lane] = s;
     __syncthreads();
-    if (w == 0 && c < N) {
-        for (int i = 1; i < 16; ++i)
+    if (w == 0 && c < db.N) {
+        for (int i = 1; i < kShares; ++i)
             s += part[i][lane];
-        out[c] = s;
+        db.out[c] = s;
     }
 }
 
@@ -865,15 +911,13 @@ bool few(int M, int N, int K) {
            (M == 1 || (M <= 32 && cdivll(M, 16) * N * (long long)K <= 1ll << 24));
 }
 
+// The product, or its parts in `workspace`: how many there are (1: it is done).
 template <bool AA, bool BA>
-void run_gemm(int type, Gemm o, void *workspace, hipStream_t stream) {
+int run_gemm(int type, Gemm &o, void *workspace, hipStream_t stream) {
     const int sz = type_size(type);
     const bool fast = whole(o.a, o.sa, AA ? o.M : o.K, sz) && whole(o.b, o.sb, BA ? o.N : o.K, sz);
     const Plan p = plan(o.M, o.N, o.K, sz, fast, BA);
-    o.split = p.split;
-    o.per = p.per;
-    o.tiles_m = (int)cdivll(o.M, p.dim);
-    o.tiles_n = (int)cdivll(o.N, p.dim);
+    o.split = 1;
     if (!AA && !BA && fast && few(o.M, o.N, o.K)) {
         with_type(type, [&](auto e) {
             typedef decltype(e) E;
@@ -883,22 +927,20 @@ void run_gemm(int type, Gemm o, void *workspace, hipStream_t stream) {
             else
                 gemm_few_kernel<E, 2><<<grid, 64 * kFewWaves, 0, stream>>>(o);
         });
-        return;
+        return 1;
     }
-    void *c = o.c;
+    o.split = p.split;
+    o.per = p.per;
+    o.tiles_m = (int)cdivll(o.M, p.dim);
+    o.tiles_n = (int)cdivll(o.N, p.dim);
+    Gemm part = o;
     if (p.split > 1)
-        o.c = workspace;
+        part.c = workspace;
     const dim3 grid = grid_of((long long)o.tiles_m * o.tiles_n * p.split);
-    with_type(type, [&](auto e) {
-        typedef decltype(e) E;
-        launch_gemm<E, AA, BA>(p, o, grid, stream);
-        if (p.split > 1) {
-            const int vecs = (o.N + 3) / 4;
-            split_sum_kernel<E><<<grid_of(cdivll((long long)o.M * vecs, kThreads)), kThreads, 0,
-                                  stream>>>(o, (const float *)workspace, (E *)c, vecs);
-        }
-    });
+    with_type(type, [&](auto e) { launch_gemm<decltype(e), AA, BA>(p, part, grid, stream); });
+    return p.split;
 }
+long long sum_groups(int M, int vecs) { return cdivll((long long)M * vecs, kThreads); }
 
 int sum_blocks(int M, int N) { return (int)cdivll(M, sum_rows(M, N)); }
 
@@ -951,7 +993,13 @@ int finc_linear_forward(const finc_linear_args *a, hipStream_t stream) {
     o.N = N;
     o.K = K;
     o.act = a->act;
-    run_gemm<false, false>(a->type, o, a->workspace, stream);
+    if (run_gemm<false, false>(a->type, o, a->workspace, stream) > 1)
+        with_type(a->type, [&](auto e) {
+            typedef decltype(e) E;
+            const int vecs = (N + 3) / 4;
+            split_sum_kernel<E><<<grid_of(sum_groups(M, vecs)), kThreads, 0, stream>>>(
+                o, (const float *)a->workspace, (E *)o.c, vecs);
+        });
     return launched();
 }
 
@@ -961,7 +1009,7 @@ size_t finc_linear_grad_workspace_bytes(int type, int act, int M, int K, int N) 
     const int sz = type_size(type);
     const size_t x = split_bytes(M, K, N, sz, true), w = split_bytes(N, K, M, sz, true);
     return (act != FINC_ACT_NONE ? round256((size_t)M * N * sz) : 0) +
-           round256((size_t)sum_blocks(M, N) * N * 4) + (x > w ? x : w);
+           round256((size_t)sum_blocks(M, N) * N * 4) + x + w;
 }
 
 int finc_linear_backward(const finc_linear_grad_args *a, hipStream_t stream) {
@@ -991,17 +1039,30 @@ int finc_linear_backward(const finc_linear_grad_args *a, hipStream_t stream) {
         return p;
     };
     void *d = act ? take((size_t)M * N * sz) : nullptr;
-    float *sums = (float *)take((size_t)sum_blocks(M, N) * N * 4);
     const int blocks = sum_blocks(M, N), slices = (N + 255) / 256;
+    float *sums = (float *)take((size_t)blocks * N * 4);
+    // one block's sums are the columns'
+    Columns db = {sums, a->dbias, blocks, N, 0};
+    if (a->dbias && blocks != 1)
+        db.blocks = (int)cdivll(N, kColumns);
     if (M > 0 && (act || a->dbias))
         with_type(a->type, [&](auto e) {
             typedef decltype(e) E;
             act_grad_kernel<E><<<grid_of((long long)blocks * slices), kThreads, 0, stream>>>(
                 (const E *)a->dy, a->sdy, (const E *)a->pre, a->spre, (E *)d,
-                a->dbias ? sums : nullptr, a->act, M, N, slices, sum_rows(M, N));
+                a->dbias && blocks == 1 ? a->dbias : (a->dbias ? sums : nullptr), a->act, M, N,
+                slices, sum_rows(M, N));
         });
-    if (a->dbias)
-        column_sum_kernel<<<grid_of(cdivll(N, 64)), 1024, 0, stream>>>(sums, a->dbias, N, blocks);
+    Product dx = {}, dw = {};
+    auto parts = [&](const Gemm &o, int split) {
+        Product p = {};
+        if (split > 1) {
+            const int vecs = (o.N + 3) / 4;
+            p = {(const float *)ws, o.c, o.sc, o.M, o.N, split, vecs, (int)sum_groups(o.M, vecs)};
+            take((size_t)split * o.M * o.N * 4);
+        }
+        return p;
+    };
     Gemm o = {};
     o.a = act ? d : a->dy;
     o.sa = act ? N : a->sdy;
@@ -1013,7 +1074,7 @@ int finc_linear_backward(const finc_linear_grad_args *a, hipStream_t stream) {
         o.M = M;
         o.N = K;
         o.K = N;
-        run_gemm<false, true>(a->type, o, ws, stream);
+        dx = parts(o, run_gemm<false, true>(a->type, o, ws, stream));
     }
     if (a->dw) {
         o.b = a->x;
@@ -1023,8 +1084,13 @@ int finc_linear_backward(const finc_linear_grad_args *a, hipStream_t stream) {
         o.M = N;
         o.N = K;
         o.K = M;
-        run_gemm<true, true>(a->type, o, ws, stream);
+        dw = parts(o, run_gemm<true, true>(a->type, o, ws, stream));
     }
+    const long long groups = (long long)dx.blocks + dw.blocks + db.blocks;
+    if (groups > 0)
+        with_type(a->type, [&](auto e) {
+            grad_sums_kernel<decltype(e)><<<grid_of(groups), kThreads, 0, stream>>>(dx, dw, db);
+        });
     return launched();
 }
 

@@ -226,6 +226,13 @@ def test_more_columns_than_a_row_of_the_grid():
     dx, dw, db = finc.linear_backward(dy, x, w)
     assert bool((dw[:, 0] == dy[0]).all()) and float(dx) > N / 2
     assert float(db[-1]) == 3.0 and bool((db[:-1] == 1).all())
+    del dx, dw, db
+    # 129 rows in two blocks, whose sums are joined
+    N = (1 << 26) + 65
+    dy = dy[:, -N:].expand(129, N)
+    dx, dw, db = finc.linear_backward(dy, x.expand(129, 1), w[:N])
+    assert float(db[-1]) == 387.0 and bool((db[:-1] == 129).all())
+    assert bool((dw[:-1] == 129).all())
 
 
 def test_the_binding_refuses():
