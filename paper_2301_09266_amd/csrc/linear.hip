@@ -172,16 +172,26 @@ struct Operand {
 };
 
 // Four waves, two by two.  Lanes hold four neighbouring columns of a row of C.
+template <typename E, int BM, int BN>
+struct AnyTile {
+    static constexpr int BK = 128 / sizeof(E);
+    // either operand along the sum or across it
+    static constexpr int kBytes =
+        (Operand<E, BM, BK, false>::kOuter * Operand<E, BM, BK, false>::kLd >
+                 Operand<E, BM, BK, true>::kOuter * Operand<E, BM, BK, true>::kLd
+             ? Operand<E, BM, BK, false>::kOuter * Operand<E, BM, BK, false>::kLd
+             : Operand<E, BM, BK, true>::kOuter * Operand<E, BM, BK, true>::kLd) *
+        (int)sizeof(E);
+    static_assert(BM == BN, "both operands' places");
+};
 template <typename E, int BM, int BN, bool AA, bool BA>
-__global__ __launch_bounds__(kThreads) void gemm_kernel(Gemm o) {
+__device__ __attribute__((always_inline)) inline void gemm_any(const Gemm &o, int at, char *lds) {
     constexpr int BK = 128 / sizeof(E), TM = BM / 32, TN = BN / 32;
     typedef Operand<E, BM, BK, AA> OA;
     typedef Operand<E, BN, BK, BA> OB;
-    __shared__ __align__(16) E sa[OA::kOuter * OA::kLd];
-    __shared__ __align__(16) E sb[OB::kOuter * OB::kLd];
+    E *sa = (E *)lds, *sb = (E *)(lds + AnyTile<E, BM, BN>::kBytes);
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int at = block_of();
     const int tiles = o.tiles_m * o.tiles_n;
     const int part = at / tiles;
     at -= part * tiles;
@@ -250,6 +260,12 @@ __global__ __launch_bounds__(kThreads) void gemm_kernel(Gemm o) {
             store_upto<E, 4>((E *)o.c + row * o.sc + col, count, v);
         }
     }
+}
+
+template <typename E, int BM, int BN, bool AA, bool BA>
+__global__ __launch_bounds__(kThreads) void gemm_kernel(Gemm o) {
+    __shared__ __align__(16) char lds[2 * AnyTile<E, BM, BN>::kBytes];
+    gemm_any<E, BM, BN, AA, BA>(o, block_of(), lds);
 }
 
 // ---- the product of aligned operands -------------------------------------------------
@@ -473,17 +489,16 @@ __device__ __attribute__((always_inline)) inline void emit(const Gemm &o, int pa
 }
 
 template <typename E, int BM, int BN, int WM, int WN, int STAGES, bool AA, bool BA>
-__global__ __launch_bounds__(64 * WM * WN, sizeof(E) == 2 ? 2 : 1) void gemm_fast_kernel(Gemm o) {
+__device__ __attribute__((always_inline)) inline void gemm_fast(
+    const Gemm &o, int at, char (*lds)[(BM + BN) * kStep * (int)sizeof(E)]) {
     typedef Stage<E, BM, WM * WN, AA> SA;
     typedef Stage<E, BN, WM * WN, BA> SB;
     constexpr int BK = kStep, TM = BM / WM / 16, TN = BN / WN / 16;
-    __shared__ __align__(1024) char lds[STAGES][SA::kBytes + SB::kBytes];
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     // Blocks go to the eight dies in turns: each die takes neighbouring tiles, in groups of
     // eight rows of tiles that are walked column by column, so that its cache holds both.
-    int at = block_of();
     const int tiles = o.tiles_m * o.tiles_n;
     const int part = at / tiles;
     if (part >= o.split)
@@ -577,6 +592,34 @@ __global__ __launch_bounds__(64 * WM * WN, sizeof(E) == 2 ? 2 : 1) void gemm_fas
         emit<E, true, BA>(o, part, at_lane, acc);
     else
         emit<E, false, BA>(o, part, at_lane, acc);
+}
+
+template <typename E, int BM, int BN, int WM, int WN, int STAGES, bool AA, bool BA>
+__global__ __launch_bounds__(64 * WM * WN, sizeof(E) == 2 ? 2 : 1) void gemm_fast_kernel(Gemm o) {
+    __shared__ __align__(1024) char lds[STAGES][(BM + BN) * kStep * (int)sizeof(E)];
+    gemm_fast<E, BM, BN, WM, WN, STAGES, AA, BA>(o, block_of(), lds);
+}
+
+// Both of a gradient's products in one launch, where both take the smallest tiles: each
+// alone leaves compute units without work at its start and end (1531 x 333 x 1000 in fp32:
+// 43 us one after the other, 37 so; all gradients of 1536 x 336 x 1000 46 us, 57 before).
+template <typename E, bool FAST>
+__global__ __launch_bounds__(kThreads, sizeof(E) == 2 ? 2 : 1) void gemm_pair_kernel(Gemm dx, Gemm dw,
+                                                                                   int first) {
+    const int at = block_of();
+    if constexpr (FAST) {
+        __shared__ __align__(1024) char lds[4][128 * kStep * (int)sizeof(E)];
+        if (at < first)
+            gemm_fast<E, 64, 64, 2, 2, 4, false, true>(dx, at, lds);
+        else
+            gemm_fast<E, 64, 64, 2, 2, 4, true, true>(dw, at - first, lds);
+    } else {
+        __shared__ __align__(16) char lds[2 * AnyTile<E, 64, 64>::kBytes];
+        if (at < first)
+            gemm_any<E, 64, 64, false, true>(dx, at, lds);
+        else
+            gemm_any<E, 64, 64, true, true>(dw, at - first, lds);
+    }
 }
 
 // ---- few rows -------------------------------------------------------------------------
@@ -911,34 +954,31 @@ bool few(int M, int N, int K) {
            (M == 1 || (M <= 32 && cdivll(M, 16) * N * (long long)K <= 1ll << 24));
 }
 
-// The product, or its parts in `workspace`: how many there are (1: it is done).
+// Sets the product's tiles and parts.
 template <bool AA, bool BA>
-int run_gemm(int type, Gemm &o, void *workspace, hipStream_t stream) {
+Plan planned(int type, Gemm &o) {
     const int sz = type_size(type);
     const bool fast = whole(o.a, o.sa, AA ? o.M : o.K, sz) && whole(o.b, o.sb, BA ? o.N : o.K, sz);
     const Plan p = plan(o.M, o.N, o.K, sz, fast, BA);
-    o.split = 1;
-    if (!AA && !BA && fast && few(o.M, o.N, o.K)) {
-        with_type(type, [&](auto e) {
-            typedef decltype(e) E;
-            const dim3 grid = grid_of(cdivll(o.N, 16));
-            if (o.M <= 16)
-                gemm_few_kernel<E, 1><<<grid, 64 * kFewWaves, 0, stream>>>(o);
-            else
-                gemm_few_kernel<E, 2><<<grid, 64 * kFewWaves, 0, stream>>>(o);
-        });
-        return 1;
-    }
     o.split = p.split;
     o.per = p.per;
     o.tiles_m = (int)cdivll(o.M, p.dim);
     o.tiles_n = (int)cdivll(o.N, p.dim);
-    Gemm part = o;
-    if (p.split > 1)
-        part.c = workspace;
-    const dim3 grid = grid_of((long long)o.tiles_m * o.tiles_n * p.split);
-    with_type(type, [&](auto e) { launch_gemm<decltype(e), AA, BA>(p, part, grid, stream); });
-    return p.split;
+    return p;
+}
+long long groups_of(const Gemm &o) { return (long long)o.tiles_m * o.tiles_n * o.split; }
+Gemm into(Gemm o, void *c) {
+    o.c = c;
+    return o;
+}
+
+// The product, or its parts in `workspace`.
+template <bool AA, bool BA>
+void run_gemm(int type, const Plan &p, const Gemm &o, void *workspace, hipStream_t stream) {
+    const Gemm part = into(o, o.split > 1 ? workspace : o.c);
+    with_type(type, [&](auto e) {
+        launch_gemm<decltype(e), AA, BA>(p, part, grid_of(groups_of(o)), stream);
+    });
 }
 long long sum_groups(int M, int vecs) { return cdivll((long long)M * vecs, kThreads); }
 
@@ -993,7 +1033,21 @@ int finc_linear_forward(const finc_linear_args *a, hipStream_t stream) {
     o.N = N;
     o.K = K;
     o.act = a->act;
-    if (run_gemm<false, false>(a->type, o, a->workspace, stream) > 1)
+    const Plan p = planned<false, false>(a->type, o);
+    if (p.fast && few(M, N, K)) {
+        o.split = 1;
+        with_type(a->type, [&](auto e) {
+            typedef decltype(e) E;
+            const dim3 grid = grid_of(cdivll(N, 16));
+            if (M <= 16)
+                gemm_few_kernel<E, 1><<<grid, 64 * kFewWaves, 0, stream>>>(o);
+            else
+                gemm_few_kernel<E, 2><<<grid, 64 * kFewWaves, 0, stream>>>(o);
+        });
+        return launched();
+    }
+    run_gemm<false, false>(a->type, p, o, a->workspace, stream);
+    if (o.split > 1)
         with_type(a->type, [&](auto e) {
             typedef decltype(e) E;
             const int vecs = (N + 3) / 4;
@@ -1054,37 +1108,59 @@ int finc_linear_backward(const finc_linear_grad_args *a, hipStream_t stream) {
                 slices, sum_rows(M, N));
         });
     Product dx = {}, dw = {};
-    auto parts = [&](const Gemm &o, int split) {
+    auto parts = [&](const Gemm &o) {
         Product p = {};
-        if (split > 1) {
+        if (o.split > 1) {
             const int vecs = (o.N + 3) / 4;
-            p = {(const float *)ws, o.c, o.sc, o.M, o.N, split, vecs, (int)sum_groups(o.M, vecs)};
-            take((size_t)split * o.M * o.N * 4);
+            p = {(const float *)ws, o.c, o.sc, o.M, o.N, o.split, vecs,
+                 (int)sum_groups(o.M, vecs)};
+            take((size_t)o.split * o.M * o.N * 4);
         }
         return p;
     };
-    Gemm o = {};
-    o.a = act ? d : a->dy;
-    o.sa = act ? N : a->sdy;
-    if (a->dx && M > 0) {
-        o.b = a->w;
-        o.sb = a->sw;
-        o.c = a->dx;
-        o.sc = a->sdx;
-        o.M = M;
-        o.N = K;
-        o.K = N;
-        dx = parts(o, run_gemm<false, true>(a->type, o, ws, stream));
+    Gemm x = {}, w = {};
+    Plan px = {}, pw = {};
+    x.a = w.a = act ? d : a->dy;
+    x.sa = w.sa = act ? N : a->sdy;
+    const bool any_x = a->dx && M > 0;
+    if (any_x) {
+        x.b = a->w;
+        x.sb = a->sw;
+        x.c = a->dx;
+        x.sc = a->sdx;
+        x.M = M;
+        x.N = K;
+        x.K = N;
+        px = planned<false, true>(a->type, x);
+        dx = parts(x);
     }
     if (a->dw) {
-        o.b = a->x;
-        o.sb = a->sx;
-        o.c = a->dw;
-        o.sc = a->sdw;
-        o.M = N;
-        o.N = K;
-        o.K = M;
-        dw = parts(o, run_gemm<true, true>(a->type, o, ws, stream));
+        w.b = a->x;
+        w.sb = a->sx;
+        w.c = a->dw;
+        w.sc = a->sdw;
+        w.M = N;
+        w.N = K;
+        w.K = M;
+        pw = planned<true, true>(a->type, w);
+        dw = parts(w);
+    }
+    if (any_x && a->dw && px.dim == 64 && pw.dim == 64 && px.fast == pw.fast)
+        with_type(a->type, [&](auto e) {
+            typedef decltype(e) E;
+            const Gemm ox = into(x, dx.blocks ? (void *)dx.part : x.c),
+                       ow = into(w, dw.blocks ? (void *)dw.part : w.c);
+            const dim3 grid = grid_of(groups_of(x) + groups_of(w));
+            if (px.fast)
+                gemm_pair_kernel<E, true><<<grid, kThreads, 0, stream>>>(ox, ow, (int)groups_of(x));
+            else
+                gemm_pair_kernel<E, false><<<grid, kThreads, 0, stream>>>(ox, ow, (int)groups_of(x));
+        });
+    else {
+        if (any_x)
+            run_gemm<false, true>(a->type, px, x, (void *)dx.part, stream);
+        if (a->dw)
+            run_gemm<true, true>(a->type, pw, w, (void *)dw.part, stream);
     }
     const long long groups = (long long)dx.blocks + dw.blocks + db.blocks;
     if (groups > 0)
