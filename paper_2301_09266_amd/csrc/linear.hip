@@ -880,10 +880,11 @@ const Tile kAny16[] = {{64, 4, 0.55, 0.55, 0.22}, {128, 2, 1.1, 1.1, 0.68}};
 const Tile kAny32[] = {{64, 4, 1.55, 1.55, 0.69}, {128, 2, 4.0, 4.0, 2.4}};
 
 // Tile and split of a product: the cheapest of all by that and by what a launch, a tile's
-// end and the parts of split sums cost (6 us and their way to memory and back at 4 TB/s).
-// The gradient of 2048 x 2048 weights over 16384 rows: 155 us in four parts with tiles of
-// 256, 173 in two with 128, 244 in one with 64; of 64 x 256 over 32768: 456 in one part,
-// 38 in sixteen.
+// end and the parts of split sums cost (6 us and their way to memory and back at 4 TB/s: 64
+// rows by 2048 x 2048 in bf16 take 9.2 us in four parts in a graph and 11.6 in one, but a
+// call outside one 14.4, for its second launch, and 11.9).  The gradient of
+// 2048 x 2048 weights over 16384 rows: 155 us in four parts with tiles of 256, 173 in two
+// with 128, 244 in one with 64; of 64 x 256 over 32768: 456 in one part, 38 in sixteen.
 struct Plan {
     int dim, split, per;
     bool fast;
