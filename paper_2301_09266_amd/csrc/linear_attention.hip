@@ -279,7 +279,7 @@ __device__ inline float two_to(int k) { return __builtin_bit_cast(float, (127 + 
 // outputs of the type; the code for all else next to it would take its registers.
 constexpr int threads_of(int DN, int NC) { return 4 * DN / NC; }
 // Tiles of columns of a wave: with two, what a wave reads of q and k serves twice as much
-// (one long bf16 prompt 139 us, 161 with one).
+// (one long bf16 prompt 132 us, 148 with one).
 constexpr int columns_of(int DN) { return DN / 64; }
 template <typename E, int DA, int DN, int NC, bool STATES, bool WHOLE>
 __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
@@ -972,7 +972,7 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepArgs a) {
 
 // Positions of a part, by the row's length alone: a short row's parts are halves, so that
 // there are more of them side by side (six rows of up to 1531 positions with 12 heads of
-// 100: 108 us, 160 with parts of 512).
+// 100: 86 us, 120 with parts of 512).
 int part_of(int L) { return L > kPart && L <= 4 * kPart ? kPart / 2 : kPart; }
 int parts_of(int L) { return L <= kPart ? 1 : (L + part_of(L) - 1) / part_of(L); }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
