@@ -140,6 +140,29 @@ def test_residual_in_place_and_leading_dimensions():
     assert torch.equal(y, y[:1].expand(5, 24))
 
 
+@pytest.mark.parametrize("M,K,N,kind", [(129, 96, 72, BF16), (37, 45, 50, F32), (300, 33, 64, F16),
+                                        (1000, 600, 520, F32), (4096, 128, 64, BF16)])
+@pytest.mark.parametrize("act", [0, 2])
+def test_each_gradient_alone_is_the_same(M, K, N, kind, act):
+    """Any of dx, dw and dbias may be absent from the call; the others keep their bits."""
+    dy, x, w, pre = (normal(i, *s, kind=kind).to(DEV) for i, s in
+                     enumerate(((M, N), (M, K), (N, K), (M, N))))
+    full = finc.linear_backward(dy, x, w, pre, act="silu" if act else None)
+    lib, code = finc._require_lib(), {F32: 0, BF16: 1, F16: 2}[kind]
+    ws = torch.empty(lib.finc_linear_grad_workspace_bytes(code, act, M, K, N) // 4 + 64, device=DEV)
+    for keep in ((0,), (1,), (2,), (0, 2), (1, 2), (0, 1), ()):
+        out = [torch.full_like(t, NAN) if i in keep else None for i, t in enumerate(full)]
+        at = [0 if t is None else t.data_ptr() for t in out]
+        a = finc.LINEAR_GRAD_ARGS.pack(code, act, M, K, N, dy.data_ptr(),
+                                       x.data_ptr() if 1 in keep else 0,
+                                       w.data_ptr() if 0 in keep else 0,
+                                       pre.data_ptr() if act else 0, at[0], at[1],
+                                       N, K, K, N, K, K, at[2], ws.data_ptr())
+        assert lib.finc_linear_backward(a, finc._stream()) == 0
+        for t, want in zip(out, full):
+            assert t is None or torch.equal(t, want), keep
+
+
 def test_no_rows():
     x, w = torch.zeros(0, 16, device=DEV), torch.ones(8, 16, device=DEV)
     assert finc.linear_forward(x, w, act="silu").shape == (0, 8)
