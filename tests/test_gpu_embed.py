@@ -45,6 +45,9 @@ CASES = [  # M, V, D, type, wide ids, how
     (10000, 3, 40, BF16, False, "any"), (7000, 65536, 12, F32, True, "few"),
     (300, 20, 1100, BF16, True, "one"), (0, 5, 16, F32, True, "any"),
     (2500, 65537, 4, BF16, False, "order"),
+    # tiles of 32 entries: many codes, and fewer of wide rows
+    (9000, 30, 512, BF16, False, "padding"), (17000, 300, 5, F32, True, "few"),
+    (20000, 5000, 33, F16, False, "any"), (8300, 2, 530, F32, False, "one"),
 ]
 
 
