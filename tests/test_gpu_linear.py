@@ -1,5 +1,7 @@
 """Projections through the binding against 64-bit references: types, odd sizes, views,
 activations, residuals in place, long sums in parts, streams and graphs."""
+import math
+
 import pytest
 import torch
 
@@ -90,6 +92,33 @@ def test_gradients(M, K, N, kind, wide, act):
     without = finc.linear_backward(place(dy, wide), place(x, wide), place(w, wide),
                                    place(pre, wide), act=act, bias=False)
     assert without[2] is None and torch.equal(without[0], dx) and torch.equal(without[1], dw)
+
+
+@pytest.mark.parametrize("M,K,N,kind", [(5000, 256, 2056, BF16), (4999, 264, 2050, F16),
+                                        (8000, 2040, 512, BF16), (512, 2040, 8000, F16),
+                                        (2040, 512, 2048, F32), (2048, 2044, 516, F32)])
+def test_large_tiles(M, K, N, kind):
+    """Products that fill the card with the largest tiles, with edges, in each place."""
+    x, w = normal(1, M, K, kind=kind), normal(2, N, K, kind=kind, scale=K ** -0.5)
+    b, r, dy = normal(3, N), normal(4, M, N, kind=kind), normal(5, M, N, kind=kind)
+    pre = torch.full((M, N), NAN, dtype=kind, device=DEV)
+    y = finc.linear_forward(x.to(DEV), w.to(DEV), b.to(DEV), act="silu", residual=r.to(DEV),
+                            pre_out=pre)
+
+    # A sum of n terms one after another: the i-th addition rounds a partial sum of sqrt(i / n)
+    # of the result's root mean square by up to 2^-24 of it, evenly, 2^-24 / sqrt(3) in the
+    # root mean square; all n make sqrt(n / 2) / sqrt(3) of it, which the worst of some 10^6
+    # sums passes six times.
+    def chain(n):
+        return max(CHAIN, 6 * math.sqrt(n / 6))
+
+    p = x.double() @ w.double().T + b.double()
+    ref.close(pre, p, "pre", chain(K))
+    ref.close(y, rows.act("silu", p) + r.double(), "y", chain(K))
+    dx, dw, db = finc.linear_backward(dy.to(DEV), x.to(DEV), w.to(DEV))
+    ref.close(dx, dy.double() @ w.double(), "dx", chain(N))
+    ref.close(dw, dy.double().T @ x.double(), "dw", chain(M))
+    ref.close(db, dy.double().sum(0), "dbias", chain(M))
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu", None])
