@@ -753,7 +753,11 @@ int finc_linear_attention_forward(const finc_attention_args *a, hipStream_t stre
 /* Its gradients, from the states that a forward of the same arguments wrote
  * (a->state, a->state_out and a->y are not used).  dy (B, L, H, DV), dq, dk, dv and
  * dg as q, k, v and g (dg may be absent); dstate_out: the gradient of state_out, (B,
- * H, DK, DV), or NULL for 0; dstate: the gradient of state, or NULL.  workspace:
+ * H, DK, DV), or NULL for 0; dstate: the gradient of state, or NULL.  dg is formed in
+ * sums over the part of up to FINC_ATTENTION_PART positions before its own, of terms that
+ * each pass a decay: its error goes by the largest dg there, so that it keeps its bits in
+ * a head that forgets within a position, and loses some at a single strong decay among
+ * weak ones.  workspace:
  * device, >= finc_linear_attention_workspace_bytes(B, L, H, G, DK, DV) bytes,
  * 256-byte aligned, overwritten. */
 typedef struct {

@@ -9,8 +9,12 @@
 // no factor passes 1 where the decays do not.  The gradients are the same form with
 // other tensors in the places of q, k and v, two of them against the order:
 //   dq: dy, v, k from S;   dk: v, dy, q and dv: k, q, dy from the state's gradient.
-// The decay's follows from them: with <,> over all that lies behind t,
-//   dg_t = sum_{s >= t} (q_s . dq_s - k_s . dk_s) + <S, dS>.
+// The decay's follows from them: with S and dS before a part, and a' for a without what
+// comes of the position's own pair of key and value,
+//   dg_t = <S, dS> + sum_{s < t} (k_s . dk'_s - q_s . dq'_s).
+// Every term passes a decay as dg does, so that it is as small where decays are strong: the
+// own pair would cancel and leave its rounding (at a = -9 1% of dg, at -16 twenty times it),
+// and so would a gradient of the last state in the same sums from the end.
 // One kernel does all four, a role a tensor.
 //
 // A workgroup takes a part of up to 512 positions of one head, block by block, with S in
@@ -50,7 +54,7 @@ struct Role {
     long long init_bh, init_p;
     float *keep;            // of a single part: the state before it and the one after it
     float *last;            // of a single part: the state after it
-    float *dots;            // (B H, L): dot . out
+    float *dots;            // (B H, L): dot . out, without the position's own pair
     int da, dn;             // elements of q and k, and of v
     int sd, sn;             // steps of a state's rows and columns
     float pscale, sscale, kscale;
@@ -115,11 +119,14 @@ struct Rows {
     __device__ static Frag<E> row(const E *s, const Lane &l, int r, int col) {
         return frag_row<E>(s + there(l.row, r, col));
     }
-    // Elements 4 g .. 4 g + 3 of the 16 from `col` on and of the 16 behind them.
+    // Elements 4 g .. 4 g + 3 of the 16 from `col` on, of row r + m.
+    typedef E Four __attribute__((ext_vector_type(4)));
+    __device__ static Four four(const E *s, const Lane &l, int r, int col) {
+        return *(const Four *)(s + there(l.half, r, col));
+    }
+    // The same and those of the 16 behind them.
     __device__ static Frag<E> halves(const E *s, const Lane &l, int r, int col) {
-        typedef E Four __attribute__((ext_vector_type(4)));
-        const Four a = *(const Four *)(s + there(l.half, r, col));
-        const Four b = *(const Four *)(s + there(l.half, r, col + 16));
+        const Four a = four(s, l, r, col), b = four(s, l, r, col + 16);
         return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     // Rows 8 g .. 8 g + 7 of the 32 from `r` on, of column col + m.
@@ -298,7 +305,7 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
     __shared__ __align__(16) P sp;
     __shared__ __align__(16) float wk[kPart], ghi[kPart], glo[kPart], wq[kPart];
     __shared__ double total[kBlocks];
-    __shared__ float sdot[WAVES][kBlock];
+    __shared__ float sdot[WAVES][kBlock], own[kBlock];
 
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -510,6 +517,14 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
                         e = __builtin_amdgcn_exp2f(rev ? -e : e) * o.pscale * p[r];
                         p[r] = (rev ? ki + r >= qi : ki + r <= qi) ? e : 0.0f;
                     }
+                    if (o.dots && qt == kt) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (ki + r == qi) {
+                                own[qt + m] = p[r];
+                                p[r] = 0.0f;
+                            }
+                    }
                     sp.set(lp, qt, kt, p);
                 }
             }
@@ -568,7 +583,35 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
                 }
             }
 
-            // ---- the rows, and their products with `dot`
+            // ---- the rows' products with `dot`, then their own pairs, in fp32
+            if (o.dots) {
+                const typename RV::Lane here = {0, afresh(first_v.half), 0, 0};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < NC; ++e)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float u = acc[q][e][r] * (float)dot[q][e][r];
+                            sum += WHOLE || n0 + 16 * e + 4 * g + r < o.dn ? u : 0.0f;
+                        }
+                    sum += __shfl_xor(sum, 16);
+                    sum += __shfl_xor(sum, 32);
+                    if (g == 0)
+                        sdot[w][16 * q + m] = sum;
+                    const float u = own[16 * q + m];
+#pragma unroll
+                    for (int e = 0; e < NC; ++e) {
+                        const auto x = RV::four(sv, here, 16 * q, n0 + 16 * e);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            acc[q][e][r] = __builtin_fmaf(u, (float)x[r], acc[q][e][r]);
+                    }
+                }
+            }
+
+            // ---- the rows
             const int rows = have - c * kBlock;   // past them: 0
             const long long row0 = b * o.ob + (t0 + c * kBlock) * o.ot + h * o.oh;
             if constexpr (WHOLE) {
@@ -612,23 +655,6 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
                                 store_upto<E, 4>((E *)o.out + i, count, x);
                         }
                     }
-            }
-            if (o.dots) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < NC; ++e)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const float u = acc[q][e][r] * (float)dot[q][e][r];
-                            sum += WHOLE || n0 + 16 * e + 4 * g + r < o.dn ? u : 0.0f;
-                        }
-                    sum += __shfl_xor(sum, 16);
-                    sum += __shfl_xor(sum, 32);
-                    if (g == 0)
-                        sdot[w][16 * q + m] = sum;
-                }
             }
         }
 
@@ -799,66 +825,62 @@ __global__ __launch_bounds__(256) void join_kernel(float *buf, const float *deca
         last[bh * (long long)size + i] = s;
 }
 
-// dg of a part: the sums from its end, and what passes over its end.
+// dg of a part: what passes its start, and the sums from there on.
 template <typename E>
 __global__ __launch_bounds__(256) void decay_grad_kernel(
     const float *qdots, const float *kdots, const float *states, const float *grads, long long gbh,
-    const float *after, E *dg, long long sb, long long st, long long sh, const int *lengths,
-    int size, int BH, int L, int H, int parts, int span) {
+    int first, E *dg, long long sb, long long st, long long sh, const int *lengths, int size,
+    int BH, int L, int H, int parts, int span) {
     __shared__ double sums[256];
     const int at = block_of(), bh = at / parts, part = at - bh * parts;
     if (bh >= BH)
         return;
     const int b = bh / H, h = bh - b * H, tid = threadIdx.x;
     const int end = lengths ? min(max(lengths[b], 0), L) : L;
-    const float *s = states + (bh * (long long)(parts + 1) + part + 1) * size;
-    const float *x = part + 1 < parts ? grads + bh * gbh + part * (long long)size
-                                      : (after ? after + bh * (long long)size : nullptr);
-    double over = 0.0;
-    if (x) {
-        // four sums of fp32 side by side, of 16 products each at most
-        float part[4] = {0, 0, 0, 0};
-        for (int i = 4 * tid; i < size; i += 1024) {
-            float u[4], v[4];
-            load_upto<float, 4>(s + i, size - i, u);
-            load_upto<float, 4>(x + i, size - i, v);
+    // the state before the part and its gradient, the first part's at `first`
+    const float *s = states + (bh * (long long)(parts + 1) + part) * size;
+    const float *x = grads + bh * gbh + (part > 0 ? part - 1 : first) * (long long)size;
+    // four sums of fp32 side by side, of 16 products each at most
+    float some[4] = {0, 0, 0, 0};
+    for (int i = 4 * tid; i < size; i += 1024) {
+        float u[4], v[4];
+        load_upto<float, 4>(s + i, size - i, u);
+        load_upto<float, 4>(x + i, size - i, v);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                part[r] = __builtin_fmaf(u[r], v[r], part[r]);
-        }
-        over = ((double)part[0] + part[1]) + ((double)part[2] + part[3]);
+        for (int r = 0; r < 4; ++r)
+            some[r] = __builtin_fmaf(u[r], v[r], some[r]);
     }
-    sums[tid] = over;
+    sums[tid] = ((double)some[0] + some[1]) + ((double)some[2] + some[3]);
     __syncthreads();
     for (int d = 128; d > 0; d /= 2) {
         if (tid < d)
             sums[tid] += sums[tid + d];
         __syncthreads();
     }
-    over = sums[0];
+    const double over = sums[0];
     __syncthreads();
-    // the sums from position t on: two positions a thread
+    // the sums of the positions before t: two positions a thread
     const int t0 = part * span + 2 * tid;
     double v[2];
     for (int j = 0; j < 2; ++j) {
         const int t = t0 + j;
         const long long i = bh * (long long)L + t;
-        v[j] = t < end && 2 * tid + j < span ? (double)qdots[i] - kdots[i] : 0.0;
+        v[j] = t < end && 2 * tid + j < span ? (double)kdots[i] - qdots[i] : 0.0;
     }
     sums[tid] = v[0] + v[1];
     __syncthreads();
     for (int d = 1; d < 256; d *= 2) {
-        const double u = tid + d < 256 ? sums[tid + d] : 0.0;
+        const double u = tid >= d ? sums[tid - d] : 0.0;
         __syncthreads();
         sums[tid] += u;
         __syncthreads();
     }
-    const double behind = tid + 1 < 256 ? sums[tid + 1] : 0.0;
+    const double before = tid > 0 ? sums[tid - 1] : 0.0;
     for (int j = 0; j < 2; ++j) {
         const int t = t0 + j;
         if (t < L && 2 * tid + j < span)
             dg[b * sb + t * st + h * sh] =
-                (E)(t < end ? (float)(over + behind + (j ? v[1] : v[0] + v[1])) : 0.0f);
+                (E)(t < end ? (float)(over + before + (j ? v[0] : 0.0)) : 0.0f);
     }
 }
 
@@ -1204,6 +1226,8 @@ size_t finc_linear_attention_workspace_bytes(int B, int L, int H, int G, int DK,
     size_t n = 2 * round256(bl * 4);   // the rows' products for dg
     if (parts_of(L) > 1)
         n += finc_linear_attention_states_bytes(B, L, H, DK, DV);
+    else
+        n += round256((size_t)B * H * DK * DV * 4);   // the gradient of the state before them
     if (G < H)
         n += 2 * round256(bl * DK * 4);
     return n;
@@ -1321,7 +1345,9 @@ int finc_linear_attention_backward(const finc_attention_args *a, const finc_atte
     } else {
         rv.init = rk.init = g->dstate_out;
         rv.init_bh = rk.init_bh = size;
-        rv.last = g->dstate;
+        if (!g->dstate && dots)
+            dstates = take((size_t)s.BH * size * 4);
+        rv.last = g->dstate ? g->dstate : dstates;
         rv.exact = true;
     }
     if (L == 0 && !g->dstate)
@@ -1341,9 +1367,9 @@ int finc_linear_attention_backward(const finc_attention_args *a, const finc_atte
         }
         if (dots)
             decay_grad_kernel<E><<<grid_of((long long)s.BH * s.parts), 256, 0, stream>>>(
-                qdots, kdots, a->states, dstates, (s.parts + 1) * size, g->dstate_out,
-                (E *)g->dg.p, g->dg.sb, g->dg.st, g->dg.sh, a->lengths, (int)size, s.BH, L, H,
-                s.parts, s.part);
+                qdots, kdots, a->states, s.parts > 1 ? dstates : rv.last,
+                s.parts > 1 ? (s.parts + 1) * size : size, s.parts > 1 ? s.parts : 0, (E *)g->dg.p,
+                g->dg.sb, g->dg.st, g->dg.sh, a->lengths, (int)size, s.BH, L, H, s.parts, s.part);
     });
     return launched();
 }

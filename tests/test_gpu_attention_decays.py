@@ -1,0 +1,116 @@
+"""The decays' gradient of linear attention where it is small: heads that forget within a
+few positions, each held to its own size, and decays that clear the state."""
+import math
+
+import pytest
+import torch
+
+import rows_ref as rows
+import seq_ref as ref
+from gpu_util import DEV
+from paper_2301_09266_amd import finc
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+NAN, INF = float("nan"), float("inf")
+
+
+def inputs(B, L, H, G, DK, DV, kind, seed, state=True, dend=True, ragged=False):
+    r = torch.Generator().manual_seed(seed)
+    normal = lambda *s: torch.randn(*s, generator=r, dtype=torch.float64)  # noqa: E731
+    lengths = torch.randint(1, L + 1, (B,), generator=r, dtype=torch.int32)
+    lengths[0] = L
+    return dict(q=normal(B, L, G, DK).to(kind), k=(normal(B, L, G, DK) * DK ** -0.5).to(kind),
+                v=normal(B, L, H, DV).to(kind), dy=normal(B, L, H, DV).to(kind),
+                g=(-0.02 * normal(B, L, H).exp()).to(kind),
+                state=normal(B, H, DK, DV).float() if state else None,
+                dend=normal(B, H, DK, DV).float() if dend else None,
+                lengths=lengths if ragged else None)
+
+
+def gradients(t, decay, scale=0.3):
+    """The device's gradients."""
+    d = {n: None if v is None else v.to(DEV) for n, v in t.items()}
+    B, L, H, DV = t["v"].shape
+    states = finc.linear_attention_states(B, L, H, t["q"].shape[3], DV, DEV)
+    kw = dict(g=d["g"], decay=None if decay is None else decay.to(DEV), scale=scale,
+              lengths=d["lengths"])
+    finc.linear_attention_forward(d["q"], d["k"], d["v"], state=d["state"], states=states, **kw)
+    return finc.linear_attention_backward(d["q"], d["k"], d["v"], d["dy"], states,
+                                          dstate_out=d["dend"], **kw)
+
+
+def reference(t, decay, scale=0.3):
+    x = {n: t[n].double() for n in ("q", "k", "v")}
+    g = t["g"].double().requires_grad_()
+    state = None if t["state"] is None else t["state"].double()
+    y, end = rows.attention(x["q"], x["k"], x["v"], g,
+                            None if decay is None else decay.double(), scale, state, t["lengths"])
+    loss = (y * t["dy"].double()).sum()
+    if t["dend"] is not None:
+        loss = loss + (end * t["dend"].double()).sum()
+    return torch.autograd.grad(loss, g)[0]
+
+
+def check(got, want, kind):
+    """Head by head.  dg is a sum over the positions of a part before its own of two products,
+    none of which passes dg's size in a head whose decays are alike; each is off by rows.CHAIN
+    units of 2^-24 of that at worst, and 2 n such errors add up to the root of 2 n of one."""
+    got = got.double().cpu()
+    n = min(want.shape[1], finc.ATTENTION_PART)
+    size = want.square().mean(1, keepdim=True).sqrt()
+    bar = ref.U[kind] * 1.01 * want.abs() + ref.TINY[kind] + rows.CHAIN[kind] * 2.0 ** -24 * (
+        math.sqrt(2 * n) * size + want.abs())
+    off = (got - want).abs()
+    worst = (off / bar).nan_to_num(nan=0.0).amax((0, 1))   # 0 / 0 past a row's length
+    assert bool((off <= bar).all()), [f"{float(v):.2f}" for v in worst]
+
+
+STRONG = torch.tensor([-0.05, -1.0, -4.0, -9.0, -12.0, -16.0])
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("B,L,G,DK,DV,opt", [
+    (2, 100, 6, 64, 64, dict()), (2, 130, 3, 64, 64, dict(ragged=True)),
+    (1, 200, 6, 128, 128, dict(state=False)), (2, 90, 2, 40, 100, dict(dend=False)),
+    (1, 700, 6, 64, 64, dict()), (2, 600, 6, 33, 72, dict(ragged=True)),
+    (1, 2100, 2, 16, 24, dict(state=False))])
+def test_strong_decays(kind, B, L, G, DK, DV, opt):
+    """Also of fp16, whose smallest steps are some of these heads' gradients."""
+    t = inputs(B, L, 6, G, DK, DV, kind, L + DK, **opt)
+    check(gradients(t, STRONG)["dg"], reference(t, STRONG), kind)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_decays_of_all_sizes_in_a_row(kind):
+    """Positions that forget nearly all of the state between others that keep it: the bar
+    goes by the head's largest gradients there."""
+    t = inputs(2, 300, 4, 4, 64, 64, kind, 5)
+    t["g"] = (-14 * torch.rand(2, 300, 4, generator=torch.Generator().manual_seed(2)) ** 6).to(kind)
+    check(gradients(t, None)["dg"], reference(t, None), kind)
+
+
+@pytest.mark.parametrize("L", [70, 600])
+def test_without_the_first_states_gradient(L):
+    """dg needs it also where the caller does not ask for it."""
+    B, H, D = 2, 3, 32
+    t = inputs(B, L, H, H, D, D, F32, L)
+    want = gradients(t, None)
+    d = {n: None if v is None else v.to(DEV) for n, v in t.items()}
+    lib = finc._require_lib()
+    states = finc.linear_attention_states(B, L, H, D, D, DEV)
+    finc.linear_attention_forward(d["q"], d["k"], d["v"], g=d["g"], scale=0.3, state=d["state"],
+                                  states=states)
+    out = {n: torch.full_like(d[n], NAN) for n in ("q", "k", "v", "g")}
+    n = lib.finc_linear_attention_workspace_bytes(B, L, H, H, D, D)
+    ws = torch.full((n + 256,), 0x7f, dtype=torch.uint8, device=DEV)
+    a = finc.ATTENTION_ARGS.pack(0, B, L, H, H, D, D, *finc._heads(d["q"]), *finc._heads(d["k"]),
+                                 *finc._heads(d["v"]), *finc._heads(d["g"]), 0, 0, 0, 0, 0, 0, 0,
+                                 states.data_ptr(), 0, 0.3)
+    o = finc.ATTENTION_GRADS.pack(*finc._heads(d["dy"]), *finc._heads(out["q"]),
+                                  *finc._heads(out["k"]), *finc._heads(out["v"]),
+                                  *finc._heads(out["g"]), d["dend"].data_ptr(), 0, ws.data_ptr())
+    assert lib.finc_linear_attention_backward(a, o, finc._stream()) == finc.OK
+    for m in ("q", "k", "v", "g"):
+        assert torch.equal(out[m], want["d" + m]), m
+    assert bool((ws[n:] == 0x7f).all())
