@@ -757,7 +757,7 @@ int finc_linear_attention_forward(const finc_attention_args *a, hipStream_t stre
  * sums over the part of up to FINC_ATTENTION_PART positions before its own, of terms that
  * each pass a decay: its error goes by the largest dg there, so that it keeps its bits in
  * a head that forgets within a position, and loses some at a single strong decay among
- * weak ones.  workspace:
+ * weak ones; 0 where decay + g is -128 or less.  workspace:
  * device, >= finc_linear_attention_workspace_bytes(B, L, H, G, DK, DV) bytes,
  * 256-byte aligned, overwritten. */
 typedef struct {

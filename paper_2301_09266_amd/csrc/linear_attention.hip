@@ -825,12 +825,13 @@ __global__ __launch_bounds__(256) void join_kernel(float *buf, const float *deca
         last[bh * (long long)size + i] = s;
 }
 
-// dg of a part: what passes its start, and the sums from there on.
+// dg of a part: what passes its start, and the sums from there on.  Log decays that count as
+// the least one have no part in it: 0 there, not what the sums leave.
 template <typename E>
 __global__ __launch_bounds__(256) void decay_grad_kernel(
     const float *qdots, const float *kdots, const float *states, const float *grads, long long gbh,
-    int first, E *dg, long long sb, long long st, long long sh, const int *lengths, int size,
-    int BH, int L, int H, int parts, int span) {
+    int first, Tensor g, const float *decay, E *dg, long long sb, long long st, long long sh,
+    const int *lengths, int size, int BH, int L, int H, int parts, int span) {
     __shared__ double sums[256];
     const int at = block_of(), bh = at / parts, part = at - bh * parts;
     if (bh >= BH)
@@ -876,11 +877,16 @@ __global__ __launch_bounds__(256) void decay_grad_kernel(
         __syncthreads();
     }
     const double before = tid > 0 ? sums[tid - 1] : 0.0;
+    const E *gp = g.p ? head_rows<E>(g, b, h) : nullptr;
+    const float base = decay ? decay[h] : 0.0f;
     for (int j = 0; j < 2; ++j) {
         const int t = t0 + j;
-        if (t < L && 2 * tid + j < span)
-            dg[b * sb + t * st + h * sh] =
-                (E)(t < end ? (float)(over + before + (j ? v[0] : 0.0)) : 0.0f);
+        if (t >= L || 2 * tid + j >= span)
+            continue;
+        float d = 0.0f;
+        if (t < end && !(base + (gp ? (float)gp[t * g.st] : 0.0f) <= kLeast))   // NaN goes on
+            d = (float)(over + before + (j ? v[0] : 0.0));
+        dg[b * sb + t * st + h * sh] = (E)d;
     }
 }
 
@@ -1368,8 +1374,9 @@ int finc_linear_attention_backward(const finc_attention_args *a, const finc_atte
         if (dots)
             decay_grad_kernel<E><<<grid_of((long long)s.BH * s.parts), 256, 0, stream>>>(
                 qdots, kdots, a->states, s.parts > 1 ? dstates : rv.last,
-                s.parts > 1 ? (s.parts + 1) * size : size, s.parts > 1 ? s.parts : 0, (E *)g->dg.p,
-                g->dg.sb, g->dg.st, g->dg.sh, a->lengths, (int)size, s.BH, L, H, s.parts, s.part);
+                s.parts > 1 ? (s.parts + 1) * size : size, s.parts > 1 ? s.parts : 0, s.g, a->decay,
+                (E *)g->dg.p, g->dg.sb, g->dg.st, g->dg.sh, a->lengths, (int)size, s.BH, L, H,
+                s.parts, s.part);
     });
     return launched();
 }

@@ -114,3 +114,55 @@ def test_without_the_first_states_gradient(L):
     for m in ("q", "k", "v", "g"):
         assert torch.equal(out[m], want["d" + m]), m
     assert bool((ws[n:] == 0x7f).all())
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("L", [70, 600, 1100])
+def test_decays_that_clear_have_no_gradient(kind, L):
+    """Minus infinity, the type's lowest value and all else up to -128 count as -128, also as
+    the sum of both decays; -127 does not, whose gradient is as small."""
+    t = inputs(2, L, 4, 2, 16, 24, kind, L)
+    low = torch.zeros(2, L, 4, dtype=torch.bool)
+    for h, v in ((0, -INF), (1, torch.finfo(kind).min), (2, -128.0)):
+        t["g"][:, 5 + h::37, h] = v
+        low[:, 5 + h::37, h] = True
+    t["g"][:, 3::29, 3] = -127.0
+    check(gradients(t, None)["dg"], reference(t, None), kind)
+    dg = gradients(t, None)["dg"].cpu()
+    assert not dg[low].any() and bool(dg[~low].any())
+    base = torch.tensor([-1.0, -200.0, 0.0, -1.0])
+    t["g"][:, 3::29, 3] = -127.5   # of three types exactly, and -128.5 with the head's
+    low[:, :, 1] = True
+    low[:, 3::29, 3] = True
+    dg = gradients(t, base)["dg"].cpu()
+    assert not dg[low].any()
+    # a gate that is NaN is not one that clears: its row's head has no values there
+    t["g"][1, 40, 2] = NAN
+    assert bool(gradients(t, base)["dg"][1, 40, 2].isnan())
+
+
+def test_decays_without_a_gate():
+    """dg of the C entry without g: the decays' own, where the gate would be 0."""
+    B, L, H, D = 1, 90, 3, 16
+    t = inputs(B, L, H, H, D, D, F32, 9, state=False, dend=False)
+    t["g"].zero_()
+    decay = torch.tensor([-0.1, -130.0, -2.0])
+    want = gradients(t, decay)
+    assert not want["dg"][:, :, 1].any()
+    d = {n: None if v is None else v.to(DEV) for n, v in t.items()}
+    lib, at = finc._require_lib(), decay.to(DEV)
+    states = finc.linear_attention_states(B, L, H, D, D, DEV)
+    finc.linear_attention_forward(d["q"], d["k"], d["v"], decay=at, scale=0.3, states=states)
+    out = {n: torch.full_like(d[n], NAN) for n in ("q", "k", "v", "g")}
+    ws = torch.empty(lib.finc_linear_attention_workspace_bytes(B, L, H, H, D, D), dtype=torch.uint8,
+                     device=DEV)
+    none = finc._NO_HEADS
+    a = finc.ATTENTION_ARGS.pack(0, B, L, H, H, D, D, *finc._heads(d["q"]), *finc._heads(d["k"]),
+                                 *finc._heads(d["v"]), *none, *none, at.data_ptr(), 0, 0,
+                                 states.data_ptr(), 0, 0.3)
+    o = finc.ATTENTION_GRADS.pack(*finc._heads(d["dy"]), *finc._heads(out["q"]),
+                                  *finc._heads(out["k"]), *finc._heads(out["v"]),
+                                  *finc._heads(out["g"]), 0, 0, ws.data_ptr())
+    assert lib.finc_linear_attention_backward(a, o, finc._stream()) == finc.OK
+    for m in ("q", "k", "v", "g"):
+        assert torch.equal(out[m], want["d" + m]), m
