@@ -790,8 +790,8 @@ int finc_linear_attention_step(const finc_attention_step_args *a, hipStream_t st
  *   normal distribution's function of p).  y may be residual itself, with its rows'
  *   step.  workspace: device, >= finc_linear_workspace_bytes(type, M, K, N) bytes, 256-byte
  *   aligned, overwritten (NULL where that is 0).  Sums are fp32, in an order that follows
- *   from the sizes alone: other than for the other sequence operators, M has a part in
- *   it.  M N, M K, N K < 2^40 (FINC_EINVAL past them). */
+ *   from the type and the sizes alone, whatever the addresses and the rows' steps: other
+ *   than for the other sequence operators, M has a part in it.  M N, M K, N K < 2^40 (FINC_EINVAL past them). */
 enum { FINC_ACT_NONE = 0, FINC_ACT_RELU = 1, FINC_ACT_SILU = 2, FINC_ACT_GELU = 3 };
 typedef struct {
     int type, act, M, K, N;

@@ -650,7 +650,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void gemm_few_kernel(Gemm o) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
         acc[i] = f32x4{0, 0, 0, 0};
-    typedef E Eight __attribute__((ext_vector_type(8), aligned(16)));
+    typedef typename Vec<E, 8>::type Eight;
     for (int s = first; s < last; s += kFewAhead) {
         Frag<E> fb[kFewAhead], fa[kFewAhead][TM];
 #pragma unroll
@@ -857,9 +857,11 @@ bool linear_shape(int type, int act, int M, int K, int N) {
            (long long)K * N < (1ll << 40);
 }
 
-// Chunks of 16 bytes that lie whole within a row and start at multiples of 16 bytes.
-bool whole(const void *p, long long s, int n, int size) {
-    return (uintptr_t)p % 16 == 0 && s * size % 16 == 0 && (long long)n * size % 16 == 0;
+// Rows of n elements that are whole chunks of 16 bytes, and whether they also start at
+// multiples of 16 bytes.
+bool chunks(int n, int size) { return (long long)n * size % 16 == 0; }
+bool aligned(const void *p, long long s, int size) {
+    return (uintptr_t)p % 16 == 0 && s * size % 16 == 0;
 }
 
 // Square tiles of the kernels, and microseconds that 32 positions of the sum take: of a
@@ -875,7 +877,7 @@ const Tile kFast16[] = {{64, 4, 0.13, 0.45, 0.13}, {128, 2, 0.30, 0.58, 0.30},
                         {256, 1, 0.87, 0.97, 0.87}};
 // 32: 8192 x 2048 x 2048 632 with 64, 557 with 128; 1536 x 336 x 1000 19 and 31.
 const Tile kFast32[] = {{64, 4, 0.65, 0.65, 0.58}, {128, 1, 2.2, 2.2, 2.2}};
-// Operands of other alignments: 8191 x 1001 x 1003 58 and 46 in 16 bits, 177 and 159 in 32.
+// Operands of any alignment: 8191 x 1001 x 1003 58 and 46 in 16 bits, 177 and 159 in 32.
 const Tile kAny16[] = {{64, 4, 0.55, 0.55, 0.22}, {128, 2, 1.1, 1.1, 0.68}};
 const Tile kAny32[] = {{64, 4, 1.55, 1.55, 0.69}, {128, 2, 4.0, 4.0, 2.4}};
 
@@ -889,42 +891,52 @@ struct Plan {
     int dim, split, per;
     bool fast;
 };
-Plan plan(int M, int N, int K, int size, bool fast, bool across) {
-    const Tile *from = fast ? (size == 2 ? kFast16 : kFast32) : (size == 2 ? kAny16 : kAny32);
-    const int kinds = fast && size == 2 ? 3 : 2, sum = K > 0 ? K : 1;   // none: zeros
+// of parts of `per` positions of the sum
+double cost(const Tile &t, int M, int N, int parts, int per, bool across) {
+    const double tiles = (double)cdivll(M, t.dim) * cdivll(N, t.dim);
+    const double n = ceil(tiles * parts / 256.0), side = n < t.side ? n : t.side;
+    const double step = (across ? t.across : t.alone) > side * t.each ? (across ? t.across : t.alone)
+                                                                      : side * t.each;
+    const double us = ceil(n / t.side) * (per / 32.0) * step + n * t.dim * t.dim / 16384.0;
+    return parts > 1 ? us + (6.0 + parts * (double)M * N * 8.0 / 4e6) : us;
+}
+// The parts, which set the sums' order, follow from type and sizes alone: operands whose rows
+// are whole chunks have the same ones at every address, also where they go by the kernel of any
+// alignment, whose best ones are others (64 rows by 2048 x 2048 in bf16 an element behind such an
+// address: 23 us, 14 with parts of its own; 256 by 4096 x 4096 53 and 33; most sizes the same).
+Plan plan(int M, int N, int K, int size, bool whole, bool across, bool fast) {
+    const Tile *from = whole ? (size == 2 ? kFast16 : kFast32) : (size == 2 ? kAny16 : kAny32);
+    const int kinds = whole && size == 2 ? 3 : 2, sum = K > 0 ? K : 1;   // none: zeros
     Plan best = {};
-    best.fast = fast;
     double least = 0.0;
-    for (int k = 0; k < kinds; ++k) {
-        const Tile &t = from[k];
-        const double tiles = (double)cdivll(M, t.dim) * cdivll(N, t.dim);
+    for (int k = 0; k < kinds; ++k)
         for (int split = 1; split <= 64; split *= 2) {
             if (split > 1 && sum / split < 128)
                 break;
             const int per = (int)(cdivll(cdivll(sum, split), 64) * 64);
             const int parts = (int)cdivll(sum, per);
-            const double n = ceil(tiles * parts / 256.0), side = n < t.side ? n : t.side;
-            const double step = (across ? t.across : t.alone) > side * t.each
-                                    ? (across ? t.across : t.alone)
-                                    : side * t.each;
-            double us = ceil(n / t.side) * (per / 32.0) * step + n * t.dim * t.dim / 16384.0;
-            if (parts > 1)
-                us += 6.0 + parts * (double)M * N * 8.0 / 4e6;
+            const double us = cost(from[k], M, N, parts, per, across);
             if (best.dim == 0 || us < least) {
                 least = us;
-                best.dim = t.dim;
+                best.dim = from[k].dim;
                 best.split = parts;
                 best.per = per;
             }
         }
+    best.fast = whole && fast;
+    if (whole && !fast) {
+        const Tile *any = size == 2 ? kAny16 : kAny32;
+        best.dim = cost(any[0], M, N, best.split, best.per, across) <=
+                           cost(any[1], M, N, best.split, best.per, across)
+                       ? any[0].dim
+                       : any[1].dim;
     }
     return best;
 }
-// For operands of any alignment.
-size_t split_bytes(int M, int N, int K, int size, bool across) {
-    const int a = plan(M, N, K, size, true, across).split,
-              b = plan(M, N, K, size, false, across).split, most = a > b ? a : b;
-    return most > 1 ? round256((size_t)most * M * N * 4) : 0;
+// whole: both operands' rows are whole chunks.
+size_t split_bytes(int M, int N, int K, int size, bool whole, bool across) {
+    const int split = plan(M, N, K, size, whole, across, true).split;
+    return split > 1 ? round256((size_t)split * M * N * 4) : 0;
 }
 
 template <typename E, bool AA, bool BA>
@@ -959,8 +971,9 @@ bool few(int M, int N, int K) {
 template <bool AA, bool BA>
 Plan planned(int type, Gemm &o) {
     const int sz = type_size(type);
-    const bool fast = whole(o.a, o.sa, AA ? o.M : o.K, sz) && whole(o.b, o.sb, BA ? o.N : o.K, sz);
-    const Plan p = plan(o.M, o.N, o.K, sz, fast, BA);
+    const Plan p = plan(o.M, o.N, o.K, sz,
+                        chunks(AA ? o.M : o.K, sz) && chunks(BA ? o.N : o.K, sz), BA,
+                        aligned(o.a, o.sa, sz) && aligned(o.b, o.sb, sz));
     o.split = p.split;
     o.per = p.per;
     o.tiles_m = (int)cdivll(o.M, p.dim);
@@ -990,7 +1003,8 @@ int sum_blocks(int M, int N) { return (int)cdivll(M, sum_rows(M, N)); }
 extern "C" {
 
 size_t finc_linear_workspace_bytes(int type, int M, int K, int N) {
-    return linear_shape(type, FINC_ACT_NONE, M, K, N) ? split_bytes(M, N, K, type_size(type), false)
+    const int sz = type_size(type);
+    return linear_shape(type, FINC_ACT_NONE, M, K, N) ? split_bytes(M, N, K, sz, chunks(K, sz), false)
                                                        : 0;
 }
 
@@ -1035,7 +1049,7 @@ int finc_linear_forward(const finc_linear_args *a, hipStream_t stream) {
     o.K = K;
     o.act = a->act;
     const Plan p = planned<false, false>(a->type, o);
-    if (p.fast && few(M, N, K)) {
+    if (few(M, N, K)) {
         o.split = 1;
         with_type(a->type, [&](auto e) {
             typedef decltype(e) E;
@@ -1062,7 +1076,8 @@ size_t finc_linear_grad_workspace_bytes(int type, int act, int M, int K, int N) 
     if (!linear_shape(type, act, M, K, N))
         return 0;
     const int sz = type_size(type);
-    const size_t x = split_bytes(M, K, N, sz, true), w = split_bytes(N, K, M, sz, true);
+    const bool whole = chunks(N, sz) && chunks(K, sz);
+    const size_t x = split_bytes(M, K, N, sz, whole, true), w = split_bytes(N, K, M, sz, whole, true);
     return (act != FINC_ACT_NONE ? round256((size_t)M * N * sz) : 0) +
            round256((size_t)sum_blocks(M, N) * N * 4) + x + w;
 }
