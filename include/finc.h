@@ -829,8 +829,8 @@ int finc_embed_forward(int type, int ttype, const void *ids, int wide, const voi
                        hipStream_t stream);
 
 /* The table's gradient: dtable[v] = scale times the sum of the rows dy[m] (M, D) with
- * ids[m] = v, in fp32 and in a fixed order, 0 for a row that no id names; (V, D) fp32,
- * contiguous.  workspace: device, >= finc_embed_workspace_bytes(M, V, D) bytes, 256-byte
+ * ids[m] = v, in fp32 and in an order that follows from the sorted ids alone (equal ones
+ * as they stand in the list), 0 for a row that no id names; (V, D) fp32, contiguous.  workspace: device, >= finc_embed_workspace_bytes(M, V, D) bytes, 256-byte
  * aligned, overwritten. */
 size_t finc_embed_workspace_bytes(int M, int V, int D);
 int finc_embed_backward(int type, const void *ids, int wide, const void *dy, long long sdy,
