@@ -1002,7 +1002,7 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepArgs a) {
 // there are more of them side by side (six rows of up to 1531 positions with 12 heads of
 // 100: 86 us, 120 with parts of 512).
 int part_of(int L) { return L > kPart && L <= 4 * kPart ? kPart / 2 : kPart; }
-int parts_of(int L) { return L <= kPart ? 1 : (L + part_of(L) - 1) / part_of(L); }
+int parts_of(int L) { return L <= kPart ? 1 : (L - 1) / part_of(L) + 1; }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 bool attention_shape(int type, int B, int L, int H, int G, int DK, int DV) {
