@@ -823,7 +823,9 @@ int finc_linear_backward(const finc_linear_grad_args *a, hipStream_t stream);
 
 /* Rows of a table: y[m] = scale table[ids[m]], of (V, D) rows st elements apart of
  * ttype (the type itself or FINC_F32); ids: M ints, or 64-bit ones with wide; an id
- * outside [0, V) is padding: its row is 0, and it takes part in no gradient. */
+ * outside [0, V) is padding: its row is 0, and it takes part in no gradient.  M, V <
+ * 2^30, D <= 2^31 - 512, and in rows of c = ceil(D / 8) M c < 2^31, V c < 2^37
+ * (FINC_EINVAL past them). */
 int finc_embed_forward(int type, int ttype, const void *ids, int wide, const void *table,
                        long long st, void *y, long long sy, int M, int V, int D, double scale,
                        hipStream_t stream);

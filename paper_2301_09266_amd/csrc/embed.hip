@@ -477,9 +477,11 @@ __global__ __launch_bounds__(kThreads) void join_runs_kernel(Sum s) {
 
 // ---- the host ----------------------------------------------------------------------------
 
+// The columns of a row's last slice, up to 512, count within 31 bits too.
 bool embed_shape(int M, int V, int D) {
-    return M >= 0 && V >= 0 && D >= 1 && (long long)M * ((D + 7) / 8) < (1ll << 31) &&
-           (long long)V * ((D + 7) / 8) < (1ll << 37) && M < (1 << 30) && V < (1 << 30);
+    return M >= 0 && V >= 0 && D >= 1 && D <= INT32_MAX - 511 &&
+           (long long)M * ((D + 7) / 8) < (1ll << 31) && (long long)V * ((D + 7) / 8) < (1ll << 37) &&
+           M < (1 << 30) && V < (1 << 30);
 }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 Region rows(const void *p, long long step, long long M, int D, int size) {
