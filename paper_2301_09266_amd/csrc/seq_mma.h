@@ -155,7 +155,6 @@ template <typename E>
 struct Mixed {
     typedef Parts Value;
     typedef bf16x8 Input;
-    __device__ static Value value(const f32x8 &v) { return split(v); }
     __device__ static Input input(const Frag<E> &v) { return v; }
     // a's rows by b's columns
     __device__ static f32x4 mma(const Value &a, const Input &b, f32x4 c) {
@@ -173,7 +172,6 @@ template <>
 struct Mixed<f16> {
     typedef Parts Value;
     typedef Parts Input;
-    __device__ static Value value(const f32x8 &v) { return split(v); }
     __device__ static Input input(const f16x8 &v) {
         return split(__builtin_convertvector(v, f32x8));
     }
@@ -197,7 +195,6 @@ template <>
 struct Mixed<float> {
     typedef f32x8 Value;
     typedef f32x8 Input;
-    __device__ static Value value(const f32x8 &v) { return v; }
     __device__ static Input input(const f32x8 &v) { return v; }
     __device__ static f32x4 mma(const f32x8 &a, const f32x8 &b, f32x4 c) {
         return finc_seq::mma(a, b, c);
