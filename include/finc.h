@@ -727,9 +727,9 @@ int finc_add_norm_backward(const finc_norm_grad_args *a, hipStream_t stream);
  *   Inputs of 16 bits are multiplied exactly, and weights and states beside them
  *   with 16 bits at least, in sums of fp32 (beside fp16 inputs, fewer of a state's
  *   element that is below 2^-22 of the largest in its column).  Positions are worked on in blocks of 64:
- *   an infinite or NaN input, or one that overflows, leaves its row's heads without
- *   finite values from the start of its block on (in the gradients: up to its
- *   block's end), and no other outputs.
+ *   an infinite or NaN input, or one that overflows, may leave its row's heads without
+ *   finite values: y, state_out and dq from the start of its block on, dk, dv and dstate up
+ *   to its block's end, dg anywhere; and no other outputs.
  *   Requirements: B H < 2^24, B L G DK and B L H DV < 2^40 (FINC_EINVAL past them). */
 #define FINC_MAX_HEAD 128
 #define FINC_ATTENTION_PART 512
