@@ -726,7 +726,8 @@ int finc_add_norm_backward(const finc_norm_grad_args *a, hipStream_t stream);
  *   only where L <= FINC_ATTENTION_PART and no gradients follow.
  *   Inputs of 16 bits are multiplied exactly, and weights and states beside them
  *   with 16 bits at least, in sums of fp32 (beside fp16 inputs, fewer of a state's
- *   element that is below 2^-22 of the largest in its column).  Positions are worked on in blocks of 64:
+ *   element that is below 2^-22 of the largest in its column).  Positions are worked on
+ *   in blocks of 64:
  *   an infinite or NaN input, or one that overflows, may leave its row's heads without
  *   finite values: y, state_out and dq from the start of its block on, dk, dv and dstate up
  *   to its block's end, dg anywhere; and no other outputs.
@@ -791,7 +792,8 @@ int finc_linear_attention_step(const finc_attention_step_args *a, hipStream_t st
  *   step.  workspace: device, >= finc_linear_workspace_bytes(type, M, K, N) bytes, 256-byte
  *   aligned, overwritten (NULL where that is 0).  Sums are fp32, in an order that follows
  *   from the type and the sizes alone, whatever the addresses and the rows' steps: other
- *   than for the other sequence operators, M has a part in it.  M N, M K, N K < 2^40 (FINC_EINVAL past them). */
+ *   than for the other sequence operators, M has a part in it.  M N, M K, N K < 2^40
+ *   (FINC_EINVAL past them). */
 enum { FINC_ACT_NONE = 0, FINC_ACT_RELU = 1, FINC_ACT_SILU = 2, FINC_ACT_GELU = 3 };
 typedef struct {
     int type, act, M, K, N;
@@ -832,8 +834,9 @@ int finc_embed_forward(int type, int ttype, const void *ids, int wide, const voi
 
 /* The table's gradient: dtable[v] = scale times the sum of the rows dy[m] (M, D) with
  * ids[m] = v, in fp32 and in an order that follows from the sorted ids alone (equal ones
- * as they stand in the list), 0 for a row that no id names; (V, D) fp32, contiguous.  workspace: device, >= finc_embed_workspace_bytes(M, V, D) bytes, 256-byte
- * aligned, overwritten. */
+ * as they stand in the list), 0 for a row that no id names; (V, D) fp32, contiguous.
+ * workspace: device, >= finc_embed_workspace_bytes(M, V, D) bytes, 256-byte aligned,
+ * overwritten. */
 size_t finc_embed_workspace_bytes(int M, int V, int D);
 int finc_embed_backward(int type, const void *ids, int wide, const void *dy, long long sdy,
                         float *dtable, int M, int V, int D, double scale, void *workspace,

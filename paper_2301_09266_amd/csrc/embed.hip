@@ -56,8 +56,8 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(Ids ids, const R *table
 
 constexpr int kDigits = 256, kWaves = kThreads / 64;
 // Entries of a block at least, and blocks at most: a block reads every block's counts, and
-// its waves take their entries in turns (a pass over 32768 codes: 6.5 us in 64 blocks of
-// 512, 14 in 16 of 2048).
+// its waves take their entries in turns (a pass over 32768 codes, 2.8 us of counts and 6.2 of
+// places in 64 blocks of 512, 4.0 and 10.7 in 16 of 2048).
 constexpr int kSortBlock = 512, kMostBlocks = 128;
 
 struct Sort {
@@ -244,10 +244,10 @@ __global__ __launch_bounds__(kShortThreads) void sort_short_kernel(Sort s) {
 // ---- the sums -------------------------------------------------------------------------
 
 // Entries of the sorted list that one wave's lanes add up: few of a short list, whose tiles
-// do not fill the card and where the chain of loads counts (2048 codes of 64 columns: 28 us
-// with 32 entries, 21 with 8; 14306 of 23 31 and 26), more of a long one, whose runs over
-// several tiles are read again (16384 codes of 256 rows of 512: 32 us with 32, 40 with 8;
-// 65536 of two rows 93 and 260).
+// do not fill the card and where the chain of loads counts (2048 codes of 64 columns: 26 us
+// with 32 entries, 21 with 8; 14306 of 16384 rows of 23 46 and 39), more of a long one, whose
+// runs over several tiles are read again (16384 codes of 256 rows of 512: 31 us with either;
+// 65536 of two rows 75 with 32, 183 with 8).
 constexpr int kAhead = 8;
 int lanes_of(int D) {   // of a row: a power of two, up to a wave
     int n = 1;

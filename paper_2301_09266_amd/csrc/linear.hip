@@ -718,6 +718,9 @@ __global__ __launch_bounds__(kThreads) void split_sum_kernel(Gemm o, const float
 }
 
 // ---- d = dy act'(pre), and the sums of its columns -----------------------------------
+// d is rounded to the type for the products, whose matrix instructions take no more: in two
+// parts both would take twice the time.  The rounding adds to that of dx and dw (2.4e-3 of
+// them in the root mean square in bf16, 1.7e-3 where only theirs is).  The sums take it whole.
 
 // Rows of a workgroup, 8 side by side of 32 lanes of 8 columns: as many as leave two
 // workgroups a compute unit (gelu' of 1531 x 1000 in fp32: 45 us with 128 rows, 14 with 16).
@@ -885,8 +888,9 @@ const Tile kAny32[] = {{64, 4, 1.55, 1.55, 0.69}, {128, 2, 4.0, 4.0, 2.4}};
 // end and the parts of split sums cost (6 us and their way to memory and back at 4 TB/s: 64
 // rows by 2048 x 2048 in bf16 take 9.2 us in four parts in a graph and 11.6 in one, but a
 // call outside one 14.4, for its second launch, and 11.9).  The gradient of
-// 2048 x 2048 weights over 16384 rows: 155 us in four parts with tiles of 256, 173 in two
-// with 128, 244 in one with 64; of 64 x 256 over 32768: 456 in one part, 38 in sixteen.
+// 2048 x 2048 weights over 16384 rows, alone and with the joining of its parts: 150 us in four
+// parts with tiles of 256, 167 in two with 128, 242 in one with 64; of 64 x 256 over 32768: 456
+// in one part, 38 in sixteen.
 struct Plan {
     int dim, split, per;
     bool fast;

@@ -22,7 +22,7 @@
 // so that a single long row fills the card; which form is used follows from L alone.
 //
 // What bounds it: instructions.  One row of 16384 positions with 16 heads of 128 in bf16
-// takes 144 us (44 the parts' sums, 18 their joining, 86 the rows), 268 MB, 52 us by memory;
+// takes 144 us (44 the parts' sums, 18 their joining, 87 the rows), 268 MB, 52 us by memory;
 // the vector ALU is busy 41% of the time and the matrix units 25%, with the two waves a SIMD
 // that 256 registers a lane leave.
 #include <type_traits>
@@ -286,7 +286,7 @@ __device__ inline float two_to(int k) { return __builtin_bit_cast(float, (127 + 
 // outputs of the type; the code for all else next to it would take its registers.
 constexpr int threads_of(int DN, int NC) { return 4 * DN / NC; }
 // Tiles of columns of a wave: with two, what a wave reads of q and k serves twice as much
-// (one long bf16 prompt 132 us, 148 with one).
+// (that bf16 prompt, again and again on the same inputs, 128 us, 145 with one).
 constexpr int columns_of(int DN) { return DN / 64; }
 template <typename E, int DA, int DN, int NC, bool STATES, bool WHOLE>
 __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
@@ -998,9 +998,11 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepArgs a) {
 
 // ---- the host ------------------------------------------------------------------------
 
-// Positions of a part, by the row's length alone: a short row's parts are halves, so that
-// there are more of them side by side (six rows of up to 1531 positions with 12 heads of
-// 100: 86 us, 120 with parts of 512).
+// Positions of a part, by the row's length alone, so that a row's bits do not depend on the
+// batch: a short row's parts are halves, of which there are more side by side.  bf16, us with
+// parts of 256 and of 512: one row of 2048 with 4 heads of 128 48 and 76, six of 1531 with 12 of
+// 100 88 and 110; where rows fill the card, 64 with 16 heads of 128, 600 positions 481 and 532,
+// 1024 681 and 590, 2048 1261 and 1066 (heads of 64: 171 and 209, 267 and 252, 472 and 459).
 int part_of(int L) { return L > kPart && L <= 4 * kPart ? kPart / 2 : kPart; }
 int parts_of(int L) { return L <= kPart ? 1 : (L - 1) / part_of(L) + 1; }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
