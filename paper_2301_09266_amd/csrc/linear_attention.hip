@@ -52,7 +52,7 @@ struct Role {
     long long ob, ot, oh;
     const float *init;      // the state before each part, init_bh and init_p apart
     long long init_bh, init_p;
-    float *keep;            // of a single part: the state before it and the one after it
+    float *keep;            // of a single part: the state before it, 2 da dn apart
     float *last;            // of a single part: the state after it
     float *dots;            // (B H, L): dot . out, without the position's own pair
     int da, dn;             // elements of q and k, and of v
@@ -747,6 +747,8 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
             for (int t = 0; t < DA / 16; ++t)
                 S[t][e] *= two_to(-k2[e]);
 
+    // One of the two.  In a loop the addresses are formed here, not ahead of the blocks, where
+    // they would spill five of heads' of 128 registers.
     float *ends[2] = {nullptr, nullptr};
     if constexpr (STATES) {
         ends[0] = a.local + (bh * (long long)(a.parts + 1) + part) * size;
@@ -757,7 +759,6 @@ __global__ __launch_bounds__(threads_of(DN, NC), sizeof(E) == 2 ? 2 : 1)
             a.decays[(long long)bh * a.parts + part] = __builtin_amdgcn_exp2f((float)s);
         }
     } else {
-        ends[0] = o.keep ? o.keep + (bh * 2 + 1) * size : nullptr;
         ends[1] = o.last ? o.last + bh * size : nullptr;
     }
 #pragma unroll 1
