@@ -22,7 +22,7 @@
 // so that a single long row fills the card; which form is used follows from L alone.
 //
 // What bounds it: instructions.  One row of 16384 positions with 16 heads of 128 in bf16
-// takes 144 us (44 the parts' sums, 18 their joining, 87 the rows), 268 MB, 52 us by memory;
+// takes 144 us (45 the parts' sums, 18 their joining, 86 the rows), 268 MB, 52 us by memory;
 // the vector ALU is busy 41% of the time and the matrix units 25%, with the two waves a SIMD
 // that 256 registers a lane leave.
 #include <type_traits>
